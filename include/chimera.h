@@ -322,6 +322,94 @@ chimera_status chimera_debug_gemm(int32_t dtype, const void* x, const void* w, i
 chimera_status chimera_gemm_static(int32_t dtype, const void* x, const void* w, int32_t M, int32_t N, int32_t K,
                                    float* y, void* stream);
 
+/* ---- 4-bit operators -------------------------------------------------------
+ * Weights and a KV cache held in 4 bits, for decoding that is bound by the
+ * bytes it streams.
+ *
+ * Format.  Groups of 32 consecutive values (of a matrix: along the reduction
+ * K; of a K or V row: along the head dimension) share one scale byte s.  A code
+ * stands for +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^(s - 127).  s is the exponent of
+ * the group's largest magnitude minus 2, one more where that magnitude lies
+ * above 1.75 times its power of two, held to [1, 252]; codes round to nearest,
+ * ties to even, and saturate at 6.  A group that holds an infinity or a NaN
+ * gets s = 255 and all its values are NaN.  Every value is exact in bf16, and
+ * values that came out of the format go back into it unchanged.
+ *
+ * All pointers are device memory of the current device unless a declaration
+ * says otherwise; the stream must belong to it (CHIMERA_EINVAL).  The calls
+ * only enqueue kernels: they allocate nothing, do not synchronise, and may be
+ * captured into a HIP graph.  A workspace is scratch of one call: calls that
+ * may run at the same time (other streams, other graphs) need their own. */
+
+/* A K x N matrix packed for chimera_gemm_fp4: N a multiple of 16, K of 32.
+ * w is row-major [K][ldw] of `dtype`, ldw >= N, at any element; `packed` is
+ * 16-byte aligned, chimera_fp4_bytes long, its layout the library's own.
+ * chimera_fp4_unpack writes the values that `packed` stands for, rounded to
+ * `dtype` (bf16: exactly). */
+chimera_status chimera_fp4_bytes(int32_t N, int32_t K, int64_t* bytes);
+chimera_status chimera_fp4_pack(int32_t dtype, const void* w, int64_t ldw, int32_t N, int32_t K, void* packed,
+                                int64_t packed_bytes, void* stream);
+chimera_status chimera_fp4_unpack(int32_t dtype, const void* packed, int32_t N, int32_t K, void* w, int64_t ldw,
+                                  void* stream);
+
+/* y[M][N] (float32, row stride ldy) = x[M][K] (row stride ldx, of `dtype`) @ the
+ * packed matrix, summed in float32.  M in [1, 4096].  x may start at any element
+ * of its type and y at any float; rows of x at multiples of 16 bytes are
+ * fastest.  A row's result does not depend on M, and for bf16 it has the bits of
+ * the library's bf16 product with the unpacked matrix.  ws: 16-byte aligned,
+ * chimera_gemm_fp4_bytes long (NULL where that is 0). */
+chimera_status chimera_gemm_fp4_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K, int64_t* bytes);
+chimera_status chimera_gemm_fp4(int32_t dtype, const void* x, int64_t ldx, const void* packed, int32_t M, int32_t N,
+                                int32_t K, float* y, int64_t ldy, void* ws, int64_t ws_bytes, void* stream);
+
+/* A paged KV cache in 4 bits (a host struct; the call copies it).  pool:
+ * 16-byte aligned, chimera_kv4_bytes long: code rows of head_dim / 2 bytes in the
+ * order [page][K | V][head][slot], the even dimension of a pair in the low half
+ * of its byte, then scale rows of head_dim / 32 bytes in the same order.
+ * page_table (device, [batch][max_pages]): position p of sequence b lies in slot
+ * p % page_size of page page_table[b][p / page_size].  Entries whose positions a
+ * call does not touch are not read as pages and may hold anything. */
+typedef struct {
+  void* pool;
+  int64_t pool_bytes;
+  const int32_t* page_table;
+  int32_t batch, max_pages, n_pages, page_size, n_heads, head_dim;
+} chimera_kv4;
+chimera_status chimera_kv4_bytes(int32_t n_pages, int32_t page_size, int32_t n_heads, int32_t head_dim,
+                                 int64_t* bytes);
+
+/* Write `rows` K and V rows (k + r ld and v + r ld, each [n_heads][head_dim] of
+ * `dtype`, at any element) to position pos[r] of sequence seq[r].  A row whose
+ * sequence, position or page the cache does not have (seq -1 marks padding) is
+ * skipped.  Rows of one call must name distinct slots: a slot named twice ends
+ * with a mixture of its rows. */
+chimera_status chimera_kv4_append(const chimera_kv4* cache, int32_t dtype, const void* k, const void* v, int64_t ld,
+                                  const int32_t* seq, const int32_t* pos, int32_t rows, void* stream);
+/* The inverse: the values held at those positions into k_out and v_out, rounded
+ * to `dtype` (bf16: exactly).  Rows the cache does not have are left as they were. */
+chimera_status chimera_kv4_read(const chimera_kv4* cache, int32_t dtype, const int32_t* seq, const int32_t* pos,
+                                int32_t rows, void* k_out, void* v_out, int64_t ld, void* stream);
+
+/* Attention of n_nodes new tokens a sequence over the cache.  Row b n_nodes + u
+ * of q and out (row strides ldq, ldo; [n_heads][head_dim] of `dtype`) is node u of
+ * sequence b; head h reads the cache's head h / (n_heads / cache->n_heads).
+ * n_b[b] tokens are committed; node u's own K and V lie at position n_b[b] + u.
+ * It sees positions 0 .. n_b[b] - 1 and those of its ancestors and itself:
+ * out = softmax(scale q K^T) V over them, in float32, rounded once.
+ * parent (host, n_nodes entries, nullable): the tree, parent[0] = -1 and a
+ * parent before its child, at most 15 levels below the root; NULL is a chain.
+ * n_b[b] < 0 marks an empty place in the batch: its rows become zeros.  Positions
+ * that the cache does not have (a page id outside 0 .. n_pages - 1, a position
+ * past the table) are not seen; a row that sees none becomes zeros.  Nothing
+ * past the visible positions is used, whatever its bytes.  q: rows at multiples
+ * of 16 bytes; out at any element; ws: 16-byte aligned, chimera_kv4_attn_bytes
+ * long.  A row's result depends on its own position, query and visible keys only,
+ * not on n_nodes, the other nodes or the batch. */
+chimera_status chimera_kv4_attn_bytes(const chimera_kv4* cache, int32_t n_heads, int32_t n_nodes, int64_t* bytes);
+chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const void* q, int64_t ldq, const int32_t* n_b,
+                                int32_t n_heads, const int32_t* parent, int32_t n_nodes, float scale, void* out,
+                                int64_t ldo, void* ws, int64_t ws_bytes, void* stream);
+
 const char* chimera_last_error(void);
 void chimera_ctx_free(chimera_ctx* ctx);
 void chimera_kv_free(chimera_kv* kv);

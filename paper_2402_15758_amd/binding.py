@@ -44,6 +44,12 @@ class chimera_profile(ctypes.Structure):
                 ("ms_verify_median", ctypes.c_double), ("ms_step_median", ctypes.c_double)]
 
 
+class chimera_kv4(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("pool_bytes", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 _lib = None
 P = ctypes.c_void_p
 I32, I64 = ctypes.c_int32, ctypes.c_int64
@@ -78,6 +84,17 @@ _PROTOS = {
     "chimera_compaction_check_bytes": [P, PI64],
     "chimera_set_compaction_check": [P, P, I64],
     "chimera_compaction_check_read": [P, PI64, PI64],
+    "chimera_fp4_bytes": [I32, I32, PI64],
+    "chimera_fp4_pack": [I32, P, I64, I32, I32, P, I64, P],
+    "chimera_fp4_unpack": [I32, P, I32, I32, P, I64, P],
+    "chimera_gemm_fp4_bytes": [I32, I32, I32, I32, PI64],
+    "chimera_gemm_fp4": [I32, P, I64, P, I32, I32, I32, P, I64, P, I64, P],
+    "chimera_kv4_bytes": [I32, I32, I32, I32, PI64],
+    "chimera_kv4_append": [ctypes.POINTER(chimera_kv4), I32, P, P, I64, P, P, I32, P],
+    "chimera_kv4_read": [ctypes.POINTER(chimera_kv4), I32, P, P, I32, P, P, I64, P],
+    "chimera_kv4_attn_bytes": [ctypes.POINTER(chimera_kv4), I32, I32, PI64],
+    "chimera_kv4_attn": [ctypes.POINTER(chimera_kv4), I32, P, I64, P, I32, PI32, I32, ctypes.c_float, P, I64, P, I64,
+                         P],
 }
 
 
@@ -247,6 +264,63 @@ def chimera_compaction_check_read(ctx: int):
     rows, bad = I64(), I64()
     _check(lib().chimera_compaction_check_read(ctx, ctypes.byref(rows), ctypes.byref(bad)))
     return rows.value, bad.value
+
+
+def chimera_fp4_bytes(N: int, K: int) -> int:
+    out = I64()
+    _check(lib().chimera_fp4_bytes(N, K, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_fp4_pack(dtype: int, w_ptr: int, ldw: int, N: int, K: int, packed_ptr: int, packed_bytes: int,
+                     stream: int):
+    _check(lib().chimera_fp4_pack(dtype, w_ptr, ldw, N, K, packed_ptr, packed_bytes, stream))
+
+
+def chimera_fp4_unpack(dtype: int, packed_ptr: int, N: int, K: int, w_ptr: int, ldw: int, stream: int):
+    _check(lib().chimera_fp4_unpack(dtype, packed_ptr, N, K, w_ptr, ldw, stream))
+
+
+def chimera_gemm_fp4_bytes(dtype: int, M: int, N: int, K: int) -> int:
+    out = I64()
+    _check(lib().chimera_gemm_fp4_bytes(dtype, M, N, K, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_gemm_fp4(dtype: int, x_ptr: int, ldx: int, packed_ptr: int, M: int, N: int, K: int, y_ptr: int, ldy: int,
+                     ws_ptr, ws_bytes: int, stream: int):
+    _check(lib().chimera_gemm_fp4(dtype, x_ptr, ldx, packed_ptr, M, N, K, y_ptr, ldy, ws_ptr, ws_bytes, stream))
+
+
+def chimera_kv4_bytes(n_pages: int, page_size: int, n_heads: int, head_dim: int) -> int:
+    out = I64()
+    _check(lib().chimera_kv4_bytes(n_pages, page_size, n_heads, head_dim, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_kv4_append(cache: chimera_kv4, dtype: int, k_ptr: int, v_ptr: int, ld: int, seq_ptr: int, pos_ptr: int,
+                       rows: int, stream: int):
+    _check(lib().chimera_kv4_append(ctypes.byref(cache), dtype, k_ptr, v_ptr, ld, seq_ptr, pos_ptr, rows, stream))
+
+
+def chimera_kv4_read(cache: chimera_kv4, dtype: int, seq_ptr: int, pos_ptr: int, rows: int, k_ptr: int, v_ptr: int,
+                     ld: int, stream: int):
+    _check(lib().chimera_kv4_read(ctypes.byref(cache), dtype, seq_ptr, pos_ptr, rows, k_ptr, v_ptr, ld, stream))
+
+
+def chimera_kv4_attn_bytes(cache: chimera_kv4, n_heads: int, n_nodes: int) -> int:
+    out = I64()
+    _check(lib().chimera_kv4_attn_bytes(ctypes.byref(cache), n_heads, n_nodes, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_kv4_attn(cache: chimera_kv4, dtype: int, q_ptr: int, ldq: int, n_ptr: int, n_heads: int, parent,
+                     n_nodes: int, scale: float, out_ptr: int, ldo: int, ws_ptr: int, ws_bytes: int, stream: int):
+    """parent: a contiguous numpy int32 array of n_nodes entries, or None for a chain."""
+    if parent is not None and len(parent) != n_nodes:
+        raise ValueError("parent needs n_nodes entries")
+    _check(lib().chimera_kv4_attn(ctypes.byref(cache), dtype, q_ptr, ldq, n_ptr, n_heads, _i32p(parent), n_nodes,
+                                  scale, out_ptr, ldo, ws_ptr, ws_bytes, stream))
 
 
 def chimera_ctx_free(ctx: int):

@@ -103,6 +103,63 @@ void launch_tile_rows(int dtype, const void* src, int M, int K, void* dst, int m
 void launch_stage_operands(int dtype, const void* x, int M, int K, void* xd, int mtiles, const void* w, int N, void* wd,
                            hipStream_t st);
 
+// The finishing pass of a split launch that left its slices in e.part.
+void launch_gemm_finish(int dtype, const GemmShape& s, const GemmEpi& e, hipStream_t st, hipEvent_t ev_stop);
+
+// ---- products with 4-bit weights (kernels_fp4.hip) ----------------------------
+// Bytes of a packed K x N matrix, N a multiple of 16, K of 32; the reduction
+// split its layout is made for (the bf16 kernels' choice).
+int fp4_splits(int N, int K);
+int64_t fp4_bytes(int N, int K);
+// dtype: of the source matrices (row-major [K][ldw]); kind: PACK_*.
+void launch_fp4_pack(int dtype, int kind, const void* s0, const void* s1, const void* s2, int64_t ldw, int N, int K,
+                     void* dst, int H, int hd, hipStream_t st);
+void launch_fp4_unpack_rows(int dtype, const void* packed, int N, int K, void* dst, int64_t ldw, hipStream_t st);
+// Row-major x [M][ldx] -> tiled.
+void launch_tile_strided(int dtype, const void* x, int64_t ldx, int M, int K, void* dst, int mtiles, hipStream_t st);
+// Whether launches of M rows run on the bf16 kernels over the unpacked matrix.
+bool gemm_fp4_unpacks(int dtype, int M, int N);
+// s.W: the packed matrix, s.splits = fp4_splits(N, K), all columns.  ldx > 0: X
+// is row-major (at most 16 rows, 16-byte aligned rows).  unpacked: room for the
+// bf16 matrix where gemm_fp4_unpacks, else nullptr.
+void launch_gemm_fp4(int dtype, const GemmShape& s, const GemmEpi& e, int64_t ldx, void* unpacked, hipStream_t st,
+                     hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
+
+// ---- paged KV cache in 4 bits (kernels_kv4.hip) --------------------------------
+struct Kv4View {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t page_stride;      // elements of a page: 2 H ps hd
+  const int* page_table;    // [B][max_pages]
+  int B, max_pages, n_pages, ps, H, hd;
+};
+// Rows r of K and V (k + r ld, v + r ld: [H][hd]) at position pos[r] of sequence
+// seq[r], or at element offset off[r]; slots the cache does not have are skipped.
+void launch_kv4_append(int dtype, const Kv4View& c, const void* k, const void* v, int64_t ld, const int* seq,
+                       const int* pos, const int64_t* off, int64_t rows, hipStream_t st);
+void launch_kv4_read(int dtype, const Kv4View& c, void* k, void* v, int64_t ld, const int* seq, const int* pos,
+                     int64_t rows, hipStream_t st);
+constexpr int KV4_MAX_DEPTH = 15;
+struct Kv4Tree {
+  uint8_t depth[64];
+  uint8_t path[64][KV4_MAX_DEPTH + 1];  // node at each depth on the root->u path
+};
+struct Kv4AttnArgs {
+  Kv4View c;
+  const void* q;            // [B N][ldq], heads of hd
+  int64_t ldq;
+  void* out;
+  int64_t ldo;
+  const int* n_b;           // [B] committed lengths
+  int Hq, N;
+  float scale;
+  void* ws;
+  Kv4Tree tree;
+};
+// Workspace for sequences of up to cap positions.
+int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int hd, int N);
+void launch_kv4_attn(int dtype, const Kv4AttnArgs& a, hipStream_t st);
+
 // ---- elementwise / norms ------------------------------------------------------
 void launch_embed(int dtype, const int* tokens, const void* E, float* x, int M, int d, int V, hipStream_t st);
 // x[r] += sum_s parts[s][r] (if parts), optionally written back; out (tiled,

@@ -668,6 +668,13 @@ bool launch_gemm(int dtype, const GemmShape& s, const GemmEpi& e, hipStream_t st
   return true;
 }
 
+void launch_gemm_finish(int dtype, const GemmShape& s, const GemmEpi& e, hipStream_t st, hipEvent_t ev_stop) {
+  if (dtype == DT_BF16)
+    launch_finish<bf16_t>(s, e, st, ev_stop);
+  else
+    launch_finish<float>(s, e, st, ev_stop);
+}
+
 void launch_repack(int dtype, int kind, const void* src0, const void* src1, const void* src2, int K, int n_src,
                    void* dst, int H, int hd, hipStream_t st) {
   const int n_packed = kind == PACK_QKV ? 3 * n_src : (kind == PACK_GU ? 2 * n_src : n_src);

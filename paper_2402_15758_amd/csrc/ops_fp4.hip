@@ -1,0 +1,279 @@
+// The C ABI's 4-bit operators (include/chimera.h): checks, workspaces and
+// launches.  None allocates device memory or synchronises.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "abi.h"
+#include "chimera.h"
+#include "kernels.h"
+
+namespace {
+
+constexpr int FP4_MAX_ROWS = 4096;  // rows of a product: two prefill chunks
+
+int64_t round256(int64_t b) { return (b + 255) / 256 * 256; }
+
+void check_dtype(int32_t dtype) {
+  REQUIRE(dtype == CHIMERA_F32 || dtype == CHIMERA_BF16, CHIMERA_EINVAL, "dtype");
+}
+void check_aligned(const void* p, const char* what) {
+  REQUIRE(((uintptr_t)p & 15) == 0, CHIMERA_EINVAL, std::string(what) + " must be 16-byte aligned");
+}
+// The caller's stream must belong to the current device: the kernels are
+// launched there.
+hipStream_t check_stream(void* stream) {
+  hipStream_t st = (hipStream_t)stream;
+  if (st != nullptr) {
+    hipDevice_t on = 0;
+    int dev = 0;
+    HIPCK(hipStreamGetDevice(st, &on));
+    HIPCK(hipGetDevice(&dev));
+    REQUIRE((int)on == dev, CHIMERA_EINVAL, "the stream belongs to another device than the current one");
+  }
+  return st;
+}
+void check_matrix(int32_t N, int32_t K) {
+  REQUIRE(N > 0 && N % 16 == 0 && K > 0 && K % 32 == 0, CHIMERA_EINVAL, "N must be a multiple of 16, K of 32");
+  REQUIRE((int64_t)N * K < (int64_t)1 << 36, CHIMERA_EINVAL, "matrix too large");
+}
+
+// Workspace of a product: tiled x, then the unpacked matrix where the launch
+// takes the bf16 kernels, then the slices' partials.
+struct GemmWs {
+  int64_t x = 0, w = 0, part = 0;
+  bool rows;  // x is read where it lies
+};
+GemmWs gemm_ws(int32_t dtype, int32_t M, int32_t N, int32_t K, bool readable) {
+  GemmWs s;
+  const int64_t es = (int64_t)esize(dtype);
+  const bool unpack = gemm_fp4_unpacks(dtype, M, N);
+  s.rows = M <= 16 && readable;
+  if (!s.rows) s.x = round256((int64_t)mcap(M) * K * es);
+  if (unpack) s.w = round256((int64_t)K * N * 2);
+  const int parts = unpack ? gemm_partials(dtype, M, N, K, mcap(M) / 16, EPI_F32)
+                           : (fp4_splits(N, K) > 1 ? fp4_splits(N, K) : 0);
+  s.part = (int64_t)parts * M * N * 4;
+  return s;
+}
+
+void check_cache(const chimera_kv4* c) {
+  REQUIRE(c != nullptr && c->pool != nullptr && c->page_table != nullptr, CHIMERA_EINVAL, "null cache");
+  REQUIRE(c->head_dim == 64 || c->head_dim == 128, CHIMERA_EINVAL, "head_dim must be 64 or 128");
+  REQUIRE(c->n_heads >= 1 && c->n_heads <= 1024, CHIMERA_EINVAL, "n_heads in [1, 1024]");
+  REQUIRE(c->page_size >= 1 && c->page_size <= 256, CHIMERA_EINVAL, "page_size in [1, 256]");
+  REQUIRE(c->n_pages >= 1 && c->batch >= 1 && c->batch <= 65535 && c->max_pages >= 1, CHIMERA_EINVAL,
+          "n_pages, batch and max_pages must be positive, batch at most 65535");
+  REQUIRE((int64_t)c->max_pages * c->page_size <= (int64_t)1 << 30, CHIMERA_EINVAL, "more than 2^30 positions");
+  check_aligned(c->pool, "pool");
+  int64_t need = 0;
+  if (chimera_kv4_bytes(c->n_pages, c->page_size, c->n_heads, c->head_dim, &need) != CHIMERA_OK)
+    throw Err(CHIMERA_EINVAL, g_err);
+  REQUIRE(c->pool_bytes >= need, CHIMERA_ENOMEM, "pool too small");
+}
+Kv4View view(const chimera_kv4* c) {
+  Kv4View v;
+  v.page_stride = (int64_t)2 * c->n_heads * c->page_size * c->head_dim;
+  v.codes = (uint8_t*)c->pool;
+  v.scales = v.codes + (int64_t)c->n_pages * v.page_stride / 2;
+  v.page_table = c->page_table;
+  v.B = c->batch;
+  v.max_pages = c->max_pages;
+  v.n_pages = c->n_pages;
+  v.ps = c->page_size;
+  v.H = c->n_heads;
+  v.hd = c->head_dim;
+  return v;
+}
+void check_rows(const chimera_kv4* c, int32_t dtype, const void* k, const void* v, int64_t ld, const int32_t* seq,
+                const int32_t* pos, int32_t rows) {
+  check_cache(c);
+  check_dtype(dtype);
+  REQUIRE(rows >= 0, CHIMERA_EINVAL, "rows");
+  REQUIRE(rows == 0 || (k && v && seq && pos), CHIMERA_EINVAL, "null argument");
+  REQUIRE(ld >= (int64_t)c->n_heads * c->head_dim, CHIMERA_EINVAL, "row stride below n_heads * head_dim");
+  REQUIRE((int64_t)rows * c->n_heads * c->head_dim / 4 < (int64_t)1 << 38, CHIMERA_EINVAL, "too many rows");
+}
+
+}  // namespace
+
+extern "C" {
+
+chimera_status chimera_fp4_bytes(int32_t N, int32_t K, int64_t* bytes) {
+  return guard([&] {
+    REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
+    check_matrix(N, K);
+    *bytes = fp4_bytes(N, K);
+  });
+}
+
+chimera_status chimera_fp4_pack(int32_t dtype, const void* w, int64_t ldw, int32_t N, int32_t K, void* packed,
+                                int64_t packed_bytes, void* stream) {
+  return guard([&] {
+    check_dtype(dtype);
+    REQUIRE(w && packed, CHIMERA_EINVAL, "null argument");
+    check_matrix(N, K);
+    REQUIRE(ldw >= N, CHIMERA_EINVAL, "ldw below N");
+    check_aligned(packed, "packed");
+    REQUIRE(packed_bytes >= fp4_bytes(N, K), CHIMERA_ENOMEM, "packed buffer too small");
+    hipStream_t st = check_stream(stream);
+    launch_fp4_pack(dtype, PACK_NATURAL, w, nullptr, nullptr, ldw, N, K, packed, 1, 64, st);
+    HIPCK(hipGetLastError());
+  });
+}
+
+chimera_status chimera_fp4_unpack(int32_t dtype, const void* packed, int32_t N, int32_t K, void* w, int64_t ldw,
+                                  void* stream) {
+  return guard([&] {
+    check_dtype(dtype);
+    REQUIRE(w && packed, CHIMERA_EINVAL, "null argument");
+    check_matrix(N, K);
+    REQUIRE(ldw >= N, CHIMERA_EINVAL, "ldw below N");
+    check_aligned(packed, "packed");
+    hipStream_t st = check_stream(stream);
+    launch_fp4_unpack_rows(dtype, packed, N, K, w, ldw, st);
+    HIPCK(hipGetLastError());
+  });
+}
+
+chimera_status chimera_gemm_fp4_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K, int64_t* bytes) {
+  return guard([&] {
+    REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
+    check_dtype(dtype);
+    REQUIRE(M >= 1 && M <= FP4_MAX_ROWS, CHIMERA_EINVAL, "M in [1, 4096]");
+    check_matrix(N, K);
+    const GemmWs s = gemm_ws(dtype, M, N, K, false);
+    *bytes = s.x + s.w + s.part;
+  });
+}
+
+chimera_status chimera_gemm_fp4(int32_t dtype, const void* x, int64_t ldx, const void* packed, int32_t M, int32_t N,
+                                int32_t K, float* y, int64_t ldy, void* ws, int64_t ws_bytes, void* stream) {
+  return guard([&] {
+    check_dtype(dtype);
+    REQUIRE(x && packed && y, CHIMERA_EINVAL, "null argument");
+    REQUIRE(M >= 1 && M <= FP4_MAX_ROWS, CHIMERA_EINVAL, "M in [1, 4096]");
+    check_matrix(N, K);
+    REQUIRE(ldx >= K && ldy >= N && ldy <= INT32_MAX, CHIMERA_EINVAL, "ldx below K, ldy below N, or ldy over 2^31 - 1");
+    check_aligned(packed, "packed");
+    const int64_t es = (int64_t)esize(dtype);
+    const bool readable = ((uintptr_t)x & 15) == 0 && (M == 1 || ldx * es % 16 == 0);
+    const GemmWs s = gemm_ws(dtype, M, N, K, readable);
+    REQUIRE(s.x + s.w + s.part == 0 || ws != nullptr, CHIMERA_EINVAL, "null workspace");
+    REQUIRE(ws_bytes >= s.x + s.w + s.part, CHIMERA_ENOMEM, "workspace too small");
+    check_aligned(ws, "workspace");
+    hipStream_t st = check_stream(stream);
+    char* base = (char*)ws;
+    GemmShape g;
+    g.x_mtiles = mcap(M) / 16;
+    g.M = M;
+    g.W = packed;
+    g.N = N;
+    g.K = K;
+    g.splits = fp4_splits(N, K);
+    g.X = x;
+    if (!s.rows) {
+      launch_tile_strided(dtype, x, ldx, M, K, base, g.x_mtiles, st);
+      g.X = base;
+    }
+    GemmEpi e;
+    e.kind = EPI_F32;
+    e.out_f = y;
+    e.ldo = (int)ldy;
+    e.part = (float*)(base + s.x + s.w);
+    launch_gemm_fp4(dtype, g, e, s.rows ? ldx : 0, s.w ? base + s.x : nullptr, st);
+    HIPCK(hipGetLastError());
+  });
+}
+
+chimera_status chimera_kv4_bytes(int32_t n_pages, int32_t page_size, int32_t n_heads, int32_t head_dim,
+                                 int64_t* bytes) {
+  return guard([&] {
+    REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
+    REQUIRE(n_pages >= 1, CHIMERA_EINVAL, "n_pages");
+    REQUIRE(page_size >= 1 && page_size <= 256, CHIMERA_EINVAL, "page_size in [1, 256]");
+    REQUIRE(n_heads >= 1 && n_heads <= 1024, CHIMERA_EINVAL, "n_heads in [1, 1024]");
+    REQUIRE(head_dim == 64 || head_dim == 128, CHIMERA_EINVAL, "head_dim must be 64 or 128");
+    const int64_t rows = (int64_t)n_pages * 2 * n_heads * page_size;
+    *bytes = rows * (head_dim / 2 + head_dim / 32);
+  });
+}
+
+chimera_status chimera_kv4_append(const chimera_kv4* cache, int32_t dtype, const void* k, const void* v, int64_t ld,
+                                  const int32_t* seq, const int32_t* pos, int32_t rows, void* stream) {
+  return guard([&] {
+    check_rows(cache, dtype, k, v, ld, seq, pos, rows);
+    hipStream_t st = check_stream(stream);
+    if (rows == 0) return;
+    launch_kv4_append(dtype, view(cache), k, v, ld, seq, pos, nullptr, rows, st);
+    HIPCK(hipGetLastError());
+  });
+}
+
+chimera_status chimera_kv4_read(const chimera_kv4* cache, int32_t dtype, const int32_t* seq, const int32_t* pos,
+                                int32_t rows, void* k_out, void* v_out, int64_t ld, void* stream) {
+  return guard([&] {
+    check_rows(cache, dtype, k_out, v_out, ld, seq, pos, rows);
+    hipStream_t st = check_stream(stream);
+    if (rows == 0) return;
+    launch_kv4_read(dtype, view(cache), k_out, v_out, ld, seq, pos, rows, st);
+    HIPCK(hipGetLastError());
+  });
+}
+
+chimera_status chimera_kv4_attn_bytes(const chimera_kv4* cache, int32_t n_heads, int32_t n_nodes, int64_t* bytes) {
+  return guard([&] {
+    check_cache(cache);
+    REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
+    REQUIRE(n_heads >= 1 && n_heads <= 1024 && n_heads % cache->n_heads == 0, CHIMERA_EINVAL,
+            "n_heads must be a multiple of the cache's heads, at most 1024");
+    REQUIRE(n_nodes >= 1 && n_nodes <= 64, CHIMERA_EINVAL, "n_nodes in [1, 64]");
+    *bytes = kv4_attn_bytes(cache->batch, (int64_t)cache->max_pages * cache->page_size, n_heads, cache->head_dim,
+                            n_nodes);
+  });
+}
+
+chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const void* q, int64_t ldq, const int32_t* n_b,
+                                int32_t n_heads, const int32_t* parent, int32_t n_nodes, float scale, void* out,
+                                int64_t ldo, void* ws, int64_t ws_bytes, void* stream) {
+  return guard([&] {
+    check_dtype(dtype);
+    int64_t need = 0;
+    if (const chimera_status s = chimera_kv4_attn_bytes(cache, n_heads, n_nodes, &need)) throw Err(s, g_err);
+    REQUIRE(q && n_b && out && ws, CHIMERA_EINVAL, "null argument");
+    REQUIRE(ws_bytes >= need, CHIMERA_ENOMEM, "workspace too small");
+    const int64_t es = (int64_t)esize(dtype), width = (int64_t)n_heads * cache->head_dim;
+    REQUIRE(ldq >= width && ldo >= width, CHIMERA_EINVAL, "row stride below n_heads * head_dim");
+    REQUIRE(ldq * es % 16 == 0, CHIMERA_EINVAL, "rows of q must start at multiples of 16 bytes");
+    check_aligned(q, "q");
+    check_aligned(ws, "workspace");
+    REQUIRE(std::isfinite(scale), CHIMERA_EINVAL, "scale must be finite");
+    Kv4AttnArgs a{};
+    for (int u = 0; u < n_nodes; ++u) {
+      const int p = parent ? parent[u] : u - 1;
+      REQUIRE(u == 0 ? p == -1 : (p >= 0 && p < u), CHIMERA_EINVAL,
+              "node 0 must be the root and a parent must precede its child");
+      const int d = u ? a.tree.depth[p] + 1 : 0;
+      REQUIRE(d <= KV4_MAX_DEPTH, CHIMERA_EINVAL, "tree deeper than 15 levels below its root");
+      a.tree.depth[u] = (uint8_t)d;
+      for (int i = 0; i < d; ++i) a.tree.path[u][i] = a.tree.path[p][i];
+      a.tree.path[u][d] = (uint8_t)u;
+    }
+    hipStream_t st = check_stream(stream);
+    a.c = view(cache);
+    a.q = q;
+    a.ldq = ldq;
+    a.out = out;
+    a.ldo = ldo;
+    a.n_b = n_b;
+    a.Hq = n_heads;
+    a.N = n_nodes;
+    a.scale = scale;
+    a.ws = ws;
+    launch_kv4_attn(dtype, a, st);
+    HIPCK(hipGetLastError());
+  });
+}
+
+}  // extern "C"
