@@ -152,10 +152,16 @@ struct Kv4AttnArgs {
   int64_t ldo;
   const int* n_b;           // [B] committed lengths
   int Hq, N;
+  int deepest;              // node depth
+  int groups;               // group slots a sequence: kv4_attn_groups
+  int o_mtiles;             // > 0: out is tiled, with this many 16-row tiles
   float scale;
-  void* ws;
+  float* part_o;            // [B][H][groups][N Hq / H][hd]
+  float* part_ml;           // [B][H][groups][N Hq / H][2]
   Kv4Tree tree;
 };
+// Partials cover positions 0 .. cap - 1.
+int kv4_attn_groups(int64_t cap);
 // Workspace for sequences of up to cap positions.
 int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int hd, int N);
 void launch_kv4_attn(int dtype, const Kv4AttnArgs& a, hipStream_t st);

@@ -255,6 +255,7 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
       REQUIRE(u == 0 ? p == -1 : (p >= 0 && p < u), CHIMERA_EINVAL,
               "node 0 must be the root and a parent must precede its child");
       const int d = u ? a.tree.depth[p] + 1 : 0;
+      a.deepest = std::max(a.deepest, d);
       REQUIRE(d <= KV4_MAX_DEPTH, CHIMERA_EINVAL, "tree deeper than 15 levels below its root");
       a.tree.depth[u] = (uint8_t)d;
       for (int i = 0; i < d; ++i) a.tree.path[u][i] = a.tree.path[p][i];
@@ -270,7 +271,10 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
     a.Hq = n_heads;
     a.N = n_nodes;
     a.scale = scale;
-    a.ws = ws;
+    const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
+    a.groups = kv4_attn_groups(cap);
+    a.part_o = (float*)ws;
+    a.part_ml = a.part_o + (int64_t)cache->batch * a.groups * n_nodes * n_heads * cache->head_dim;
     launch_kv4_attn(dtype, a, st);
     HIPCK(hipGetLastError());
   });
