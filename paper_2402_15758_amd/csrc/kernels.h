@@ -140,9 +140,18 @@ void launch_kv4_append(int dtype, const Kv4View& c, const void* k, const void* v
 void launch_kv4_read(int dtype, const Kv4View& c, void* k, void* v, int64_t ld, const int* seq, const int* pos,
                      int64_t rows, hipStream_t st);
 constexpr int KV4_MAX_DEPTH = 15;
+// By value in the kernels' arguments, so words that scalar loads bring whole:
+// arguments may lie in host memory, where a lane's own loads take microseconds.
 struct Kv4Tree {
-  uint8_t depth[64];
-  uint8_t path[64][KV4_MAX_DEPTH + 1];  // node at each depth on the root->u path
+  uint32_t depth[8];                           // four bits a node
+  uint32_t path[64][(KV4_MAX_DEPTH + 1) / 4];  // a byte a depth: node at that depth on the root->u path
+  void set(int u, int parent) {  // nodes in order, parents first
+    const int d = u == 0 ? 0 : depth_of(parent) + 1;
+    depth[u / 8] |= (uint32_t)d << (4 * (u % 8));
+    for (int i = 0; i < 4; ++i) path[u][i] = u == 0 ? 0 : path[parent][i];
+    path[u][d / 4] |= (uint32_t)u << (8 * (d % 4));
+  }
+  int depth_of(int u) const { return (int)(depth[u / 8] >> (4 * (u % 8))) & 15; }
 };
 struct Kv4AttnArgs {
   Kv4View c;
@@ -153,17 +162,18 @@ struct Kv4AttnArgs {
   const int* n_b;           // [B] committed lengths
   int Hq, N;
   int deepest;              // node depth
-  int groups;               // group slots a sequence: kv4_attn_groups
+  int blocks, units;        // kv4_attn_blocks, kv4_attn_units
   int o_mtiles;             // > 0: out is tiled, with this many 16-row tiles
   float scale;
-  float* part_o;            // [B][H][groups][N Hq / H][hd]
-  float* part_ml;           // [B][H][groups][N Hq / H][2]
+  float* part_o;            // [B][H][units][N Hq / H][hd]
+  float* part_ml;           // [B][H][units][N Hq / H][2]
   Kv4Tree tree;
 };
-// Partials cover positions 0 .. cap - 1.
-int kv4_attn_groups(int64_t cap);
-// Workspace for sequences of up to cap positions.
-int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int hd, int N);
+// Blocks of 16 queries of all sequences and cache heads; slots for partials of
+// a sequence and cache head over positions 0 .. cap - 1; bytes of all partials.
+int kv4_attn_blocks(int B, int Hq, int H, int N);
+int kv4_attn_units(int64_t cap, int blocks);
+int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int H, int hd, int N);
 void launch_kv4_attn(int dtype, const Kv4AttnArgs& a, hipStream_t st);
 
 // ---- elementwise / norms ------------------------------------------------------

@@ -5,6 +5,9 @@
 // scale rows in the same order after all code rows.  So an element offset into
 // a plain cache of that order is twice a code byte's offset and 32 times a
 // scale byte's.
+#include <algorithm>
+#include <type_traits>
+
 #include "common.h"
 #include "fp4.h"
 #include "kernels.h"
@@ -77,61 +80,82 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T* __res
 // As in the verify pass (kernels_attn.hip) the reduction depends on P alone, so
 // a query has the same bits in a tree, in a chain and by itself:
 //   * positions 0 .. P - 16 are committed keys that all queries of a sequence
-//     share: an MFMA pass over chunks of 64 positions.  A run of chunks (1 below
-//     position 1024, 4 from there on) is reduced by the online softmax, four
-//     runs make a group, folded in run order, and a group leaves one partial
-//     (m, l, O);
-//   * the last 16 positions are reduced per query, one wave each, after the
-//     groups' partials are folded in group order.
-// A plain key is visible to every query that could see it masked in the shared
-// pass, so nothing that a query does not see is multiplied into its result.
+//     share.  An MFMA pass reduces each chunk of 64 positions by itself to
+//     (m, l, O); four chunks are folded in order to a group, four groups to a
+//     super, and the supers in order to the whole;
+//   * the last 16 positions are reduced per query, one wave each, on top.
+// Who folds does not matter, so the work is dealt by its amount.  With little of
+// it a workgroup takes a group, a wave a chunk, and leaves the group's partial;
+// with more it takes a super, a wave a group, and leaves a quarter of the
+// partials for a quarter of the prologues (kv4_supers).
+// A key that one query of the shared pass does not see and another does lies in
+// the first one's window, so nothing unseen is multiplied into a result.
 // ---------------------------------------------------------------------------
-constexpr int CHUNK = 64, WIN = 16, RUNS = 4;
-constexpr int NEAR_CHUNKS = 16, FAR_RUN = 4;              // runs of one chunk below NEAR_CHUNKS
-constexpr int NEAR_GROUPS = NEAR_CHUNKS / RUNS;
-__host__ __device__ __forceinline__ int run_chunks(int grp) { return grp < NEAR_GROUPS ? 1 : FAR_RUN; }
-__host__ __device__ __forceinline__ int first_chunk(int grp) {
-  return grp < NEAR_GROUPS ? grp * RUNS : NEAR_CHUNKS + (grp - NEAR_GROUPS) * RUNS * FAR_RUN;
-}
-__host__ __device__ __forceinline__ int groups_of(int64_t positions) {  // that cover positions 0 .. positions - 1
-  const int64_t c = (positions + CHUNK - 1) / CHUNK;
-  if (c <= NEAR_CHUNKS) return (int)((c + RUNS - 1) / RUNS);
-  return NEAR_GROUPS + (int)((c - NEAR_CHUNKS + RUNS * FAR_RUN - 1) / (RUNS * FAR_RUN));
-}
+constexpr int CHUNK = 64, WIN = 16, FAN = 4;
+constexpr int GROUP = FAN * CHUNK, SUPER = FAN * GROUP;  // positions
+constexpr int SUPER_WGS = 256;
 static_assert(WIN == KV4_MAX_DEPTH + 1, "the window holds every position of a tree");
+
+// Depth of a lane's node, and a lane's entry of one node's path.
+__device__ __forceinline__ int node_depth(const Kv4Tree& t, int u) {
+  uint32_t w = t.depth[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) w = u / 8 == i ? t.depth[i] : w;
+  return (int)(w >> (4 * (u & 7))) & 15;
+}
+__device__ __forceinline__ int path_node(const uint32_t (&path)[4], int depth) {
+  uint32_t w = path[0];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) w = depth / 4 == i ? path[i] : w;
+  return (int)(w >> (8 * (depth & 3))) & 255;
+}
 
 __device__ __forceinline__ float exp2_from(float a, float b) {  // 2^(a - b), 0 from nothing
   return a == -CH_INF ? 0.f : __builtin_amdgcn_exp2f(a - b);
 }
-// (m, l) takes in (m2, l2); o = o * x + o2 * y does the rest.  A side without
-// visible keys has l == 0; a NaN is not one.
+// (m, l, O) takes in (m2, l2, O2): l here, O = fma(O, x, O2 y) by the caller.  A
+// side without visible keys has l == 0; a NaN is not one.
 __device__ __forceinline__ bool fold(float& m, float& l, float m2, float l2, float& x, float& y) {
   if (l2 == 0.f) return false;
   const float mn = fmaxf(m, m2);
   x = exp2_from(m, mn);
   y = __builtin_amdgcn_exp2f(m2 - mn);
-  l = l * x + l2 * y;
+  l = fmaf(l, x, l2 * y);
   m = mn;
   return true;
+}
+__device__ __forceinline__ float fold_value(float o, float x, float o2, float y) { return fmaf(o, x, o2 * y); }
+__device__ __forceinline__ f32x4 fold_value(f32x4 o, float x, f32x4 o2, float y) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) o[r] = fmaf(o[r], x, o2[r] * y);
+  return o;
+}
+
+// Whether a sequence's shared positions 0 .. maxk are dealt in supers: where
+// those alone give every CU a workgroup.  blocks: B x H x blocks of 16 queries.
+__host__ __device__ __forceinline__ bool kv4_supers(int maxk, int blocks) {
+  return (int64_t)blocks * (maxk / SUPER + 1) >= SUPER_WGS;
 }
 
 // A lane's quarter of a row: dimensions HD/4 g .. HD/4 (g + 1) - 1, eight codes
 // a word, under one scale.  MFMA k-block ks takes its word ks, so the reduction
-// over dimensions runs in an order of its own, the queries' too.
+// over dimensions runs in an order of its own, the queries' too.  A row is named
+// by the index of its first group of 32 values: 16 code bytes and one scale byte
+// each, 32 bits for every pool that fits the card (the host checks).
 template <int HD>
 struct Quarter {
   uint32_t w[HD / 32];
   uint32_t s;
-  __device__ __forceinline__ void load(const Kv4View& c, int64_t e, int g) {  // e: the row's element offset
-    const uint8_t* p = c.codes + e / 2 + g * (HD / 8);
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, uint32_t row, int g) {
     if constexpr (HD == 128) {
-      const int4 v = ld16(p);
+      const int4 v = ld16(codes + (uint64_t)(row + g) * 16);
       w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+      s = scales[row + g];
     } else {
-      const int2 v = *reinterpret_cast<const int2*>(p);
+      const int2 v = *reinterpret_cast<const int2*>(codes + (uint64_t)(row + (g >> 1)) * 16 + 8 * (g & 1));
       w[0] = v.x, w[1] = v.y;
+      s = scales[row + (g >> 1)];
     }
-    s = c.scales[e / 32 + g * (HD / 4) / 32];
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -139,13 +163,18 @@ struct Quarter {
     s = 0;
   }
 };
-// Queries' operand fragments in the same order of dimensions.
+// Queries' operand fragments in the same order of dimensions, negated for a
+// negative scale: the scores' scale is then its magnitude.
 template <typename T, int HD>
-__device__ __forceinline__ void load_query(const T* q, int g, Frag32<T> (&f)[HD / 32]) {
+__device__ __forceinline__ void load_query(const T* q, int g, bool negate, Frag32<T> (&f)[HD / 32]) {
+  const int flip = !negate ? 0 : (sizeof(T) == 2 ? (int)0x80008000 : (int)0x80000000);
 #pragma unroll
   for (int ks = 0; ks < HD / 32; ++ks)
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j) f[ks].v[j] = ld16(q + (HD / 4) * g + 8 * ks + 4 * j);
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+      const int4 v = ld16(q + (HD / 4) * g + 8 * ks + 4 * j);
+      f[ks].v[j] = int4{v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
+    }
 }
 
 // Row pitch of values staged in LDS.  16-bit V is read back transposed by
@@ -175,39 +204,31 @@ __device__ __forceinline__ int2 ld_tr16(const void* p) {
   return __builtin_bit_cast(int2, v);
 }
 
-// One chunk's scores become weights.  s: S^T, lane (g, c16) holding query c16 and
-// keys 16 kb + 4 g + r.  vis: the chunk's keys that the query sees.  Updates
-// (m, l) and returns the factor for O; all: every key is visible to every
-// query of the wave (the masked path computes the same values then).
-__device__ __forceinline__ float chunk_weights(f32x4 (&s)[4], float scale2, bool all, uint64_t vis, int g, float& m,
-                                               float& l) {
+// One chunk's scores become weights and its (m, l).  s: S^T, lane (g, c16) holding
+// query c16 and keys 16 kb + 4 g + r.  vis: the chunk's keys that the query sees;
+// ALL: every key, for every query of the wave (the masked path computes the same
+// values then).  scale2 >= 0.
+template <bool ALL>
+__device__ __forceinline__ void chunk_weights(f32x4 (&s)[4], float scale2, uint64_t vis, int g, float& m, float& l) {
+  const uint64_t mine = ALL ? 0 : vis >> (4 * g);
   float mc = -CH_INF;
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float v = s[kb][r] * scale2;
-      if (!all && !((vis >> (16 * kb + 4 * g + r)) & 1)) v = -CH_INF;
-      s[kb][r] = v;
-      mc = fmaxf(mc, v);
-    }
+    for (int r = 0; r < 4; ++r) mc = fmaxf(mc, ALL || ((mine >> (16 * kb + r)) & 1) ? s[kb][r] : -CH_INF);
   mc = rows_max(mc);
-  const float mn = fmaxf(m, mc);
-  const float alpha = vis != 0 || all ? exp2_from(m, mn) : 1.f;
+  m = ALL || vis != 0 ? mc * scale2 : -CH_INF;
   float ls = 0.f;
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      float p = __builtin_amdgcn_exp2f(s[kb][r] - mn);
-      if (!all && !((vis >> (16 * kb + 4 * g + r)) & 1)) p = 0.f;
+      float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], scale2, -m));
+      if constexpr (!ALL) p = (mine >> (16 * kb + r)) & 1 ? p : 0.f;
       s[kb][r] = p;
       ls = ls + p;
     }
-  ls = rows_sum(ls);
-  l = l * alpha + ls;
-  m = mn;
-  return alpha;
+  l = rows_sum(ls);
 }
 
 // O^T += V^T P^T over the 32 keys of half kp, staged as rows v.  A weight enters
@@ -257,274 +278,220 @@ __device__ __forceinline__ void pv_half(const f32x4 (&s)[4], int kp, const T* v,
   }
 }
 
-// What both shapes of the shared pass need of a workgroup: sequence b, cache
-// head h, group grp.
-struct SharedPart {
-  int n, grp, c_begin, c_end;  // chunks of the group with visible keys
-  int maxk;                    // last position any query treats as shared
-};
-__device__ __forceinline__ bool shared_part(const Kv4AttnArgs& a, int b, SharedPart& p) {
-  p.grp = blockIdx.x;
-  p.n = min(a.n_b[b], a.c.max_pages * a.c.ps);
-  p.maxk = p.n < 0 ? -1 : p.n + a.deepest - WIN;
-  p.c_begin = first_chunk(p.grp);
-  p.c_end = min(p.c_begin + RUNS * run_chunks(p.grp) - 1, p.maxk < 0 ? -1 : p.maxk / CHUNK);
-  return p.c_begin <= p.c_end;
-}
-// The query of lane column c16: index qi of the sequence's N Hq / H queries of a
-// cache head, node-major.
-template <typename T, int HD>
-__device__ __forceinline__ int query_of(const Kv4AttnArgs& a, int b, int h, int qi, int n, int g,
-                                        Frag32<T> (&qf)[HD / 32]) {
-  const int gq = a.Hq / a.c.H, u = qi / gq;
-  load_query<T, HD>((const T*)a.q + ((int64_t)b * a.N + u) * a.ldq + (h * gq + qi % gq) * HD, g, qf);
-  return n + a.tree.depth[u] - WIN;  // its last shared position
-}
-// Keys of chunk c that a query with last shared position lim sees.
-__device__ __forceinline__ uint64_t visible(int c, int lim, uint64_t bad) {
-  const int k = lim - c * CHUNK;  // last visible key of the chunk
-  const uint64_t in = k < 0 ? 0 : (k >= CHUNK - 1 ? ~0ull : (2ull << k) - 1);
-  return in & ~bad;
-}
-__device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h, int grp, int nq) {
-  return (((int64_t)b * a.c.H + h) * a.groups + grp) * nq;
+// Partials of sequence b, cache head h, unit (group or super): one a query.
+__device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h, int unit, int nq) {
+  return (((int64_t)b * a.c.H + h) * a.units + unit) * nq;
 }
 
-// Up to 16 queries a cache head (single tokens, short chains, few grouped
-// heads): grid (groups, H, B), a wave takes a run of the group's chunks with
-// all queries as its 16 MFMA columns.  Waves share nothing until their runs are
-// done: K goes from memory through the conversion into the MFMA, V through 32
-// rows of wave-private LDS for its transposition; K of the next chunk is
-// requested as soon as the scores have taken this chunk's, V likewise.
+// The shared pass: grid (blocks of 16 queries x H, units, B), a wave with the
+// block's queries (of the N Hq / H of a cache head, node-major) as its 16 MFMA
+// columns over its chunks.  K goes from memory through the conversion into the
+// MFMA, V through 32 rows of wave-private LDS for its transposition: the waves
+// share nothing until their partials meet.  The next chunk's K is requested when
+// the scores have taken this one's, its V when this one's is used up.  Several
+// query blocks of a workgroup sharing one conversion of V, with a barrier a
+// chunk, were slower: 64 nodes at 512 tokens 12.8 us against MARK.
+//
+// Workgroups are dealt to the eight dies round-robin, the first grid dimension
+// first: heads, whose work is equal, and a head's query blocks on the die whose
+// L2 has its keys (where H is a multiple of 8).  With the groups first, die i
+// took group i of every head (8 ragged sequences of 1024 to 4096 tokens, single
+// queries: 60 us instead of 37).
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void kv4_shared_few(const Kv4AttnArgs a) {
-  constexpr int VP = v_pitch<T, HD>();
-  __shared__ __attribute__((aligned(16))) T vs[RUNS][32 * VP];
-  __shared__ int64_t slots[RUNS][CHUNK];
-  __shared__ float ml[RUNS][16][2];
-  static_assert(sizeof(T) * 32 * VP >= 16 * HD * 4, "a run's partial fits its staging rows");
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 3 : 2))) void kv4_shared(
+    const Kv4AttnArgs a) {
+  constexpr int VP = v_pitch<T, HD>(), OP = HD + 4, QP = HD + 16 / sizeof(T);  // row pitches: V, partials, queries
+  union alignas(16) Stage {
+    T v[32 * VP];
+    float o[16 * OP];
+  };
+  __shared__ Stage stage_[FAN];
+  __shared__ uint32_t rows_[FAN][FAN * CHUNK];
+  __shared__ float ml[FAN][16][2];
+  __shared__ __attribute__((aligned(16))) T qs[16 * QP];  // registers are what bounds the waves a SIMD holds
   const Kv4View& cv = a.c;
-  const int h = blockIdx.y, b = blockIdx.z;
+  const int h = blockIdx.x % cv.H, q0 = 16 * (blockIdx.x / cv.H), b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, c16 = lane & 15;
-  SharedPart sp;
-  if (!shared_part(a, b, sp)) return;  // uniform
-  const int nq = a.N * (a.Hq / cv.H);
-  Frag32<T> qf[HD / 32];
-  const int lim = query_of<T, HD>(a, b, h, min(c16, nq - 1), sp.n, g, qf);
-  const int rc = run_chunks(sp.grp), c0 = sp.c_begin + wave * rc, c1 = min(c0 + rc - 1, sp.c_end);
-  const float scale2 = a.scale * LOG2E;
-  float m = -CH_INF, l = 0.f;
-  f32x4 o[HD / 16];
+  const int cap = cv.max_pages * cv.ps;
+  const int n = min(a.n_b[b], cap);
+  const int gq = a.Hq / cv.H, nq = a.N * gq;
+  const int qi = min(q0 + c16, nq - 1), u = qi / gq;
+  const int maxk = n < 0 ? -1 : n + a.deepest - WIN;  // last position any query treats as shared
+  if (maxk < 0) return;                               // uniform
+  const bool supers = kv4_supers(maxk, a.blocks);
+  const int nu = maxk / (supers ? SUPER : GROUP) + 1, per = supers ? FAN : 1;  // chunks a wave
+  const int lim = n + node_depth(a.tree, u) - WIN;                             // this column's last shared position
+  const uint8_t* vcodes = cv.codes + (int64_t)cv.H * cv.ps * HD / 2;
+  const uint8_t* vscales = cv.scales + (int64_t)cv.H * cv.ps * HD / 32;
+  const int* ptab = cv.page_table + (int64_t)b * cv.max_pages;
+  const float scale2 = fabsf(a.scale) * LOG2E;
+  T* const v = stage_[wave].v;
+  uint32_t* const rows = rows_[wave];
+  if (wave == 0) {
+    Frag32<T> f[HD / 32];
+    load_query<T, HD>((const T*)a.q + ((int64_t)b * a.N + u) * a.ldq + (h * gq + qi % gq) * HD, g, a.scale < 0.f, f);
 #pragma unroll
-  for (int d = 0; d < HD / 16; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  T* v = vs[wave];
-  int64_t* sl = slots[wave];
-  const int64_t head = (int64_t)h * cv.ps * HD, vofs = (int64_t)cv.H * cv.ps * HD;
-  if (c0 <= c1) {  // wave-uniform
-    // lane i works out key i's slot; rows past the last shared position and
-    // those the cache does not have read slot 0 of page 0 and count as bad
-    auto slot = [&](int c) {
-      const int p = c * CHUNK + lane;
-      return p <= sp.maxk ? kv4_slot(cv, b, p) : (int64_t)-1;
-    };
-    uint64_t bad = 0, bad_next = 0;
-    auto put = [&](int64_t e) {
-      sl[lane] = (e < 0 ? 0 : e) + head;
-      __builtin_amdgcn_wave_barrier();
-    };
-    Quarter<HD> k[4], vq[4];
-    int64_t e = slot(c0);
-    bad = __ballot(e < 0);
-    put(e);
+    for (int ks = 0; ks < HD / 32; ++ks)
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      const int64_t r = sl[16 * kb + c16];
-      k[kb].load(cv, r, g);
-      vq[kb].load(cv, r + vofs, g);
-    }
-    for (int c = c0; c <= c1; ++c) {
-      int64_t en = c < c1 ? slot(c + 1) : (int64_t)-1;
-      f32x4 s[4];
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        const float sc = fp4_scale(k[kb].s);
-        s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < HD / 32; ++ks) {
-          Frag32<T> f;
-          f.from_fp4(k[kb].w[ks], sc);
-          s[kb] = mfma32<T>(f, qf[ks], s[kb]);
-        }
-      }
-      if (c < c1) {
-        bad_next = __ballot(en < 0);
-        put(en);
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) k[kb].load(cv, sl[16 * kb + c16], g);
-      }
-      const uint64_t vis = visible(c, lim, bad);
-      const bool all = __ballot(vis != ~0ull) == 0;
-      const float alpha = chunk_weights(s, scale2, all, vis, g, m, l);
-#pragma unroll
-      for (int d = 0; d < HD / 16; ++d) o[d] = o[d] * alpha;
-#pragma unroll
-      for (int kp = 0; kp < 2; ++kp) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          Quarter<HD>& r = vq[2 * kp + j];
-          if (bad != 0 && ((bad >> (32 * kp + 16 * j + c16)) & 1)) r.clear();  // adds exact zeros
-          stage_quarter<T, HD>(r, v + (16 * j + c16) * VP, g);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        pv_half<T, HD>(s, kp, v, g, c16, o);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      }
-      if (c < c1) {
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) vq[kb].load(cv, sl[16 * kb + c16] + vofs, g);
-      }
-      bad = bad_next;
-    }
-  }
-  // the runs meet in LDS, in run order
-  float* po = reinterpret_cast<float*>(v);
-  if (c16 < nq) {
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) *reinterpret_cast<f32x4*>(po + c16 * HD + 16 * d + 4 * g) = o[d];
-    if (g == 0) {
-      ml[wave][c16][0] = m;
-      ml[wave][c16][1] = l;
-    }
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) st16(qs + c16 * QP + (HD / 4) * g + 8 * ks + 4 * j, f[ks].v[j]);
   }
   __syncthreads();
-  const int64_t base = part_slot(a, b, h, sp.grp, nq);
-  for (int i = tid; i < nq * HD; i += 256) {
-    const int q = i / HD;
-    float M = -CH_INF, L = 0.f, O = 0.f;
-#pragma unroll
-    for (int w = 0; w < RUNS; ++w) {
-      float x, y;
-      if (fold(M, L, ml[w][q][0], ml[w][q][1], x, y)) O = O * x + reinterpret_cast<const float*>(vs[w])[i] * y;
-    }
-    a.part_o[base * HD + i] = O;
-    if (i % HD == 0) {
-      a.part_ml[(base + q) * 2] = M;
-      a.part_ml[(base + q) * 2 + 1] = L;
-    }
-  }
-}
 
-// More queries: grid (groups, H x blocks of 64 queries, B).  The workgroup
-// converts each chunk once into LDS, the waves own 16 queries each and walk the
-// chunks, folding a run at its end.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void kv4_shared_many(const Kv4AttnArgs a) {
-  constexpr int VP = v_pitch<T, HD>(), KP = HD + 16 / sizeof(T);
-  __shared__ __attribute__((aligned(16))) T ks_[CHUNK * KP];
-  __shared__ __attribute__((aligned(16))) T vs[CHUNK * VP];
-  const Kv4View& cv = a.c;
-  const int h = blockIdx.y % cv.H, qb = blockIdx.y / cv.H, b = blockIdx.z;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c16 = lane & 15;
-  SharedPart sp;
-  if (!shared_part(a, b, sp)) return;
-  const int nq = a.N * (a.Hq / cv.H), qi = 64 * qb + 16 * wave + c16;
-  const bool wave_on = 64 * qb + 16 * wave < nq;  // wave-uniform
-  Frag32<T> qf[HD / 32];
-  const int lim = query_of<T, HD>(a, b, h, min(qi, nq - 1), sp.n, g, qf);
-  const int rc = run_chunks(sp.grp);
-  const float scale2 = a.scale * LOG2E;
-  float m = -CH_INF, l = 0.f, fm = -CH_INF, fl = 0.f;
-  f32x4 o[HD / 16], fo[HD / 16];
+  for (int unit = blockIdx.y; unit < nu; unit += gridDim.y) {
+    const int c0 = (unit * FAN + wave) * per;
+    const int nc = min(per, maxk / CHUNK - c0 + 1);  // chunks with shared keys; may be <= 0
+    float m = -CH_INF, l = 0.f;
+    f32x4 o[HD / 16];
 #pragma unroll
-  for (int d = 0; d < HD / 16; ++d) o[d] = fo[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int64_t head = (int64_t)h * cv.ps * HD, vofs = (int64_t)cv.H * cv.ps * HD;
-  // thread (key, quarter) brings that quarter of K's and V's row
-  const int key = tid >> 2, quarter = tid & 3;
-  auto slot = [&](int c) {
-    const int p = c * CHUNK + key;
-    return p <= sp.maxk ? kv4_slot(cv, b, p) : (int64_t)-1;
-  };
-  __shared__ uint32_t bad_bits[2][4];  // of the chunk in LDS: 16 keys a wave
-  Quarter<HD> k, v;
-  int64_t e = slot(sp.c_begin);
-  k.load(cv, (e < 0 ? 0 : e) + head, quarter);
-  v.load(cv, (e < 0 ? 0 : e) + head + vofs, quarter);
-  for (int c = sp.c_begin; c <= sp.c_end; ++c) {
-    const int64_t en = c < sp.c_end ? slot(c + 1) : (int64_t)-1;
-    const uint64_t wb = __ballot(e < 0);
-    if (c > sp.c_begin) __syncthreads();  // the last chunk's readers are done
-    if (e < 0) v.clear();
-    stage_quarter<T, HD>(k, ks_ + key * KP, quarter);
-    stage_quarter<T, HD>(v, vs + key * VP, quarter);
-    if (lane == 0) {
-      uint32_t x = 0;  // one bit a key: its four threads agree
+    for (int d = 0; d < HD / 16; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (nc > 0) {
+      // where the chunks' keys lie, a lane a key; keys past maxk and those the
+      // cache does not have read group 0 and count as bad
+      uint64_t bad[FAN];
+      int page[FAN];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x |= (uint32_t)((wb >> (4 * i)) & 1) << i;
-      bad_bits[c & 1][wave] = x;
+      for (int i = 0; i < FAN; ++i) {
+        const int p = (c0 + i) * CHUNK + lane;
+        page[i] = i < nc && p <= maxk ? ptab[(unsigned)p / (unsigned)cv.ps] : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < FAN; ++i) {
+        const bool have = (unsigned)page[i] < (unsigned)cv.n_pages;
+        bad[i] = __ballot(!have);
+        const unsigned slot = (unsigned)((c0 + i) * CHUNK + lane) % (unsigned)cv.ps;
+        if (i < per)
+          rows[i * CHUNK + lane] =
+              have ? (uint32_t)((int64_t)page[i] * (cv.page_stride / 32)) + (h * cv.ps + slot) * (HD / 32) : 0;
+      }
+      __builtin_amdgcn_wave_barrier();
+      Quarter<HD> k[4], vq[4];
+      auto load_k = [&](int i) {
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) k[kb].load(cv.codes, cv.scales, rows[i * CHUNK + 16 * kb + c16], g);
+      };
+      auto load_v = [&](int i, int j) { vq[j].load(vcodes, vscales, rows[i * CHUNK + 16 * j + c16], g); };
+      load_k(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_v(0, j);
+      for (int i = 0; i < nc; ++i) {
+        const uint64_t gone = i == 0 ? bad[0] : (i == 1 ? bad[1] : (i == 2 ? bad[2] : bad[3]));
+        f32x4 s[4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < HD / 32; ++ks) {
+          Frag32<T> q;
+#pragma unroll
+          for (int j = 0; j < (int)sizeof(T) / 2; ++j) q.v[j] = ld16(qs + c16 * QP + (HD / 4) * g + 8 * ks + 4 * j);
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb) {
+            Frag32<T> f;
+            f.from_fp4(k[kb].w[ks], fp4_scale(k[kb].s));
+            s[kb] = mfma32<T>(f, q, s[kb]);
+          }
+        }
+        if (i + 1 < nc) load_k(i + 1);
+        const int last = lim - (c0 + i) * CHUNK;  // the query's last key of the chunk
+        const uint64_t vis = (last < 0 ? 0 : (last >= CHUNK - 1 ? ~0ull : (2ull << last) - 1)) & ~gone;
+        float mc, lc;
+        if (__ballot(vis != ~0ull) == 0)
+          chunk_weights<true>(s, scale2, vis, g, mc, lc);
+        else
+          chunk_weights<false>(s, scale2, vis, g, mc, lc);
+        f32x4 oc[HD / 16];
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) oc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kp = 0; kp < 2; ++kp) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            Quarter<HD>& r = vq[2 * kp + j];
+            if ((gone >> (32 * kp + 16 * j + c16)) & 1) r.clear();  // adds exact zeros
+            stage_quarter<T, HD>(r, v + (16 * j + c16) * VP, g);
+          }
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+          pv_half<T, HD>(s, kp, v, g, c16, oc);
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+        if (i + 1 < nc) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) load_v(i + 1, j);
+        }
+        float x, y;
+        if (i == 0) {  // into nothing: itself
+          m = mc;
+          l = lc;
+#pragma unroll
+          for (int d = 0; d < HD / 16; ++d) o[d] = oc[d];
+        } else if (fold(m, l, mc, lc, x, y)) {
+#pragma unroll
+          for (int d = 0; d < HD / 16; ++d) o[d] = fold_value(o[d], x, oc[d], y);
+        }
+      }
+    }
+    // the waves' partials meet, in order
+    float* po = stage_[wave].o;
+    if (q0 + c16 < nq) {
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) *reinterpret_cast<f32x4*>(po + c16 * OP + 16 * d + 4 * g) = o[d];
+      if (g == 0) {
+        ml[wave][c16][0] = m;
+        ml[wave][c16][1] = l;
+      }
     }
     __syncthreads();
-    if (c < sp.c_end) {
-      k.load(cv, (en < 0 ? 0 : en) + head, quarter);
-      v.load(cv, (en < 0 ? 0 : en) + head + vofs, quarter);
-    }
-    e = en;
-    if (!wave_on) continue;
-    const uint32_t* bb = bad_bits[c & 1];
-    const uint64_t bad = (uint64_t)(bb[0] | bb[1] << 16) | (uint64_t)(bb[2] | bb[3] << 16) << 32;
-    f32x4 s[4];
+    const int64_t base = part_slot(a, b, h, unit, nq) + q0;
+    const int mine = min(nq - q0, 16);
+    for (int i = tid; i < mine * (HD / 4); i += 256) {
+      const int q = i / (HD / 4), d = i % (HD / 4) * 4;
+      float M = -CH_INF, L = 0.f;
+      f32x4 O = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t = 0; t < HD / 32; ++t) {
-        Frag32<T> f;
-#pragma unroll
-        for (int j = 0; j < (int)sizeof(T) / 2; ++j)
-          f.v[j] = ld16(ks_ + (16 * kb + c16) * KP + (HD / 4) * g + 8 * t + 4 * j);
-        s[kb] = mfma32<T>(f, qf[t], s[kb]);
+      for (int w = 0; w < FAN; ++w) {
+        const f32x4 p = *reinterpret_cast<const f32x4*>(stage_[w].o + q * OP + d);
+        float x, y;
+        if (fold(M, L, ml[w][q][0], ml[w][q][1], x, y)) O = fold_value(O, x, p, y);
       }
+      *reinterpret_cast<f32x4*>(a.part_o + (base + q) * HD + d) = O;
+      if (d == 0) *reinterpret_cast<float2*>(a.part_ml + (base + q) * 2) = float2{M, L};
     }
-    const uint64_t vis = visible(c, lim, bad);
-    const bool all = __ballot(vis != ~0ull) == 0;
-    const float alpha = chunk_weights(s, scale2, all, vis, g, m, l);
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) o[d] = o[d] * alpha;
-#pragma unroll
-    for (int kp = 0; kp < 2; ++kp) pv_half<T, HD>(s, kp, vs + 32 * kp * VP, g, c16, o);
-    if (c == sp.c_end || (c + 1 - sp.c_begin) % rc == 0) {  // a run ends
-      float x, y;
-      if (fold(fm, fl, m, l, x, y)) {
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d) fo[d] = fo[d] * x + o[d] * y;
-      }
-#pragma unroll
-      for (int d = 0; d < HD / 16; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m = -CH_INF;
-      l = 0.f;
-    }
-  }
-  if (qi >= nq) return;
-  const int64_t at = part_slot(a, b, h, sp.grp, nq) + qi;
-#pragma unroll
-  for (int d = 0; d < HD / 16; ++d) *reinterpret_cast<f32x4*>(a.part_o + at * HD + 16 * d + 4 * g) = fo[d];
-  if (g == 0) {
-    a.part_ml[at * 2] = fm;
-    a.part_ml[at * 2 + 1] = fl;
+    __syncthreads();
   }
 }
 
-// The window: grid (ceil(Hq / 4), N, B), a wave per query.  Lane 4 k + j scores
-// quarter j of window key k; for the output each lane reads its own dimensions
-// of every row.  The groups' partials are folded while the rows are in flight.
+// x of the lanes with bit B clear and y of those with it set, each summed over
+// the pair of lanes that differ in bit B.
+template <int B>
+__device__ __forceinline__ float pair_reduce(float x, float y, int lane) {
+  if constexpr (B == 5) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else if constexpr (B == 4) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else {
+    const bool up = (lane >> B) & 1;
+    const float keep = up ? y : x, give = up ? x : y;
+    if constexpr (B == 3) return keep + dpp_mov<DPP_ROR8>(give);
+    // lane ^ 4: mirrored within 8 (lane ^ 7), then within 4 (lane ^ 3)
+    return keep + dpp_mov<0x1B>(dpp_mov<DPP_MIRROR8>(give));
+  }
+}
+
+// The window: grid (ceil(Hq / 4), N, B), a wave per query.  Lane 4 k + j takes
+// quarter j of window key k, of K for the score and of V for its share of the
+// output; the shares of the 16 keys are then added over the lanes, halving the
+// dimensions a lane holds with each of the four steps: the lane ends with
+// dimensions HD/4 j + (HD/64) rev .., rev the bits 5, 4, 3, 2 of the lane.  The
+// partials are folded, for those dimensions, while the rows are in flight.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
-  constexpr int DPL = HD / 64, BATCH = 8;
+  constexpr int DPL = HD / 64, DQ = HD / 4;
   const Kv4View& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hq = 4 * blockIdx.x + wave, u = blockIdx.y, b = blockIdx.z;
@@ -532,60 +499,68 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
   const int gq = a.Hq / c.H, h = hq / gq, nq = a.N * gq, qi = u * gq + hq % gq;
   const int64_t row = (int64_t)b * a.N + u;
   const int kw = lane >> 2, sub = lane & 3;
+  const int dim = DQ * sub + DPL * (8 * (lane >> 5) + 4 * ((lane >> 4) & 1) + 2 * ((lane >> 3) & 1) + ((lane >> 2) & 1));
   const int n = min(a.n_b[b], c.max_pages * c.ps);
-  Frag32<T> qf[HD / 32];
-  load_query<T, HD>((const T*)a.q + row * a.ldq + hq * HD, sub, qf);
-  const int P = n + a.tree.depth[u];
-  const int lim = P - WIN;
-  const int ngrp = n < 0 || lim < 0 ? 0 : groups_of((int64_t)lim + 1);
-  const int64_t base = part_slot(a, b, h, 0, nq) + qi;
-  float bm[BATCH], bl[BATCH], bo[BATCH][DPL];
-  auto load_batch = [&](int g0) {
-#pragma unroll
-    for (int t = 0; t < BATCH; ++t) {
-      const int64_t at = base + (int64_t)min(g0 + t, ngrp - 1) * nq;
-      bm[t] = a.part_ml[at * 2];
-      bl[t] = a.part_ml[at * 2 + 1];
-#pragma unroll
-      for (int d = 0; d < DPL; ++d) bo[t][d] = a.part_o[at * HD + DPL * lane + d];
-    }
-  };
-  if (ngrp > 0) load_batch(0);
+  const int P = n + ((a.tree.depth[u / 8] >> (4 * (u & 7))) & 15);
   // this lane's window key
   const int p = P - WIN + 1 + kw;
-  const int at = p < n ? p : n + a.tree.path[u][min(max(p - n, 0), KV4_MAX_DEPTH)];
-  int64_t e = n >= 0 && p >= 0 ? kv4_slot(c, b, at) : (int64_t)-1;
+  const int at = p < n ? p : n + path_node(a.tree.path[u], min(max(p - n, 0), KV4_MAX_DEPTH));
+  const int64_t e = n >= 0 && p >= 0 ? kv4_slot(c, b, at) : (int64_t)-1;
   const bool valid = e >= 0;
-  e = (valid ? e : 0) + (int64_t)h * c.ps * HD;
-  const uint64_t ok = __ballot(valid);
-  Quarter<HD> k;
-  k.load(c, e, sub);
-  uint32_t vc[WIN], vsc[WIN];
-  const int64_t vofs = (int64_t)c.H * c.ps * HD + DPL * lane;
+  Frag32<T> qf[HD / 32];
+  load_query<T, HD>((const T*)a.q + row * a.ldq + hq * HD, sub, a.scale < 0.f, qf);
+  const int maxk = n < 0 ? -1 : n + a.deepest - WIN;
+  const bool supers = maxk >= 0 && kv4_supers(maxk, a.blocks);
+  const int lim = n < 0 ? -1 : P - WIN;  // last shared position of this query
+  const int nu = lim < 0 ? 0 : lim / (supers ? SUPER : GROUP) + 1;
+  const int64_t base = part_slot(a, b, h, 0, nq) + qi;
+  const uint32_t r = valid ? (uint32_t)(e / 32 + h * (c.ps * HD / 32)) : 0;
+  Quarter<HD> k, v;
+  k.load(c.codes, c.scales, r, sub);
+  v.load(c.codes + (int64_t)c.H * c.ps * HD / 2, c.scales + (int64_t)c.H * c.ps * HD / 32, r, sub);
+  float m = -CH_INF, l = 0.f, o[DPL], gm = -CH_INF, gl = 0.f, go[DPL];
 #pragma unroll
-  for (int i = 0; i < WIN; ++i) {
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)e, 4 * i);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(e >> 32), 4 * i);
-    const int64_t ve = (int64_t)((uint64_t)hi << 32 | lo) + vofs;
-    vc[i] = c.codes[ve / 2];
-    vsc[i] = c.scales[ve / 32];
-  }
-  float m = -CH_INF, l = 0.f, o[DPL];
+  for (int d = 0; d < DPL; ++d) o[d] = go[d] = 0.f;
+  // BATCH partials a round trip, folded in order
+  auto fold_units = [&](auto batch) {
+    constexpr int BATCH = decltype(batch)::value;
+    for (int g0 = 0; g0 < nu; g0 += BATCH) {
+      float2 bml[BATCH];
+      float bo[BATCH][DPL];
 #pragma unroll
-  for (int d = 0; d < DPL; ++d) o[d] = 0.f;
-  for (int g0 = 0; g0 < ngrp; g0 += BATCH) {
-    if (g0 > 0) load_batch(g0);
+      for (int t = 0; t < BATCH; ++t) {
+        const int64_t at = base + (int64_t)min(g0 + t, nu - 1) * nq;
+        bml[t] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
 #pragma unroll
-    for (int t = 0; t < BATCH; ++t) {
-      float x, y;
-      if (g0 + t < ngrp && fold(m, l, bm[t], bl[t], x, y)) {
+        for (int d = 0; d < DPL; ++d) bo[t][d] = a.part_o[at * HD + dim + d];
+      }
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) o[d] = o[d] * x + bo[t][d] * y;
+      for (int t = 0; t < BATCH; ++t) {
+        if (g0 + t >= nu) break;
+        float x, y;
+        if (fold(gm, gl, bml[t].x, bml[t].y, x, y)) {  // groups make a super; a super is itself
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, bo[t][d], y);
+        }
+        if (supers || t % FAN == FAN - 1 || g0 + t == nu - 1) {
+          if (fold(m, l, gm, gl, x, y)) {
+#pragma unroll
+            for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
+          }
+          gm = -CH_INF;
+          gl = 0.f;
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) go[d] = 0.f;
+        }
       }
     }
-  }
+  };
+  if (nu <= 4)  // uniform
+    fold_units(std::integral_constant<int, 4>{});
+  else
+    fold_units(std::integral_constant<int, 16>{});
   float acc = 0.f;
-  const float sc = fp4_scale(k.s);
+  float sc = fp4_scale(k.s);
 #pragma unroll
   for (int i = 0; i < HD / 32; ++i) {
     const f32x4 x0 = fp4_to_f32x4<0>(k.w[i], sc), x1 = fp4_to_f32x4<1>(k.w[i], sc);
@@ -595,39 +570,48 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
   }
   acc = acc + dpp_mov<DPP_XOR1>(acc);
   acc = acc + dpp_mov<DPP_XOR2>(acc);
-  const float s = valid ? acc * (a.scale * LOG2E) : -CH_INF;
+  const float s = valid ? acc * (fabsf(a.scale) * LOG2E) : -CH_INF;
   const float mn = fmaxf(m, wave_max(s));
-  const float alpha = ok != 0 ? exp2_from(m, mn) : 1.f;
+  const float alpha = __ballot(valid) != 0 ? exp2_from(m, mn) : 1.f;
   const float pe = valid ? __builtin_amdgcn_exp2f(s - mn) : 0.f;
   l = l * alpha + wave_sum(sub == 0 ? pe : 0.f);
+  if (!valid) v.clear();
+  sc = fp4_scale(v.s);
+  float w[DQ];
 #pragma unroll
-  for (int d = 0; d < DPL; ++d) o[d] = o[d] * alpha;
+  for (int i = 0; i < HD / 32; ++i) {
+    const f32x4 x0 = fp4_to_f32x4<0>(v.w[i], sc), x1 = fp4_to_f32x4<1>(v.w[i], sc);
 #pragma unroll
-  for (int i = 0; i < WIN; ++i) {
-    if (!((ok >> (4 * i)) & 1)) continue;  // wave-uniform
-    const float pk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(pe), 4 * i));
-    const uint32_t w = DPL == 1 ? vc[i] >> (4 * (lane & 1)) : vc[i];
-    const f32x4 x = fp4_to_f32x4<0>(w, fp4_scale(vsc[i]));
-#pragma unroll
-    for (int d = 0; d < DPL; ++d) o[d] = fmaf(pk, x[d], o[d]);
+    for (int t = 0; t < 4; ++t) {
+      w[8 * i + t] = pe * x0[t];
+      w[8 * i + 4 + t] = pe * x1[t];
+    }
   }
 #pragma unroll
+  for (int d = 0; d < DQ / 2; ++d) w[d] = pair_reduce<5>(w[d], w[d + DQ / 2], lane);
+#pragma unroll
+  for (int d = 0; d < DQ / 4; ++d) w[d] = pair_reduce<4>(w[d], w[d + DQ / 4], lane);
+#pragma unroll
+  for (int d = 0; d < DQ / 8; ++d) w[d] = pair_reduce<3>(w[d], w[d + DQ / 8], lane);
+#pragma unroll
+  for (int d = 0; d < DQ / 16; ++d) w[d] = pair_reduce<2>(w[d], w[d + DQ / 16], lane);
+#pragma unroll
   for (int d = 0; d < DPL; ++d) {
-    const float r = l == 0.f ? 0.f : o[d] / l;  // no visible key
+    const float y = l == 0.f ? 0.f : (o[d] * alpha + w[d]) / l;  // 0: no visible key
     if (a.o_mtiles > 0)
-      store_tiled<T>((T*)a.out, a.o_mtiles, (int)row, hq * HD + DPL * lane + d, r);
+      store_tiled<T>((T*)a.out, a.o_mtiles, (int)row, hq * HD + dim + d, y);
     else
-      ((T*)a.out)[row * a.ldo + hq * HD + DPL * lane + d] = ET<T>::from_f(r);
+      ((T*)a.out)[row * a.ldo + hq * HD + dim + d] = ET<T>::from_f(y);
   }
 }
 
 template <typename T, int HD>
 void kv4_attn_go(const Kv4AttnArgs& a, hipStream_t st) {
-  const int nq = a.N * (a.Hq / a.c.H);
-  if (nq <= 16)
-    hipLaunchKernelGGL((kv4_shared_few<T, HD>), dim3(a.groups, a.c.H, a.c.B), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((kv4_shared_many<T, HD>), dim3(a.groups, a.c.H * ((nq + 63) / 64), a.c.B), dim3(256), 0, st, a);
+  const int x = a.c.H * ((a.N * (a.Hq / a.c.H) + 15) / 16);
+  // a workgroup walks the units of its place; more places than four rounds over
+  // the chip only cost their start where a long table holds a short sequence
+  const int y = std::max(1, std::min(a.units, 4096 / std::min(4096, x * a.c.B)));
+  hipLaunchKernelGGL((kv4_shared<T, HD>), dim3(x, y, a.c.B), dim3(256), 0, st, a);
   hipLaunchKernelGGL((kv4_window<T, HD>), dim3((a.Hq + 3) / 4, a.N, a.c.B), dim3(256), 0, st, a);
 }
 
@@ -653,10 +637,16 @@ void launch_kv4_read(int dtype, const Kv4View& c, void* k, void* v, int64_t ld, 
     hipLaunchKernelGGL(kv4_read_kernel<float>, grid, dim3(256), 0, st, c, (float*)k, (float*)v, ld, seq, pos, rows);
 }
 
-int kv4_attn_groups(int64_t cap) { return groups_of(cap); }
+int kv4_attn_blocks(int B, int Hq, int H, int N) { return B * H * ((N * (Hq / H) + 15) / 16); }
 
-int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int hd, int N) {
-  return (int64_t)B * groups_of(cap) * N * Hq * (hd + 2) * 4;
+int kv4_attn_units(int64_t cap, int blocks) {
+  // groups are left only by sequences of fewer than SUPER_WGS / blocks supers
+  const int64_t supers = (cap + SUPER - 1) / SUPER, groups = (cap + GROUP - 1) / GROUP;
+  return (int)std::max(supers, std::min<int64_t>(groups, FAN * (int64_t)((SUPER_WGS + blocks - 1) / blocks)));
+}
+
+int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int H, int hd, int N) {
+  return (int64_t)B * kv4_attn_units(cap, kv4_attn_blocks(B, Hq, H, N)) * N * Hq * (hd + 2) * 4;
 }
 
 void launch_kv4_attn(int dtype, const Kv4AttnArgs& a, hipStream_t st) {

@@ -70,6 +70,8 @@ void check_cache(const chimera_kv4* c) {
   int64_t need = 0;
   if (chimera_kv4_bytes(c->n_pages, c->page_size, c->n_heads, c->head_dim, &need) != CHIMERA_OK)
     throw Err(CHIMERA_EINVAL, g_err);
+  // groups of 32 values are named by 32 bits
+  REQUIRE(need / 17 < (int64_t)1 << 32, CHIMERA_EINVAL, "pool over 68 GiB");
   REQUIRE(c->pool_bytes >= need, CHIMERA_ENOMEM, "pool too small");
 }
 Kv4View view(const chimera_kv4* c) {
@@ -229,8 +231,8 @@ chimera_status chimera_kv4_attn_bytes(const chimera_kv4* cache, int32_t n_heads,
     REQUIRE(n_heads >= 1 && n_heads <= 1024 && n_heads % cache->n_heads == 0, CHIMERA_EINVAL,
             "n_heads must be a multiple of the cache's heads, at most 1024");
     REQUIRE(n_nodes >= 1 && n_nodes <= 64, CHIMERA_EINVAL, "n_nodes in [1, 64]");
-    *bytes = kv4_attn_bytes(cache->batch, (int64_t)cache->max_pages * cache->page_size, n_heads, cache->head_dim,
-                            n_nodes);
+    *bytes = kv4_attn_bytes(cache->batch, (int64_t)cache->max_pages * cache->page_size, n_heads, cache->n_heads,
+                            cache->head_dim, n_nodes);
   });
 }
 
@@ -254,12 +256,9 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
       const int p = parent ? parent[u] : u - 1;
       REQUIRE(u == 0 ? p == -1 : (p >= 0 && p < u), CHIMERA_EINVAL,
               "node 0 must be the root and a parent must precede its child");
-      const int d = u ? a.tree.depth[p] + 1 : 0;
-      a.deepest = std::max(a.deepest, d);
-      REQUIRE(d <= KV4_MAX_DEPTH, CHIMERA_EINVAL, "tree deeper than 15 levels below its root");
-      a.tree.depth[u] = (uint8_t)d;
-      for (int i = 0; i < d; ++i) a.tree.path[u][i] = a.tree.path[p][i];
-      a.tree.path[u][d] = (uint8_t)u;
+      REQUIRE(u == 0 || a.tree.depth_of(p) < KV4_MAX_DEPTH, CHIMERA_EINVAL, "tree deeper than 15 levels below its root");
+      a.tree.set(u, p);
+      a.deepest = std::max(a.deepest, a.tree.depth_of(u));
     }
     hipStream_t st = check_stream(stream);
     a.c = view(cache);
@@ -272,9 +271,10 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
     a.N = n_nodes;
     a.scale = scale;
     const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
-    a.groups = kv4_attn_groups(cap);
+    a.blocks = kv4_attn_blocks(cache->batch, n_heads, cache->n_heads, n_nodes);
+    a.units = kv4_attn_units(cap, a.blocks);
     a.part_o = (float*)ws;
-    a.part_ml = a.part_o + (int64_t)cache->batch * a.groups * n_nodes * n_heads * cache->head_dim;
+    a.part_ml = a.part_o + (int64_t)cache->batch * a.units * n_nodes * n_heads * cache->head_dim;
     launch_kv4_attn(dtype, a, st);
     HIPCK(hipGetLastError());
   });
