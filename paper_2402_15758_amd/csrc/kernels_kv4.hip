@@ -313,10 +313,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
   const int h = blockIdx.x % cv.H, q0 = 16 * (blockIdx.x / cv.H), b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, c16 = lane & 15;
-  const int cap = cv.max_pages * cv.ps;
-  const int n = min(a.n_b[b], cap);
+  const int n = min(a.n_b[b], cv.max_pages * cv.ps);
   const int gq = a.Hq / cv.H, nq = a.N * gq;
   const int qi = min(q0 + c16, nq - 1), u = qi / gq;
+  Frag32<T> qf[HD / 32];  // one wave brings the queries
+  if (wave == 0)
+    load_query<T, HD>((const T*)a.q + ((int64_t)b * a.N + u) * a.ldq + (h * gq + qi % gq) * HD, g, a.scale < 0.f, qf);
   const int maxk = n < 0 ? -1 : n + a.deepest - WIN;  // last position any query treats as shared
   if (maxk < 0) return;                               // uniform
   const bool supers = kv4_supers(maxk, a.blocks);
@@ -328,13 +330,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
   const float scale2 = fabsf(a.scale) * LOG2E;
   T* const v = stage_[wave].v;
   uint32_t* const rows = rows_[wave];
+  // page ids of a unit's keys for this wave, a lane a key: -1 past maxk
+  int page[FAN];
+  auto load_pages = [&](int unit) {
+#pragma unroll
+    for (int i = 0; i < FAN; ++i) {
+      const int p = ((unit * FAN + wave) * per + i) * CHUNK + lane;
+      page[i] = i < per && p <= maxk ? ptab[(unsigned)p / (unsigned)cv.ps] : -1;
+    }
+  };
+  load_pages(blockIdx.y);
   if (wave == 0) {
-    Frag32<T> f[HD / 32];
-    load_query<T, HD>((const T*)a.q + ((int64_t)b * a.N + u) * a.ldq + (h * gq + qi % gq) * HD, g, a.scale < 0.f, f);
 #pragma unroll
     for (int ks = 0; ks < HD / 32; ++ks)
 #pragma unroll
-      for (int j = 0; j < (int)sizeof(T) / 2; ++j) st16(qs + c16 * QP + (HD / 4) * g + 8 * ks + 4 * j, f[ks].v[j]);
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) st16(qs + c16 * QP + (HD / 4) * g + 8 * ks + 4 * j, qf[ks].v[j]);
   }
   __syncthreads();
 
@@ -349,12 +359,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
       // where the chunks' keys lie, a lane a key; keys past maxk and those the
       // cache does not have read group 0 and count as bad
       uint64_t bad[FAN];
-      int page[FAN];
-#pragma unroll
-      for (int i = 0; i < FAN; ++i) {
-        const int p = (c0 + i) * CHUNK + lane;
-        page[i] = i < nc && p <= maxk ? ptab[(unsigned)p / (unsigned)cv.ps] : -1;
-      }
 #pragma unroll
       for (int i = 0; i < FAN; ++i) {
         const bool have = (unsigned)page[i] < (unsigned)cv.n_pages;
@@ -365,6 +369,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
               have ? (uint32_t)((int64_t)page[i] * (cv.page_stride / 32)) + (h * cv.ps + slot) * (HD / 32) : 0;
       }
       __builtin_amdgcn_wave_barrier();
+      if (unit + (int)gridDim.y < nu) load_pages(unit + gridDim.y);
       Quarter<HD> k[4], vq[4];
       auto load_k = [&](int i) {
 #pragma unroll
@@ -422,16 +427,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
 #pragma unroll
           for (int j = 0; j < 4; ++j) load_v(i + 1, j);
         }
-        float x, y;
-        if (i == 0) {  // into nothing: itself
-          m = mc;
-          l = lc;
+        float x = 1.f, y = 0.f;  // a query without keys here keeps what it has
+        (void)fold(m, l, mc, lc, x, y);
 #pragma unroll
-          for (int d = 0; d < HD / 16; ++d) o[d] = oc[d];
-        } else if (fold(m, l, mc, lc, x, y)) {
-#pragma unroll
-          for (int d = 0; d < HD / 16; ++d) o[d] = fold_value(o[d], x, oc[d], y);
-        }
+        for (int d = 0; d < HD / 16; ++d) o[d] = fold_value(o[d], x, oc[d], y);
       }
     }
     // the waves' partials meet, in order
@@ -608,9 +607,9 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
 template <typename T, int HD>
 void kv4_attn_go(const Kv4AttnArgs& a, hipStream_t st) {
   const int x = a.c.H * ((a.N * (a.Hq / a.c.H) + 15) / 16);
-  // a workgroup walks the units of its place; more places than four rounds over
-  // the chip only cost their start where a long table holds a short sequence
-  const int y = std::max(1, std::min(a.units, 4096 / std::min(4096, x * a.c.B)));
+  // A workgroup walks the units of its place.  Three a CU are resident; more only
+  // cost their start, 5 to 8 ns each, where a long table holds short sequences.
+  const int y = std::min(a.units, std::max(1, 2048 / (x * a.c.B)));
   hipLaunchKernelGGL((kv4_shared<T, HD>), dim3(x, y, a.c.B), dim3(256), 0, st, a);
   hipLaunchKernelGGL((kv4_window<T, HD>), dim3((a.Hq + 3) / 4, a.N, a.c.B), dim3(256), 0, st, a);
 }
