@@ -49,6 +49,12 @@ typedef enum {
 } chimera_status;
 
 typedef enum { CHIMERA_F32 = 0, CHIMERA_BF16 = 1 } chimera_dtype;
+/* Added to chimera_config.dtype: the target layers' matrices (wq .. w_down) are
+ * rounded to the 4-bit format of the 4-bit operators below as they are loaded
+ * (groups along d_in) and held in it, 17/64 of their bytes in bf16.  Tensors are
+ * given as without it; embeddings, the LM head and the draft keep the dtype.  A
+ * bf16 model has the bits of the same model loaded with the rounded matrices. */
+enum { CHIMERA_WEIGHTS_FP4 = 0x100 };
 
 /* Shapes.  The target is a Llama-style decoder (the paper's backbones,
  * Table 1): pre-RMSNorm blocks with multi-head attention and rotary
@@ -60,7 +66,7 @@ typedef struct {
   int32_t n_layers, d_model, n_heads, head_dim, d_ffn, vocab, n_draft_heads;
   float rope_base; /* 10000 */
   float rms_eps;   /* 1e-5 */
-  int32_t dtype;   /* chimera_dtype of weights and stored activations */
+  int32_t dtype;   /* chimera_dtype of weights and stored activations, plus CHIMERA_WEIGHTS_FP4 */
   int32_t max_positions; /* size of the rotary tables: positions 0..max_positions-1 */
 } chimera_config;
 
@@ -104,6 +110,21 @@ chimera_status chimera_kv_bytes(const chimera_model* m, int32_t max_batch, int32
 chimera_status chimera_kv_create(chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
                                  int32_t page_size, const int32_t* page_order, void* arena, int64_t arena_bytes,
                                  chimera_kv** out);
+
+/* The same with the target's K and V held in 4 bits (the format of the 4-bit
+ * operators below): each layer is a 4-bit paged cache of its own, 17/64 of the
+ * bytes in bf16, and one layer's K and V as values, which prefill attention
+ * reads.  Every position's K and V are rounded as they are written, in prefill
+ * and in steps, so the model is the one whose attention reads those values;
+ * everything else is as with chimera_kv_create (greedy verification is lossless
+ * against greedy decoding over the same kind of cache).  chimera_kv_read gives
+ * the values held.  The compaction check refuses such a cache
+ * (CHIMERA_EINVAL).  A layer's pool is at most 68 GiB. */
+chimera_status chimera_kv_fp4_bytes(const chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                                    int32_t page_size, int64_t* bytes);
+chimera_status chimera_kv_fp4_create(chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                                     int32_t page_size, const int32_t* page_order, void* arena, int64_t arena_bytes,
+                                     chimera_kv** out);
 
 /* Decode context for a static candidate tree of n_nodes nodes (root
  * included, n_nodes <= 64).  Node i has parent parent[i] (< i; -1 for the

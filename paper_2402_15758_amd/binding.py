@@ -10,6 +10,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libchimera.so")
 
 CHIMERA_F32, CHIMERA_BF16 = 0, 1
+CHIMERA_WEIGHTS_FP4 = 0x100
 CHIMERA_DECODE_GREEDY, CHIMERA_DECODE_TYPICAL = 0, 1
 CHIMERA_DRAFT_CHAIN, CHIMERA_DRAFT_BRANCH = 0, 1
 DBG_VERIFY_LOGITS, DBG_DRAFT_LOGITS, DBG_TREE_TOKENS, DBG_DRAFT_LISTS, DBG_SEQ_LEN, DBG_TOKENS = range(6)
@@ -62,6 +63,8 @@ _PROTOS = {
                      ctypes.POINTER(P)],
     "chimera_kv_bytes": [P, I32, I32, I32, I32, PI64],
     "chimera_kv_create": [P, I32, I32, I32, I32, PI32, P, I64, ctypes.POINTER(P)],
+    "chimera_kv_fp4_bytes": [P, I32, I32, I32, I32, PI64],
+    "chimera_kv_fp4_create": [P, I32, I32, I32, I32, PI32, P, I64, ctypes.POINTER(P)],
     "chimera_ctx_bytes": [P, P, I32, PI64],
     "chimera_ctx_create": [P, P, PI32, PI32, I32, P, I64, ctypes.POINTER(P)],
     "chimera_prefill": [P, P, P, PI32, PI32, I32, PI32, P],
@@ -158,6 +161,20 @@ def chimera_kv_create(model: int, max_batch: int, max_len: int, n_pages: int, pa
     out = P()
     _check(lib().chimera_kv_create(model, max_batch, max_len, n_pages, page_size, _i32p(page_order), arena_ptr,
                                    arena_bytes, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_kv_fp4_bytes(model: int, max_batch: int, max_len: int, n_pages: int, page_size: int) -> int:
+    out = I64()
+    _check(lib().chimera_kv_fp4_bytes(model, max_batch, max_len, n_pages, page_size, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_kv_fp4_create(model: int, max_batch: int, max_len: int, n_pages: int, page_size: int, page_order,
+                          arena_ptr: int, arena_bytes: int) -> int:
+    out = P()
+    _check(lib().chimera_kv_fp4_create(model, max_batch, max_len, n_pages, page_size, _i32p(page_order), arena_ptr,
+                                       arena_bytes, ctypes.byref(out)))
     return out.value
 
 

@@ -45,8 +45,16 @@ struct BlockW {
   void* wdown = nullptr;
 };
 
-void validate_config(const chimera_config* c) {
-  REQUIRE(c != nullptr, CHIMERA_EINVAL, "null config");
+// The config without its weight-format flag, and whether that is set.
+struct ModelConfig {
+  chimera_config cfg;
+  bool w4;
+};
+ModelConfig validate_config(const chimera_config* given) {
+  REQUIRE(given != nullptr, CHIMERA_EINVAL, "null config");
+  ModelConfig mc{*given, (given->dtype & CHIMERA_WEIGHTS_FP4) != 0};
+  mc.cfg.dtype &= ~CHIMERA_WEIGHTS_FP4;
+  const chimera_config* c = &mc.cfg;
   REQUIRE(c->dtype == CHIMERA_F32 || c->dtype == CHIMERA_BF16, CHIMERA_EINVAL, "dtype");
   REQUIRE(c->n_layers >= 1 && c->n_heads >= 1, CHIMERA_EINVAL, "layers/heads");
   REQUIRE(c->head_dim == 64 || c->head_dim == 128, CHIMERA_EINVAL, "head_dim must be 64 or 128");
@@ -57,6 +65,7 @@ void validate_config(const chimera_config* c) {
   REQUIRE(c->n_draft_heads >= 0 && c->n_draft_heads <= 8, CHIMERA_EINVAL, "n_draft_heads in [0, 8]");
   REQUIRE(c->max_positions >= 16, CHIMERA_EINVAL, "max_positions");
   REQUIRE(c->rms_eps > 0.f && c->rope_base > 1.f, CHIMERA_EINVAL, "eps/base");
+  return mc;
 }
 
 }  // namespace
@@ -65,6 +74,7 @@ struct chimera_model {
   chimera_config cfg{};
   int dt = 0;
   size_t es = 4;
+  bool w4 = false;  // the target layers' matrices are held in 4 bits
   void* embed = nullptr;
   std::vector<BlockW> layers;
   BlockW enc;
@@ -87,7 +97,9 @@ struct chimera_kv {
   chimera_model* m = nullptr;
   int B = 0, max_len = 0, n_pages = 0, ps = 0, max_pages = 0, cap = 0;
   void* pool = nullptr;
-  int64_t page_stride = 0, layer_stride = 0;
+  int64_t page_stride = 0, layer_stride = 0;  // elements; layer_stride: bytes of a 4-bit layer
+  bool fp4 = false;     // target K/V in 4 bits: each layer a 4-bit paged cache of its own
+  void* wide = nullptr;  // fp4: one layer's K/V as values (what prefill attention reads)
   int* page_table = nullptr;  // device [B][max_pages]
   std::vector<int> page_table_host;
   void* enc_k = nullptr;
@@ -142,6 +154,7 @@ struct chimera_ctx {
   // verify workspaces
   float* x = nullptr;
   void* xn = nullptr;
+  void* w4_wide = nullptr;  // 4-bit weights: the matrix a launch of many rows reads as values
   void* q = nullptr;
   void* attn = nullptr;
   void* hbuf = nullptr;
@@ -157,6 +170,11 @@ struct chimera_ctx {
   int* v_pos = nullptr;
   int64_t* v_kvoff = nullptr;
   int64_t* rowtab = nullptr;  // [B][TREE_ATTN_TAIL_ROWS]: window rows of the current verify pass
+  // 4-bit KV: a pass's K and V rows on their way to the cache ([rows][K | V][H hd]),
+  // the offset of row r in them, and the step's attention (all but its layer)
+  void* kv_rows = nullptr;
+  int64_t* kv_row = nullptr;
+  Kv4AttnArgs attn4{};
   // trigram lookup cache (attached by chimera_set_trigram_cache; hit/miss/stats live in this arena)
   TriCache tri;
   bool tri_on = false;
@@ -231,26 +249,27 @@ namespace {
 // ---------------------------------------------------------------------------
 // Model layout
 // ---------------------------------------------------------------------------
-void carve_block(const chimera_config& c, size_t es, Arena& a, BlockW& w) {
+void carve_block(const chimera_config& c, size_t es, Arena& a, BlockW& w, bool w4) {
   const size_t d = c.d_model, hd = (size_t)c.n_heads * c.head_dim, F = c.d_ffn;
+  auto matrix = [&](size_t K, size_t N) { return a.take(w4 ? (size_t)fp4_bytes((int)N, (int)K) : K * N * es); };
   w.attn_norm = a.arr<float>(d);
-  w.wqkv = a.take(d * 3 * hd * es);
-  w.wo = a.take(hd * d * es);
+  w.wqkv = matrix(d, 3 * hd);
+  w.wo = matrix(hd, d);
   w.ffn_norm = a.arr<float>(d);
-  w.wgu = a.take(d * 2 * F * es);
-  w.wdown = a.take(F * d * es);
+  w.wgu = matrix(d, 2 * F);
+  w.wdown = matrix(F, d);
 }
 
 void carve_model(const chimera_config& c, Arena& a, chimera_model& m) {
   const size_t es = esize(c.dtype), d = c.d_model, V = c.vocab;
   m.embed = a.take(V * d * es);
   m.layers.assign(c.n_layers, BlockW{});
-  for (auto& l : m.layers) carve_block(c, es, a, l);
+  for (auto& l : m.layers) carve_block(c, es, a, l, m.w4);
   m.final_norm = a.arr<float>(d);
   m.lm_head = a.take(d * V * es);
   m.tri_w1 = a.take(3 * d * d * es);
   m.tri_w2 = a.take(d * d * es);
-  carve_block(c, es, a, m.enc);
+  carve_block(c, es, a, m.enc, false);
   m.head_a.assign(c.n_draft_heads, nullptr);
   m.head_theta.assign(c.n_draft_heads, nullptr);
   for (int k = 0; k < c.n_draft_heads; ++k) {
@@ -275,8 +294,17 @@ struct Gemm {
   hipStream_t st;
   bool timed;  // record events around the launch (verify GEMMs while profiling)
 
+  // A product with one of the target layers' matrices, in the format they are held in.
+  void run_layer(const void* X, int x_mtiles, int M, const void* W, int N, int K, GemmEpi e) const {
+    run(X, x_mtiles, M, W, N, K, e, 0, 0, nullptr, c->m->w4);
+  }
+  // Partials that a run_layer launch of kind EPI_PARTIAL leaves.
+  int layer_partials(int M, int N, int K, int x_mtiles) const {
+    return c->m->w4 && !gemm_fp4_unpacks(c->m->dt, M, N) ? fp4_splits(N, K) : gemm_partials(c->m->dt, M, N, K, x_mtiles);
+  }
+
   void run(const void* X, int x_mtiles, int M, const void* W, int N, int K, GemmEpi e, int nb_off = 0,
-           int nb_count = 0, const int* skip = nullptr) const {
+           int nb_count = 0, const int* skip = nullptr, bool w4 = false) const {
     GemmShape s;
     s.X = X;
     s.x_mtiles = x_mtiles;
@@ -288,7 +316,7 @@ struct Gemm {
     s.nb_count = nb_count;
     s.skip = skip;
     const int cols = nb_count ? nb_count * 16 : N;
-    s.splits = gemm_pick_splits(cols, K, c->m->dt);
+    s.splits = w4 ? fp4_splits(N, K) : gemm_pick_splits(cols, K, c->m->dt);
     const int tiles_read = M <= 16 ? 1 : (M <= 32 ? 2 : 4 * ((M + 63) / 64));
     REQUIRE(tiles_read <= x_mtiles, CHIMERA_EINVAL, "GEMM rows exceed the input buffer");
     if (e.kind != EPI_PARTIAL) e.part = c->scratch;
@@ -299,13 +327,20 @@ struct Gemm {
     if (timed && c->prof && !c->capturing && c->ev_created && c->ev_used < c->ev_pool.size()) {
       ev = &c->ev_pool[c->ev_used];
       const double es = (double)c->m->es;
-      c->ev_bytes[c->ev_used] = (double)K * cols * es + (double)M * K * es + (double)M * cols * 4.0;
+      c->ev_bytes[c->ev_used] = (double)K * cols * (w4 ? 17.0 / 32.0 : es) + (double)M * K * es + (double)M * cols * 4.0;
       c->ev_used++;
     }
     // the kernels record the events at their own start and end
+    if (w4) {
+      launch_gemm_fp4(c->m->dt, s, e, 0, gemm_fp4_unpacks(c->m->dt, M, N) ? c->w4_wide : nullptr, st,
+                      ev ? ev->a : nullptr, ev ? ev->b : nullptr);
+      return;
+    }
     REQUIRE(launch_gemm(c->m->dt, s, e, st, ev ? ev->a : nullptr, ev ? ev->b : nullptr), CHIMERA_EINVAL, NO_GEMM);
   }
 };
+
+Kv4View kv4_layer(const chimera_kv* kv, int l, int batch);
 
 struct VerifyRows {
   const int* tokens;
@@ -317,6 +352,7 @@ struct VerifyRows {
   int N, D, B;
   int mtiles;                // 16-row tiles of the activation buffers
   const PrefillBlock* blk;   // prefill: B query blocks; nullptr: B trees of N nodes
+  const PrefillChunk* chunk;  // of those blocks
 };
 
 // Target layer stack over M rows; leaves the post-final-norm states in c->hl.
@@ -336,7 +372,8 @@ void verify_layers(chimera_ctx* c, const VerifyRows& r, hipStream_t st, bool tim
     const BlockW& w = m->layers[l];
     launch_rmsnorm(dt, c->x, nparts ? c->parts : nullptr, nparts, w.attn_norm, c->xn, r.mtiles, nullptr, r.M, d,
                    cf.rms_eps, 1, nullptr, 0, 0, st);
-    char* kbase = (char*)kv->pool + (size_t)l * kv->layer_stride * m->es;
+    // a 4-bit layer takes the rows from kv_rows; prefill attention reads it as values
+    char* kbase = kv->fp4 ? (char*)kv->wide : (char*)kv->pool + (size_t)l * kv->layer_stride * m->es;
     char* vbase = kbase + (size_t)H * kv->ps * hd * m->es;
     GemmEpi e;
     e.kind = EPI_QKV;
@@ -346,13 +383,25 @@ void verify_layers(chimera_ctx* c, const VerifyRows& r, hipStream_t st, bool tim
     e.kbase = kbase;
     e.vbase = vbase;
     e.head_stride = (int64_t)kv->ps * hd;
+    if (kv->fp4) {
+      e.kvoff = c->kv_row;
+      e.kbase = c->kv_rows;
+      e.vbase = (char*)c->kv_rows + (size_t)hdim * m->es;
+      e.head_stride = hd;
+    }
     e.qout = c->q;
     e.ldq = hdim;
     e.rcos = m->rcos;
     e.rsin = m->rsin;
     e.H = H;
     e.hd = hd;
-    g.run(c->xn, r.mtiles, r.M, w.wqkv, 3 * hdim, d, e);
+    g.run_layer(c->xn, r.mtiles, r.M, w.wqkv, 3 * hdim, d, e);
+    if (kv->fp4) {
+      const Kv4View view = kv4_layer(kv, l, r.blk ? kv->B : r.B);
+      launch_kv4_append(dt, view, c->kv_rows, (char*)c->kv_rows + (size_t)hdim * m->es, 2 * hdim, nullptr, nullptr,
+                        c->v_kvoff, r.M, st);
+      if (r.blk != nullptr) launch_kv4_expand(dt, view, *r.chunk, kv->wide, st);
+    }
 
     TreeAttnArgs a{};
     a.q = c->q;
@@ -379,25 +428,35 @@ void verify_layers(chimera_ctx* c, const VerifyRows& r, hipStream_t st, bool tim
     a.B = r.B;
     a.rowtab = c->rowtab;
     a.blk = r.blk;
-    launch_tree_attn(dt, a, st);
+    if (kv->fp4 && r.blk == nullptr) {
+      Kv4AttnArgs& f = c->attn4;
+      f.c = kv4_layer(kv, l, r.B);
+      f.blocks = kv4_attn_blocks(r.B, H, H, r.N);
+      f.units = kv4_attn_units((int64_t)kv->max_pages * kv->ps, f.blocks);
+      f.part_ml = f.part_o + (int64_t)r.B * f.units * r.N * hdim;
+      f.o_mtiles = r.mtiles;
+      launch_kv4_attn(dt, f, st);
+    } else {
+      launch_tree_attn(dt, a, st);
+    }
 
     GemmEpi eo;
     eo.kind = EPI_PARTIAL;
     eo.part = c->parts;
-    g.run(c->attn, r.mtiles, r.M, w.wo, d, hdim, eo);
-    nparts = gemm_partials(dt, r.M, d, hdim, r.mtiles);
+    g.run_layer(c->attn, r.mtiles, r.M, w.wo, d, hdim, eo);
+    nparts = g.layer_partials(r.M, d, hdim, r.mtiles);
     launch_rmsnorm(dt, c->x, c->parts, nparts, w.ffn_norm, c->xn, r.mtiles, nullptr, r.M, d, cf.rms_eps, 1, nullptr, 0,
                    0, st);
     GemmEpi egu;
     egu.kind = EPI_SWIGLU;
     egu.out_t = c->hbuf;
     egu.o_mtiles = r.mtiles;
-    g.run(c->xn, r.mtiles, r.M, w.wgu, 2 * F, d, egu);
+    g.run_layer(c->xn, r.mtiles, r.M, w.wgu, 2 * F, d, egu);
     GemmEpi ed;
     ed.kind = EPI_PARTIAL;
     ed.part = c->parts;
-    g.run(c->hbuf, r.mtiles, r.M, w.wdown, d, F, ed);
-    nparts = gemm_partials(dt, r.M, d, F, r.mtiles);
+    g.run_layer(c->hbuf, r.mtiles, r.M, w.wdown, d, F, ed);
+    nparts = g.layer_partials(r.M, d, F, r.mtiles);
   }
   launch_rmsnorm(dt, c->x, c->parts, nparts, m->final_norm, c->hl, r.mtiles, c->hl_rm, r.M, d, cf.rms_eps, 1, nullptr,
                  0, 0, st);
@@ -604,6 +663,7 @@ void prefill_chunk(chimera_ctx* c, const StepState& s, const PrefillChunk& ch, c
   r.B = nblk;
   r.mtiles = mt;
   r.blk = c->pf_blk;
+  r.chunk = &ch;
   verify_layers(c, r, st, false);
   if (draft) {
     // target-state entries (rows [0, M)) and trigram entries (rows [M, 2M))
@@ -679,6 +739,23 @@ void sync_or_poison(chimera_ctx* c, hipStream_t st) {
   }
 }
 
+// Layer l of a 4-bit cache.
+Kv4View kv4_layer(const chimera_kv* kv, int l, int batch) {
+  const chimera_config& c = kv->m->cfg;
+  Kv4View v;
+  v.page_stride = kv->page_stride;
+  v.codes = (uint8_t*)kv->pool + (size_t)l * kv->layer_stride;
+  v.scales = v.codes + (int64_t)kv->n_pages * kv->page_stride / 2;
+  v.page_table = kv->page_table;
+  v.B = batch;
+  v.max_pages = kv->max_pages;
+  v.n_pages = kv->n_pages;
+  v.ps = kv->ps;
+  v.H = c.n_heads;
+  v.hd = c.head_dim;
+  return v;
+}
+
 // Size (and, with a real arena, carve) a context.
 void carve_ctx(chimera_ctx* c, Arena& a) {
   chimera_model* m = c->m;
@@ -725,16 +802,27 @@ void carve_ctx(chimera_ctx* c, Arena& a) {
   c->attn = a.take(Px * d * es);
   c->hbuf = a.take(Px * F * es);
   const int hdim = (int)(H * hd);
-  c->parts = a.arr<float>(d * std::max(gemm_partial_rows(m->dt, (int)Px, (int)d, hdim, EPI_PARTIAL),
-                                       gemm_partial_rows(m->dt, (int)Px, (int)d, (int)F, EPI_PARTIAL)));
+  // partial rows of a layer's product
+  auto layer_rows = [&](size_t M, int N, int Kd, int kind) {
+    int64_t rows = gemm_partial_rows(m->dt, (int)M, N, Kd, kind);
+    if (m->w4 && (kind == EPI_PARTIAL || fp4_splits(N, Kd) > 1)) {
+      const int64_t direct = gemm_fp4_unpacks(m->dt, (int)M, N) ? FP4_DIRECT_ROWS : (int64_t)M;
+      rows = std::max(rows, (int64_t)fp4_splits(N, Kd) * direct);
+    }
+    return rows;
+  };
+  c->parts = a.arr<float>(d * std::max(layer_rows(Px, (int)d, hdim, EPI_PARTIAL),
+                                       layer_rows(Px, (int)d, (int)F, EPI_PARTIAL)));
+  if (m->w4 && gemm_fp4_unpacks(m->dt, (int)Px, (int)d))
+    c->w4_wide = a.take(d * std::max<size_t>(3 * hdim, 2 * F) * es);
   // split-K scratch: the most that a launch of this context leaves to a
   // finishing pass (partials are indexed with the full packed width)
   size_t scr = 1;
   auto need = [&](size_t M, int cols, int n_full, int Kd, int kind) {
     scr = std::max(scr, (size_t)gemm_partial_rows(m->dt, (int)M, cols, Kd, kind) * n_full);
   };
-  need(Px, 3 * hdim, 3 * hdim, (int)d, EPI_QKV);
-  need(Px, 2 * (int)F, 2 * (int)F, (int)d, EPI_SWIGLU);
+  scr = std::max(scr, (size_t)layer_rows(Px, 3 * hdim, (int)d, EPI_QKV) * 3 * hdim);
+  scr = std::max(scr, (size_t)layer_rows(Px, 2 * (int)F, (int)d, EPI_SWIGLU) * 2 * F);
   need(Mv, (int)V, (int)V, (int)d, EPI_F32);
   if (K > 0) {
     need(Pd, (int)d, (int)d, 3 * (int)d, EPI_SILU);
@@ -754,6 +842,16 @@ void carve_ctx(chimera_ctx* c, Arena& a) {
   c->part_o = a.arr<float>(part_rows * H * hd);
   c->part_ml = a.arr<float>(part_rows * H * 2);
   c->rowtab = a.arr<int64_t>(std::max(B, nblk_pf) * TREE_ATTN_TAIL_ROWS);
+  if (c->kv->fp4) {
+    c->kv_rows = a.take(Px * 2 * hdim * es);
+    c->kv_row = a.arr<int64_t>(Px);
+    // the largest over the batches a prefill may bring
+    size_t most = 0;
+    for (int b = 1; b <= (int)B; ++b)
+      most = std::max(most, (size_t)kv4_attn_bytes(b, (int64_t)c->kv->max_pages * c->kv->ps, (int)H, (int)H, (int)hd,
+                                                   (int)N));
+    c->attn4.part_o = (float*)a.take(most);
+  }
   c->t_lse = a.arr<double>(Mv);
   c->t_H = a.arr<double>(Mv);
   c->t_sample = a.arr<int>(Mv);
@@ -864,9 +962,10 @@ double verify_pass_bytes(const chimera_ctx* c, double sum_n) {
   const chimera_config& cf = m->cfg;
   const double es = (double)m->es, d = cf.d_model, F = cf.d_ffn, V = cf.vocab;
   const double hdim = (double)cf.n_heads * cf.head_dim;
-  const double w_layer = (d * 3 * hdim + hdim * d + d * 2 * F + F * d) * es + 2 * d * 4;
+  const double w_layer = (d * 3 * hdim + hdim * d + d * 2 * F + F * d) * (m->w4 ? 17.0 / 32.0 : es) + 2 * d * 4;
   const double bytes = cf.n_layers * w_layer + d * V * es + d * 4;
-  return bytes + (double)cf.n_layers * 2 * hdim * es * (sum_n + (double)c->batch * c->N);
+  const double kv_es = c->kv->fp4 ? 17.0 / 32.0 : es;
+  return bytes + (double)cf.n_layers * 2 * hdim * kv_es * (sum_n + (double)c->batch * c->N);
 }
 
 }  // namespace
@@ -880,12 +979,13 @@ const char* chimera_last_error(void) { return g_err.c_str(); }
 
 chimera_status chimera_weight_bytes(const chimera_config* cfg, int64_t* bytes) {
   return guard([&] {
-    validate_config(cfg);
+    const ModelConfig mc = validate_config(cfg);
     REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
     Arena a{nullptr, 0};
     chimera_model tmp;
-    tmp.cfg = *cfg;
-    carve_model(*cfg, a, tmp);
+    tmp.cfg = mc.cfg;
+    tmp.w4 = mc.w4;
+    carve_model(mc.cfg, a, tmp);
     *bytes = (int64_t)a.off + 256;
   });
 }
@@ -893,10 +993,10 @@ chimera_status chimera_weight_bytes(const chimera_config* cfg, int64_t* bytes) {
 chimera_status chimera_load(const chimera_config* cfg, const chimera_tensor* tensors, int32_t n_tensors, void* arena,
                             int64_t arena_bytes, void* stream, chimera_model** out) {
   return guard([&] {
-    validate_config(cfg);
+    const ModelConfig mc = validate_config(cfg);
     REQUIRE(out != nullptr && arena != nullptr && tensors != nullptr, CHIMERA_EINVAL, "null argument");
     hipStream_t st = (hipStream_t)stream;
-    const chimera_config& c = *cfg;
+    const chimera_config& c = mc.cfg;
     const int dt = c.dtype;
     const size_t es = esize(dt);
     const int64_t d = c.d_model, F = c.d_ffn, V = c.vocab, hdim = (int64_t)c.n_heads * c.head_dim;
@@ -942,6 +1042,7 @@ chimera_status chimera_load(const chimera_config* cfg, const chimera_tensor* ten
     {
       Arena a{nullptr, 0};
       chimera_model tmp;
+      tmp.w4 = mc.w4;
       carve_model(c, a, tmp);
       need = (int64_t)a.off;
     }
@@ -951,6 +1052,7 @@ chimera_status chimera_load(const chimera_config* cfg, const chimera_tensor* ten
       m->cfg = c;
       m->dt = dt;
       m->es = es;
+      m->w4 = mc.w4;
       Arena a{(char*)arena, (size_t)arena_bytes};
       carve_model(c, a, *m);
       auto dev = [&](const std::string& name) -> const void* { return have[name]->data; };
@@ -960,28 +1062,32 @@ chimera_status chimera_load(const chimera_config* cfg, const chimera_tensor* ten
         HIPCK(hipMemcpyAsync(dst, t->data, bytes, hipMemcpyDeviceToDevice, st));
       };
       auto pack = [&](void* dst, int kind, const std::string& a0, const std::string& a1, const std::string& a2, int K,
-                      int n_src) {
+                      int n_src, bool w4 = false) {
         const void* s0 = dev(a0);
         const void* s1 = a1.empty() ? nullptr : dev(a1);
         const void* s2 = a2.empty() ? nullptr : dev(a2);
-        launch_repack(dt, kind, s0, s1, s2, K, n_src, dst, c.n_heads, c.head_dim, st);
+        if (w4)
+          launch_fp4_pack(dt, kind, s0, s1, s2, n_src, n_src * (kind == PACK_QKV ? 3 : (kind == PACK_GU ? 2 : 1)), K, dst,
+                          c.n_heads, c.head_dim, st);
+        else
+          launch_repack(dt, kind, s0, s1, s2, K, n_src, dst, c.n_heads, c.head_dim, st);
         HIPCK(hipGetLastError());
       };
-      auto block = [&](const std::string& p, BlockW& w) {
+      auto block = [&](const std::string& p, BlockW& w, bool w4) {
         copy(w.attn_norm, p + "attn_norm");
         copy(w.ffn_norm, p + "ffn_norm");
-        pack(w.wqkv, PACK_QKV, p + "wq", p + "wk", p + "wv", (int)d, (int)hdim);
-        pack(w.wo, PACK_NATURAL, p + "wo", "", "", (int)hdim, (int)d);
-        pack(w.wgu, PACK_GU, p + "w_gate", p + "w_up", "", (int)d, (int)F);
-        pack(w.wdown, PACK_NATURAL, p + "w_down", "", "", (int)F, (int)d);
+        pack(w.wqkv, PACK_QKV, p + "wq", p + "wk", p + "wv", (int)d, (int)hdim, w4);
+        pack(w.wo, PACK_NATURAL, p + "wo", "", "", (int)hdim, (int)d, w4);
+        pack(w.wgu, PACK_GU, p + "w_gate", p + "w_up", "", (int)d, (int)F, w4);
+        pack(w.wdown, PACK_NATURAL, p + "w_down", "", "", (int)F, (int)d, w4);
       };
       copy(m->embed, "tok_embed");
-      for (int l = 0; l < c.n_layers; ++l) block("layers." + std::to_string(l) + ".", m->layers[l]);
+      for (int l = 0; l < c.n_layers; ++l) block("layers." + std::to_string(l) + ".", m->layers[l], mc.w4);
       copy(m->final_norm, "final_norm");
       pack(m->lm_head, PACK_NATURAL, "lm_head", "", "", (int)d, (int)V);
       pack(m->tri_w1, PACK_NATURAL, "draft.tri_w1", "", "", (int)(3 * d), (int)d);
       pack(m->tri_w2, PACK_NATURAL, "draft.tri_w2", "", "", (int)d, (int)d);
-      block("draft.enc.", m->enc);
+      block("draft.enc.", m->enc, false);
       for (int k = 0; k < c.n_draft_heads; ++k) {
         const std::string p = "draft.heads." + std::to_string(k) + ".";
         pack(m->head_a[k], PACK_NATURAL, p + "a", "", "", (int)(2 * d), (int)d);
@@ -1022,49 +1128,59 @@ static void carve_kv(chimera_kv* kv, Arena& a) {
   const chimera_model* m = kv->m;
   const chimera_config& c = m->cfg;
   const size_t es = m->es, H = c.n_heads, hd = c.head_dim;
-  kv->pool = a.take((size_t)c.n_layers * kv->n_pages * 2 * H * kv->ps * hd * es);
+  const size_t layer = (size_t)kv->n_pages * 2 * H * kv->ps * hd;  // elements
+  if (kv->fp4) {
+    kv->pool = a.take((size_t)c.n_layers * kv->layer_stride);
+    kv->wide = a.take(layer * es);
+  } else {
+    kv->pool = a.take((size_t)c.n_layers * layer * es);
+  }
   kv->page_table = a.arr<int>((size_t)kv->B * kv->max_pages);
   kv->enc_k = a.take((size_t)kv->B * 2 * H * kv->cap * hd * es);
   kv->enc_v = a.take((size_t)kv->B * 2 * H * kv->cap * hd * es);
 }
 
-chimera_status chimera_kv_bytes(const chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
-                                int32_t page_size, int64_t* bytes) {
+static void kv_shape(chimera_kv* kv, chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                     int32_t page_size, bool fp4) {
+  kv->m = m;
+  kv->B = max_batch;
+  kv->max_len = max_len;
+  kv->n_pages = n_pages;
+  kv->ps = page_size;
+  kv->max_pages = (max_len + 64 + page_size - 1) / page_size;
+  kv->cap = max_len + 64 + ENC_TREE_SLOTS;
+  kv->fp4 = fp4;
+  const int64_t H = m->cfg.n_heads, hd = m->cfg.head_dim;
+  kv->page_stride = 2 * H * page_size * hd;
+  kv->layer_stride = (int64_t)n_pages * kv->page_stride;
+  if (fp4) {
+    REQUIRE(kv->layer_stride / 32 < (int64_t)1 << 32, CHIMERA_EINVAL, "a 4-bit layer's pool over 68 GiB");
+    kv->layer_stride = (kv->layer_stride / 32 * 17 + 255) / 256 * 256;
+  }
+}
+
+static chimera_status kv_bytes(const chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                               int32_t page_size, bool fp4, int64_t* bytes) {
   return guard([&] {
     kv_dims(m, max_batch, max_len, n_pages, page_size);
     REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
     chimera_kv kv;
-    kv.m = const_cast<chimera_model*>(m);
-    kv.B = max_batch;
-    kv.max_len = max_len;
-    kv.n_pages = n_pages;
-    kv.ps = page_size;
-    kv.max_pages = (max_len + 64 + page_size - 1) / page_size;
-    kv.cap = max_len + 64 + ENC_TREE_SLOTS;
+    kv_shape(&kv, const_cast<chimera_model*>(m), max_batch, max_len, n_pages, page_size, fp4);
     Arena a{nullptr, 0};
     carve_kv(&kv, a);
     *bytes = (int64_t)a.off + 256;
   });
 }
 
-chimera_status chimera_kv_create(chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
-                                 int32_t page_size, const int32_t* page_order, void* arena, int64_t arena_bytes,
-                                 chimera_kv** out) {
+static chimera_status kv_create(chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                                int32_t page_size, const int32_t* page_order, bool fp4, void* arena,
+                                int64_t arena_bytes, chimera_kv** out) {
   return guard([&] {
     kv_dims(m, max_batch, max_len, n_pages, page_size);
     REQUIRE(out != nullptr && arena != nullptr, CHIMERA_EINVAL, "null argument");
     auto* kv = new chimera_kv();
     try {
-      kv->m = m;
-      kv->B = max_batch;
-      kv->max_len = max_len;
-      kv->n_pages = n_pages;
-      kv->ps = page_size;
-      kv->max_pages = (max_len + 64 + page_size - 1) / page_size;
-      kv->cap = max_len + 64 + ENC_TREE_SLOTS;
-      const int64_t H = m->cfg.n_heads, hd = m->cfg.head_dim;
-      kv->page_stride = 2 * H * page_size * hd;
-      kv->layer_stride = (int64_t)n_pages * kv->page_stride;
+      kv_shape(kv, m, max_batch, max_len, n_pages, page_size, fp4);
       Arena a{(char*)arena, (size_t)arena_bytes};
       carve_kv(kv, a);
       std::vector<int> order(n_pages);
@@ -1087,6 +1203,25 @@ chimera_status chimera_kv_create(chimera_model* m, int32_t max_batch, int32_t ma
     }
     *out = kv;
   });
+}
+
+chimera_status chimera_kv_bytes(const chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                                int32_t page_size, int64_t* bytes) {
+  return kv_bytes(m, max_batch, max_len, n_pages, page_size, false, bytes);
+}
+chimera_status chimera_kv_create(chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                                 int32_t page_size, const int32_t* page_order, void* arena, int64_t arena_bytes,
+                                 chimera_kv** out) {
+  return kv_create(m, max_batch, max_len, n_pages, page_size, page_order, false, arena, arena_bytes, out);
+}
+chimera_status chimera_kv_fp4_bytes(const chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                                    int32_t page_size, int64_t* bytes) {
+  return kv_bytes(m, max_batch, max_len, n_pages, page_size, true, bytes);
+}
+chimera_status chimera_kv_fp4_create(chimera_model* m, int32_t max_batch, int32_t max_len, int32_t n_pages,
+                                     int32_t page_size, const int32_t* page_order, void* arena, int64_t arena_bytes,
+                                     chimera_kv** out) {
+  return kv_create(m, max_batch, max_len, n_pages, page_size, page_order, true, arena, arena_bytes, out);
 }
 
 static void tree_from(const int32_t* parent, const int32_t* rank, int32_t n_nodes, int n_heads, chimera_ctx* c) {
@@ -1164,6 +1299,23 @@ chimera_status chimera_ctx_create(chimera_model* m, chimera_kv* kv, const int32_
       }
       upload_meta(c->chain, cp, cr, cd, ca);
       set_draft_plan(c);
+      if (kv->fp4) {
+        const size_t rows = std::max(c->Mv, c->Mp), hdim = (size_t)m->cfg.n_heads * m->cfg.head_dim;
+        std::vector<int64_t> off(rows);
+        for (size_t r = 0; r < rows; ++r) off[r] = (int64_t)(r * 2 * hdim);
+        HIPCK(hipMemcpy(c->kv_row, off.data(), rows * sizeof(int64_t), hipMemcpyHostToDevice));
+        Kv4AttnArgs& f = c->attn4;
+        f.q = c->q;
+        f.ldq = (int64_t)hdim;
+        f.out = c->attn;
+        f.ldo = (int64_t)hdim;
+        f.n_b = c->n;
+        f.Hq = m->cfg.n_heads;
+        f.N = c->N;
+        f.deepest = c->D;
+        f.scale = 1.0f / std::sqrt((float)m->cfg.head_dim);
+        for (int u = 0; u < c->N; ++u) f.tree.set(u, c->parent[u]);
+      }
       HIPCK(hipMemcpy(c->s_k_dev, c->s_k.data(), 8 * sizeof(int), hipMemcpyHostToDevice));
       HIPCK(hipMemset(c->inject_on, 0, sizeof(int)));
       HIPCK(hipMemset(c->tri.miss, 0, sizeof(int)));
@@ -1280,7 +1432,7 @@ void enqueue_step(chimera_ctx* ctx, hipStream_t st) {
     launch_verify_setup(dt, s, m->embed, ctx->x, ctx->rowtab, q);
     const int M = ctx->batch * ctx->N;
     VerifyRows r{ctx->tree_tok, M, ctx->n, kv->page_table, ctx->tree.depth, ctx->tree.path, ctx->N, ctx->D,
-                 ctx->batch, ctx->mt_v, nullptr};
+                 ctx->batch, ctx->mt_v, nullptr, nullptr};
     verify_layers(ctx, r, q, true);
     GemmEpi el;
     el.kind = EPI_F32;
@@ -1293,7 +1445,10 @@ void enqueue_step(chimera_ctx* ctx, hipStream_t st) {
     else
       launch_argmax(ctx->logits, M, V, ctx->amax, q);
     if (ctx->cc_side) launch_kv_snapshot(dt, s, kv->pool, cf.n_layers, kv->layer_stride, ctx->cc_side, q);
-    launch_step_end(dt, s, kv->pool, cf.n_layers, kv->layer_stride, q);
+    if (kv->fp4)
+      launch_step_end_fp4(dt, s, kv4_layer(kv, 0, ctx->batch), cf.n_layers, kv->layer_stride, q);
+    else
+      launch_step_end(dt, s, kv->pool, cf.n_layers, kv->layer_stride, q);
     if (ctx->cc_side)
       launch_kv_check(dt, s, kv->pool, cf.n_layers, kv->layer_stride, ctx->cc_side, ctx->cc_counts, q);
     launch_stamp(s, q);
@@ -1483,6 +1638,35 @@ chimera_status chimera_kv_read(chimera_kv* kv, int32_t layer, int32_t b, int32_t
     REQUIRE(pos0 >= 0 && count >= 0 && pos0 + count <= kv->max_pages * kv->ps, CHIMERA_EINVAL, "position range");
     const size_t es = kv->m->es, H = c.n_heads, hd = c.head_dim;
     HIPCK(hipDeviceSynchronize());
+    if (kv->fp4) {
+      // the values that the codes stand for, in the model's dtype (exact in both)
+      const Kv4View view = kv4_layer(kv, layer, kv->B);
+      std::vector<uint8_t> codes(hd / 2), scales(hd / 32);
+      for (int i = 0; i < count; ++i)
+        for (size_t t = 0; t < 2 * H; ++t) {  // K's heads, then V's
+          const int p = pos0 + i;
+          const int64_t page = kv->page_table_host[(size_t)b * kv->max_pages + p / kv->ps];
+          const int64_t e = page * kv->page_stride + ((int64_t)t * kv->ps + p % kv->ps) * (int64_t)hd;
+          HIPCK(hipMemcpy(codes.data(), view.codes + e / 2, hd / 2, hipMemcpyDeviceToHost));
+          HIPCK(hipMemcpy(scales.data(), view.scales + e / 32, hd / 32, hipMemcpyDeviceToHost));
+          char* dst = (char*)(t < H ? k_out : v_out) + (((size_t)i * H + t % H) * hd) * es;
+          for (size_t x = 0; x < hd; ++x) {
+            static const float grid[8] = {0.f, 0.5f, 1.f, 1.5f, 2.f, 3.f, 4.f, 6.f};
+            const int code = (codes[x / 2] >> (4 * (x & 1))) & 15, sc = scales[x / 32];
+            float val = sc == 255 ? NAN : std::ldexp(grid[code & 7], sc - 127);
+            if (code & 8) val = -val;
+            uint32_t bits;
+            std::memcpy(&bits, &val, 4);
+            if (es == 2) {
+              const uint16_t h = (uint16_t)(bits >> 16);
+              std::memcpy(dst + x * 2, &h, 2);
+            } else {
+              std::memcpy(dst + x * 4, &bits, 4);
+            }
+          }
+        }
+      return;
+    }
     for (int i = 0; i < count; ++i) {
       const int p = pos0 + i;
       const int page = kv->page_table_host[(size_t)b * kv->max_pages + p / kv->ps];
@@ -1781,6 +1965,7 @@ chimera_status chimera_set_compaction_check(chimera_ctx* ctx, void* arena, int64
       ctx->cc_counts = nullptr;
       return;
     }
+    REQUIRE(!ctx->kv->fp4, CHIMERA_EINVAL, "the compaction check reads a cache of the model's dtype, not a 4-bit one");
     int64_t need = 0;
     chimera_compaction_check_bytes(ctx, &need);
     REQUIRE(arena_bytes >= need, CHIMERA_ENOMEM, "compaction check arena too small");

@@ -117,7 +117,9 @@ void launch_fp4_pack(int dtype, int kind, const void* s0, const void* s1, const 
 void launch_fp4_unpack_rows(int dtype, const void* packed, int N, int K, void* dst, int64_t ldw, hipStream_t st);
 // Row-major x [M][ldx] -> tiled.
 void launch_tile_strided(int dtype, const void* x, int64_t ldx, int M, int K, void* dst, int mtiles, hipStream_t st);
-// Whether launches of M rows run on the bf16 kernels over the unpacked matrix.
+// Whether launches of M rows run on the bf16 kernels over the unpacked matrix:
+// bf16, whole 64-column groups, more than FP4_DIRECT_ROWS rows.
+constexpr int FP4_DIRECT_ROWS = 128;
 bool gemm_fp4_unpacks(int dtype, int M, int N);
 // s.W: the packed matrix, s.splits = fp4_splits(N, K), all columns.  ldx > 0: X
 // is row-major (at most 16 rows, 16-byte aligned rows).  unpacked: room for the
@@ -427,3 +429,12 @@ void launch_prefill_finish(const StepState& s, const PrefillEnds& e, const int* 
 constexpr int STAMP_RING = 4096;
 constexpr int STAMP_WORDS = 8;
 void launch_stamp(const StepState& s, hipStream_t st);
+
+// ---- a 4-bit cache in the step ----------------------------------------------
+// The positions that a prefill chunk's sequences hold, through the chunk's last
+// ones, as values into a pool of the model's dtype with the same page table.
+void launch_kv4_expand(int dtype, const Kv4View& c, const PrefillChunk& chunk, void* pool, hipStream_t st);
+// launch_step_end with the compaction in 4-bit layers; layer0: the first, the
+// others layer_bytes apart.
+void launch_step_end_fp4(int dtype, const StepState& s, const Kv4View& layer0, int n_layers, int64_t layer_bytes,
+                         hipStream_t st);

@@ -458,4 +458,4 @@ void launch_gemm_fp4(int dtype, const GemmShape& s, const GemmEpi& e, int64_t ld
   if (finish) launch_gemm_finish(dtype, s, e, st, ev_stop);
 }
 
-bool gemm_fp4_unpacks(int dtype, int M, int N) { return dtype == DT_BF16 && N % 64 == 0 && M > 128; }
+bool gemm_fp4_unpacks(int dtype, int M, int N) { return dtype == DT_BF16 && N % 64 == 0 && M > FP4_DIRECT_ROWS; }

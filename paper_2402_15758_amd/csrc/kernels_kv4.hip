@@ -74,6 +74,26 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T* __res
   for (int j = 0; j < 8; ++j) dst[j] = ET<T>::from_f(j < 4 ? a[j & 3] : b[j & 3]);
 }
 
+// A layer's rows as values, for prefill attention: grid (positions / 64, 2 H,
+// segments), a thread 8 values of one of 64 positions at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void kv4_expand_kernel(const Kv4View c, const PrefillChunk ch, T* __restrict__ pool) {
+  const int seg = blockIdx.z, b = ch.seq[seg], t = blockIdx.y;
+  const int end = ch.p0[seg] + ch.row0[seg + 1] - ch.row0[seg];  // positions this sequence holds
+  const int per = c.hd / 8;
+  for (int i = threadIdx.x; i < 64 * per; i += 256) {
+    const int p = blockIdx.x * 64 + i / per;
+    const int64_t base = p < end ? kv4_slot(c, b, p) : (int64_t)-1;
+    if (base < 0) continue;
+    const int64_t e = base + (int64_t)t * c.ps * c.hd + i % per * 8;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(c.codes + e / 2);
+    Frag32<T> f;
+    f.from_fp4(w, fp4_scale(c.scales[e / 32]));
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) st16(pool + e + 4 * j, f.v[j]);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Attention.  Query (u, h) sits at position P = n + depth(u) and sees the
 // logical keys 0 .. P, position n + e being the slot of u's depth-e ancestor.
@@ -634,6 +654,16 @@ void launch_kv4_read(int dtype, const Kv4View& c, void* k, void* v, int64_t ld, 
     hipLaunchKernelGGL(kv4_read_kernel<bf16_t>, grid, dim3(256), 0, st, c, (bf16_t*)k, (bf16_t*)v, ld, seq, pos, rows);
   else
     hipLaunchKernelGGL(kv4_read_kernel<float>, grid, dim3(256), 0, st, c, (float*)k, (float*)v, ld, seq, pos, rows);
+}
+
+void launch_kv4_expand(int dtype, const Kv4View& c, const PrefillChunk& chunk, void* pool, hipStream_t st) {
+  int end = 0;
+  for (int k = 0; k < chunk.n_seg; ++k) end = std::max(end, chunk.p0[k] + chunk.row0[k + 1] - chunk.row0[k]);
+  const dim3 grid((end + 63) / 64, 2 * c.H, chunk.n_seg);
+  if (dtype == DT_BF16)
+    hipLaunchKernelGGL(kv4_expand_kernel<bf16_t>, grid, dim3(256), 0, st, c, chunk, (bf16_t*)pool);
+  else
+    hipLaunchKernelGGL(kv4_expand_kernel<float>, grid, dim3(256), 0, st, c, chunk, (float*)pool);
 }
 
 int kv4_attn_blocks(int B, int Hq, int H, int N) { return B * H * ((N * (Hq / H) + 15) / 16); }

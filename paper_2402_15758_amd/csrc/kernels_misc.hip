@@ -666,8 +666,11 @@ __global__ __launch_bounds__(256) void kv_check_kernel(StepState s, const T* poo
 //     for the last one); idx 0 also publishes the path, commits the tokens and
 //     advances n -- the committed length the others use is the root's position,
 //     which only the next step rewrites.
-template <typename T>
-__global__ __launch_bounds__(256) void step_end_kernel(StepState s, T* pool, int n_layers, int64_t layer_stride) {
+// FP4: pool is the first layer's codes, its scale bytes `scales` further (fp4.h);
+// layer_stride is then in bytes.
+template <typename T, bool FP4>
+__global__ __launch_bounds__(256) void step_end_kernel(StepState s, T* pool, int64_t scales, int n_layers,
+                                                       int64_t layer_stride) {
   __shared__ int nodes[2 * MAX_PATH];  // path nodes, then accepted tokens and bonus
   __shared__ int len;
   const int b = blockIdx.y, part = blockIdx.x - 2 * n_layers;
@@ -682,6 +685,24 @@ __global__ __launch_bounds__(256) void step_end_kernel(StepState s, T* pool, int
   constexpr int VEC = ET<T>::VEC;
   if (part < 0) {
     const int layer = blockIdx.x / 2, kv = blockIdx.x % 2;
+    if constexpr (FP4) {  // a thread a group of 32 values: 16 code bytes and a scale byte
+      uint8_t* codes = (uint8_t*)pool + (int64_t)layer * layer_stride;
+      const int* ptab = s.page_table + (int64_t)b * s.max_pages;
+      const int groups = s.H * s.hd / 32;
+      for (int dd = 1; dd < L; ++dd) {
+        const int src = n + nodes[dd], dst = n + dd;
+        if (src == dst) continue;
+        const int64_t half = (int64_t)kv * s.H * s.ps * s.hd;
+        const int64_t sb = half + (int64_t)ptab[src / s.ps] * s.page_stride + (int64_t)(src % s.ps) * s.hd;
+        const int64_t db = half + (int64_t)ptab[dst / s.ps] * s.page_stride + (int64_t)(dst % s.ps) * s.hd;
+        for (int e = threadIdx.x; e < groups; e += 256) {
+          const int64_t ho = (int64_t)(e * 32 / s.hd) * s.ps * s.hd + e * 32 % s.hd;
+          st16(codes + (db + ho) / 2, ld16(codes + (sb + ho) / 2));
+          codes[scales + (db + ho) / 32] = codes[scales + (sb + ho) / 32];
+        }
+      }
+      return;
+    }
     T* base = pool + (int64_t)layer * layer_stride + (int64_t)kv * s.H * s.ps * s.hd;
     const int* ptab = s.page_table + (int64_t)b * s.max_pages;
     const int nvec = s.H * s.hd / VEC;
@@ -1085,9 +1106,22 @@ void launch_typical_stats(const float* logits, int rows, int V, int N, int b0, c
 void launch_step_end(int dtype, const StepState& s, void* pool, int n_layers, int64_t layer_stride, hipStream_t st) {
   const dim3 grid(2 * n_layers + s.K + 1, s.B);
   if (dtype == DT_BF16)
-    hipLaunchKernelGGL(step_end_kernel<bf16_t>, grid, dim3(256), 0, st, s, (bf16_t*)pool, n_layers, layer_stride);
+    hipLaunchKernelGGL((step_end_kernel<bf16_t, false>), grid, dim3(256), 0, st, s, (bf16_t*)pool, (int64_t)0, n_layers,
+                       layer_stride);
   else
-    hipLaunchKernelGGL(step_end_kernel<float>, grid, dim3(256), 0, st, s, (float*)pool, n_layers, layer_stride);
+    hipLaunchKernelGGL((step_end_kernel<float, false>), grid, dim3(256), 0, st, s, (float*)pool, (int64_t)0, n_layers,
+                       layer_stride);
+}
+void launch_step_end_fp4(int dtype, const StepState& s, const Kv4View& layer0, int n_layers, int64_t layer_bytes,
+                         hipStream_t st) {
+  const dim3 grid(2 * n_layers + s.K + 1, s.B);
+  const int64_t scales = layer0.scales - layer0.codes;
+  if (dtype == DT_BF16)
+    hipLaunchKernelGGL((step_end_kernel<bf16_t, true>), grid, dim3(256), 0, st, s, (bf16_t*)layer0.codes, scales,
+                       n_layers, layer_bytes);
+  else
+    hipLaunchKernelGGL((step_end_kernel<float, true>), grid, dim3(256), 0, st, s, (float*)layer0.codes, scales,
+                       n_layers, layer_bytes);
 }
 
 void launch_kv_snapshot(int dtype, const StepState& s, const void* pool, int n_layers, int64_t layer_stride,

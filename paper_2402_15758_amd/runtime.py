@@ -28,12 +28,19 @@ class Session:
 
     ``cfg`` provides n_layers, d_model, n_heads, head_dim, d_ffn, vocab,
     n_draft_heads, rope_base, rms_eps and dtype ("f32" | "bf16");
-    ``weights`` maps the canonical tensor names to torch tensors."""
+    ``weights`` maps the canonical tensor names to torch tensors.
+    ``weight_format`` "fp4" holds the target layers' matrices in 4 bits,
+    ``kv_format`` "fp4" the target's K and V."""
 
     def __init__(self, cfg, weights: Optional[Dict[str, "object"]], tree_ranks, max_batch: int = 1,
                  max_len: int = 1024, page_size: int = 16, page_order: Optional[np.ndarray] = None,
-                 device: str = "cuda", share_model: Optional["Session"] = None):
+                 device: str = "cuda", share_model: Optional["Session"] = None,
+                 weight_format: str = "native", kv_format: str = "native"):
         import torch
+
+        for f in (weight_format, kv_format):
+            if f not in ("native", "fp4"):
+                raise ValueError('weight_format and kv_format are "native" or "fp4"')
 
         self.torch = torch
         self.device = torch.device(device)
@@ -41,13 +48,14 @@ class Session:
         self.dt = B.CHIMERA_BF16 if cfg.dtype == "bf16" else B.CHIMERA_F32
         self.max_batch, self.max_len = max_batch, max_len
         c = B.chimera_config(cfg.n_layers, cfg.d_model, cfg.n_heads, cfg.head_dim, cfg.d_ffn, cfg.vocab,
-                             cfg.n_draft_heads, float(cfg.rope_base), float(cfg.rms_eps), self.dt, max_len + 128)
+                             cfg.n_draft_heads, float(cfg.rope_base), float(cfg.rms_eps),
+                             self.dt | (B.CHIMERA_WEIGHTS_FP4 if weight_format == "fp4" else 0), max_len + 128)
         self._c = c
         self._owner = share_model is None
         if share_model is not None:
             # another decode state over the same loaded weights
-            if share_model.cfg != cfg or share_model.max_len < max_len:
-                raise ValueError("shared model has another config or a shorter rotary table")
+            if share_model.cfg != cfg or share_model.max_len < max_len or share_model._c.dtype != c.dtype:
+                raise ValueError("shared model has another config or weight format, or a shorter rotary table")
             self.w_arena, self.model = share_model.w_arena, share_model.model
             self._c = share_model._c
         else:
@@ -67,10 +75,12 @@ class Session:
         self.n_pages = max_batch * math.ceil((max_len + 64) / page_size)
         if page_order is not None:
             page_order = np.ascontiguousarray(page_order, dtype=np.int32)
-        kb = B.chimera_kv_bytes(self.model, max_batch, max_len, self.n_pages, page_size)
+        kv_bytes, kv_create = ((B.chimera_kv_fp4_bytes, B.chimera_kv_fp4_create) if kv_format == "fp4" else
+                               (B.chimera_kv_bytes, B.chimera_kv_create))
+        kb = kv_bytes(self.model, max_batch, max_len, self.n_pages, page_size)
         self.kv_arena = torch.empty(kb, dtype=torch.uint8, device=self.device)
-        self.kv = B.chimera_kv_create(self.model, max_batch, max_len, self.n_pages, page_size, page_order,
-                                      self.kv_arena.data_ptr(), kb)
+        self.kv = kv_create(self.model, max_batch, max_len, self.n_pages, page_size, page_order,
+                            self.kv_arena.data_ptr(), kb)
         parent, rank = tree_arrays(tree_ranks)
         self.n_nodes = len(parent)
         self.K = max((len(r) for r in tree_ranks), default=0)

@@ -1,0 +1,202 @@
+"""The decode engine over 4-bit weights and a 4-bit KV cache."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+import fp4_ref as R
+import oracle
+import synth
+from gpu_helpers import TieLog, check_step, gpu_step, log, tau
+from paper_2402_15758_amd import Session
+from paper_2402_15758_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+SMALL = synth.small_config()
+LAYER_MATS = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down")
+
+
+def rounded(w):
+    """The weights with the target layers' matrices as 4 bits hold them."""
+    out = dict(w)
+    for name, t in w.items():
+        if name.startswith("layers.") and name.split(".")[-1] in LAYER_MATS:
+            out[name] = R.held(t.t().contiguous().cpu()).t().contiguous().to(t.dtype)
+    return out
+
+
+def prompts(lens, vocab, seed):
+    rng = np.random.default_rng(seed)
+    return [rng.integers(0, vocab, n).astype(np.int32) for n in lens]
+
+
+def run(sess, ps, steps, pipelined=False):
+    first = sess.prefill(ps)
+    toks, lens, logits = [], [], []
+    if pipelined:
+        t, n, _ = sess.steps(steps)
+        return first, list(t), list(n), logits
+    for _ in range(steps):
+        t, n, _ = sess.step()
+        toks.append(t)
+        lens.append(n)
+        logits.append(sess.debug(B.DBG_VERIFY_LOGITS))
+    return first, toks, lens, logits
+
+
+@pytest.mark.parametrize("lens,tree,batch", [([61], "T64", 1), ([300, 7, 129], "T32", 3), ([700], "none", 1)])
+def test_4bit_weights_are_the_rounded_model_bit_for_bit(lens, tree, batch):
+    """Verify launches below and above 128 rows, prefill chunks, graph replay."""
+    w = synth.make_weights(SMALL, std=0.06)
+    tr = () if tree == "none" else synth.TREES[tree]
+    a = Session(SMALL, w, tr, max_batch=batch, max_len=1024, weight_format="fp4")
+    b = Session(SMALL, rounded(w), tr, max_batch=batch, max_len=1024)
+    assert a.w_arena.numel() < b.w_arena.numel()
+    ps = prompts(lens, SMALL.vocab, 3)
+    ra, rb = run(a, ps, 4), run(b, ps, 4)
+    assert np.array_equal(ra[0], rb[0])
+    for x, y in zip(ra[1] + ra[2] + ra[3], rb[1] + rb[2] + rb[3]):
+        assert np.array_equal(x, y)
+    a.close()
+    b.close()
+
+
+@pytest.mark.parametrize("d,ffn,layers", [(1024, 4096, 1)])
+def test_4bit_weights_with_split_reductions(d, ffn, layers):
+    """A width whose products split the reduction, up to 288 verify rows."""
+    cfg = dataclasses.replace(SMALL, d_model=d, n_heads=d // 128, d_ffn=ffn, n_layers=layers)
+    w = synth.make_weights(cfg, std=0.04)
+    ps = prompts([40, 11, 70, 25, 8, 33, 90, 64, 17], cfg.vocab, 5)
+    outs = []
+    for weights, fmt in ((w, "fp4"), (rounded(w), "native")):
+        s = Session(cfg, weights, synth.TREES["T32"], max_batch=9, max_len=256, weight_format=fmt)
+        outs.append(run(s, ps, 3))
+        s.close()
+    for i in range(1, 4):
+        for x, y in zip(outs[0][i], outs[1][i]):
+            assert np.array_equal(x, y)
+
+
+class Kv4Oracle(oracle.Oracle):
+    """The oracle with the target's K and V rounded to 4 bits where they are stored."""
+
+    def block_kv(self, prefix, x, pos):
+        xn, k, v = super().block_kv(prefix, x, pos)
+        if prefix.startswith("layers."):
+            k, v = (R.held(torch.from_numpy(np.ascontiguousarray(a)).double()).numpy().astype(self.ct) for a in (k, v))
+        return xn, k, v
+
+
+@pytest.mark.parametrize("wfmt", ["native", "fp4"])
+def test_tiny_fp32_against_the_oracle(wfmt):
+    """Every step's lists, tree, logits and path against the oracle driven along
+    the GPU's state."""
+    cfg = synth.TINY
+    w = synth.make_weights(cfg)
+    log(f"tiny fp32, 4-bit KV, {wfmt} weights")
+    orc = Kv4Oracle(cfg, synth.weights_to_numpy(rounded(w) if wfmt == "fp4" else w))
+    sess = Session(cfg, w, synth.TREE_T8, max_len=256, weight_format=wfmt, kv_format="fp4")
+    prompt = synth.WORKLOADS["tiny"].prompts()[0]
+    dec = oracle.Decoder(orc, synth.TREE_T8)
+    assert int(sess.prefill([prompt])[0]) == dec.prefill(list(prompt))
+    ties = TieLog()
+    for _ in range(12):
+        art = gpu_step(sess)
+        check_step(art, 0, dec, tau(cfg), ties)
+    sess.close()
+
+
+@pytest.mark.parametrize("n,tree", [(90, "T64"), (600, "T32")])
+def test_small_bf16_against_the_oracle(n, tree):
+    w = synth.make_weights(SMALL)
+    orc = Kv4Oracle(SMALL, synth.weights_to_numpy(w))
+    sess = Session(SMALL, w, synth.TREES[tree], max_len=1024, kv_format="fp4")
+    p = prompts([n], SMALL.vocab, 8)[0]
+    dec = oracle.Decoder(orc, synth.TREES[tree])
+    first = int(sess.prefill([p])[0])
+    if first != dec.prefill([int(x) for x in p]):
+        z = dec.o.causal_forward(dec.seq[: dec.n])[0][-1]
+        assert abs(z[first] - z[dec.pending]) <= 2 * tau(SMALL) * (z.max() - z.min())
+        dec.pending = dec.seq[-1] = first
+    ties = TieLog()
+    for i in range(4):
+        _, err = check_step(gpu_step(sess), 0, dec, tau(SMALL), ties)
+        log(f"small bf16, 4-bit KV, n {n}: step {i}: verify rel err {err:.2e}")
+    sess.close()
+
+
+def greedy(cfg, w, ps, n_new, **kw):
+    s = Session(cfg, w, (), max_batch=len(ps), max_len=2048, **kw)
+    out, _ = s.generate(ps, n_new)
+    s.close()
+    return out
+
+
+@pytest.mark.parametrize("cfg,tree,lens,page", [(synth.TINY, "T8", [32, 3], 16), (SMALL, "T64", [1100], 16),
+                                                (SMALL, "T32", [61, 250, 90], 7)])
+@pytest.mark.parametrize("wfmt", ["native", "fp4"])
+def test_speculative_steps_are_lossless(cfg, tree, lens, page, wfmt):
+    """The stream of speculative steps, replayed and eager, chain and branch
+    drafting, over shuffled pages, equals greedy decoding over the 4-bit cache."""
+    w = synth.make_weights(cfg, std=0.06)
+    ps = prompts(lens, cfg.vocab, 4)
+    want = greedy(cfg, w, ps, 40, weight_format=wfmt, kv_format="fp4")
+    for branch, graph in ((False, True), (True, False)):
+        n_pages = len(ps) * -(-(2048 + 64) // page)
+        order = np.random.default_rng(1).permutation(n_pages).astype(np.int32)
+        s = Session(cfg, w, synth.TREES[tree], max_batch=len(ps), max_len=2048, page_size=page, page_order=order,
+                    weight_format=wfmt, kv_format="fp4")
+        s.set_drafting(branch)
+        s.set_graph(graph)
+        got, _ = s.generate(ps, 40)
+        assert got == want, (branch, graph)
+        s.close()
+
+
+def test_cache_holds_rounded_rows_and_compacts_them():
+    """chimera_kv_read gives values of the format (rounding them again changes
+    nothing), the same after speculative steps as after greedy ones; and pipelined
+    steps equal single ones."""
+    w = synth.make_weights(SMALL, std=0.06)
+    ps = prompts([70, 33], SMALL.vocab, 9)
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        s = Session(SMALL, w, synth.TREES["T32"], max_batch=2, max_len=512, kv_format="fp4")
+        first, toks, lens, _ = run(s, ps, 6)
+        g = Session(SMALL, w, (), max_batch=2, max_len=512, kv_format="fp4")
+        total = [int(sum(l[b] for l in lens)) for b in range(2)]
+        g.prefill(ps)
+        for _ in range(max(total)):
+            g.step()
+        for b in range(2):
+            for layer in range(SMALL.n_layers):
+                k, v = s.kv_read(layer, b, 0, len(ps[b]) + total[b])
+                kg, vg = g.kv_read(layer, b, 0, len(ps[b]) + total[b])
+                assert np.array_equal(k, kg) and np.array_equal(v, vg)
+                for a in (k, v):
+                    t = torch.from_numpy(a.view(np.int16)).view(torch.bfloat16)
+                    assert torch.equal(R.held(t), t.double())
+        p = Session(SMALL, w, synth.TREES["T32"], max_batch=2, max_len=512, kv_format="fp4")
+        f2, t2, l2, _ = run(p, ps, 6, pipelined=True)
+        assert np.array_equal(first, f2) and all(np.array_equal(x, y) for x, y in zip(toks + lens, t2 + l2))
+        with pytest.raises(B.ChimeraError) as e:
+            s.compaction_check(True)
+        assert e.value.status == B.CHIMERA_EINVAL
+        for x in (s, g, p):
+            x.close()
+
+
+def test_formats_and_sizes():
+    with pytest.raises(ValueError):
+        Session(SMALL, None, (), kv_format="int8")
+    w = synth.make_weights(SMALL)
+    a = Session(SMALL, w, (), max_len=512)
+    with pytest.raises(ValueError):
+        Session(SMALL, None, (), max_len=512, share_model=a, weight_format="fp4")
+    b = Session(SMALL, None, (), max_len=512, share_model=a, kv_format="fp4")
+    assert b.kv_arena.numel() < a.kv_arena.numel() * 1.2
+    p = prompts([20], SMALL.vocab, 1)
+    assert len(b.generate(p, 5)[0][0]) == 5
+    b.close()
+    a.close()
