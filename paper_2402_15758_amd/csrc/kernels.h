@@ -122,7 +122,7 @@ void launch_tile_strided(int dtype, const void* x, int64_t ldx, int M, int K, vo
 constexpr int FP4_DIRECT_ROWS = 128;
 bool gemm_fp4_unpacks(int dtype, int M, int N);
 // s.W: the packed matrix, s.splits = fp4_splits(N, K), all columns.  ldx > 0: X
-// is row-major (at most 16 rows, 16-byte aligned rows).  unpacked: room for the
+// is row-major (at most 16 rows, 16-byte aligned).  unpacked: room for the
 // bf16 matrix where gemm_fp4_unpacks, else nullptr.
 void launch_gemm_fp4(int dtype, const GemmShape& s, const GemmEpi& e, int64_t ldx, void* unpacked, hipStream_t st,
                      hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
@@ -142,16 +142,16 @@ void launch_kv4_append(int dtype, const Kv4View& c, const void* k, const void* v
 void launch_kv4_read(int dtype, const Kv4View& c, void* k, void* v, int64_t ld, const int* seq, const int* pos,
                      int64_t rows, hipStream_t st);
 constexpr int KV4_MAX_DEPTH = 15;
-// By value in the kernels' arguments, so words that scalar loads bring whole:
-// arguments may lie in host memory, where a lane's own loads take microseconds.
+// By value in the kernels' arguments, as words that scalar loads bring whole
+// (arguments may lie in host memory, where a lane's own loads take microseconds)
+// and few of them (a launch's arguments are held until it has run).
 struct Kv4Tree {
-  uint32_t depth[8];                           // four bits a node
-  uint32_t path[64][(KV4_MAX_DEPTH + 1) / 4];  // a byte a depth: node at that depth on the root->u path
-  void set(int u, int parent) {  // nodes in order, parents first
-    const int d = u == 0 ? 0 : depth_of(parent) + 1;
+  uint32_t depth[8];    // four bits a node
+  uint32_t parent[16];  // a byte a node
+  void set(int u, int p) {  // nodes in order, parents first; the root's parent counts as itself
+    const int d = u == 0 ? 0 : depth_of(p) + 1;
     depth[u / 8] |= (uint32_t)d << (4 * (u % 8));
-    for (int i = 0; i < 4; ++i) path[u][i] = u == 0 ? 0 : path[parent][i];
-    path[u][d / 4] |= (uint32_t)u << (8 * (d % 4));
+    parent[u / 4] |= (uint32_t)(u == 0 ? 0 : p) << (8 * (u % 4));
   }
   int depth_of(int u) const { return (int)(depth[u / 8] >> (4 * (u % 8))) & 15; }
 };

@@ -15,6 +15,7 @@
 #include <hip/hip_ext.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "fp4.h"
@@ -123,37 +124,29 @@ __global__ __launch_bounds__(256) void fp4_unpack_kernel(const uint8_t* __restri
   }
 }
 
-// X rows of a launch: tiled (fragment order, x_mtiles 16-row tiles) or row-major
-// with a row stride (up to 16 rows: M == 1 reads 64 bytes a k-block).
+// X rows of a launch: tiled (fragment order, x_mtiles 16-row tiles), or one block
+// of up to 16 rows where they lie (RM, row stride ldx).
 template <typename T, bool RM>
 struct XRows {
   const T* base;
-  int64_t step;   // elements from one 32-wide k-block to the next
-  int64_t tile;   // from one 16-row tile to the next
-  int64_t half;   // fp32: from the first four indices of a lane to the next four
+  int64_t step;  // elements from one 32-wide k-block to the next
   __device__ __forceinline__ XRows(const GemmShape& sh, int64_t ldx, int mb0, int lane) {
     const int g = lane >> 4, r = lane & 15;
     if constexpr (RM) {  // rows past M repeat the last one; they are not stored
       base = (const T*)sh.X + (int64_t)min(r, sh.M - 1) * ldx + 8 * g;
       step = 32;
-      tile = 0;
-      half = 4;
-    } else if constexpr (sizeof(T) == 2) {
-      base = (const T*)sh.X + ((int64_t)mb0 * 64 + lane) * 8;
+    } else {
       step = (int64_t)sh.x_mtiles * 64 * 8;
-      tile = 64 * 8;
-      half = 0;
-    } else {  // two fp32 k-blocks of 16: lanes of pieces 2 (g & 1) and 2 (g & 1) + 1 of block g >> 1
-      base = (const T*)sh.X + (((int64_t)(g >> 1) * sh.x_mtiles + mb0) * 64 + 32 * (g & 1) + r) * 4;
-      step = (int64_t)sh.x_mtiles * 64 * 8;
-      tile = 64 * 4;
-      half = 16 * 4;
+      if constexpr (sizeof(T) == 2)
+        base = (const T*)sh.X + ((int64_t)mb0 * 64 + lane) * 8;
+      else  // two k-blocks of 16: lanes of pieces 2 (g & 1) and 2 (g & 1) + 1 of block g >> 1
+        base = (const T*)sh.X + (((int64_t)(g >> 1) * sh.x_mtiles + mb0) * 64 + 32 * (g & 1) + r) * 4;
     }
   }
   __device__ __forceinline__ void load(int kb, int i, Frag32<T>& f) const {
-    const T* p = base + (int64_t)kb * step + i * tile;
+    const T* p = base + (int64_t)kb * step + i * 64 * (16 / sizeof(T));
     f.v[0] = ld16(p);
-    if constexpr (sizeof(T) == 4) f.v[1] = ld16(p + half);
+    if constexpr (sizeof(T) == 4) f.v[1] = ld16(p + (RM ? 4 : 16 * 4));
   }
 };
 
@@ -166,11 +159,46 @@ __device__ __forceinline__ uint32_t word(const int4& v, int i) {
   return (uint32_t)(i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)));
 }
 
+// A 16x16 output tile: rows of tile mb, column block blk; rm: its rows' targets.
+template <typename T>
+__device__ __forceinline__ void store_output(const GemmShape& sh, const GemmEpi& e, int kind, int mb, int blk,
+                                             int slice, f32x4 v, float* tw, const RowMeta* rm, int lane) {
+  if (kind == EPI_F32) {
+    store_tile<T, EPI_F32>(sh, e, mb, blk, v, nullptr, tw, nullptr, f32x4{}, f32x4{}, lane);
+  } else if (kind == EPI_PARTIAL) {
+    float* part = e.part + (int64_t)slice * sh.M * sh.N;
+    store_tile<T, EPI_PARTIAL>(sh, e, mb, blk, v, part, tw, nullptr, f32x4{}, f32x4{}, lane);
+  } else if (kind == EPI_SWIGLU) {
+    store_tile<T, EPI_SWIGLU>(sh, e, mb, blk, v, nullptr, tw, nullptr, f32x4{}, f32x4{}, lane);
+  } else if (kind == EPI_QKV) {
+    f32x4 cs = f32x4{1.f, 1.f, 1.f, 1.f}, sn = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (blk < 2 * e.H * (e.hd / 16)) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int lr = 4 * (lane >> 4) + r;
+        if (16 * mb + lr < sh.M) {
+          const int64_t ti = (int64_t)rm[lr].pos * (e.hd / 2) + 8 * (blk % (e.hd / 16)) + (lane & 7);
+          cs[r] = e.rcos[ti];
+          sn[r] = e.rsin[ti];
+        }
+      }
+    }
+    store_tile<T, EPI_QKV>(sh, e, mb, blk, v, nullptr, tw, rm, cs, sn, lane);
+  }
+}
+// The QKV epilogue's targets of `rows` rows from `first`, into LDS.
+__device__ __forceinline__ void row_targets(const GemmShape& sh, const GemmEpi& e, int first, int rows, RowMeta* rm) {
+  if ((int)threadIdx.x >= rows) return;
+  const int row = first + threadIdx.x;
+  RowMeta t{-1, 0, -1};
+  if (row < sh.M) t = RowMeta{e.kvoff[row], e.pos[row], e.qrow[row]};
+  rm[threadIdx.x] = t;
+}
+
 // One workgroup's run of CB column blocks from cb0, rows 16 mb0 .. 16 (mb0 +
 // MB) - 1 of one slice; the four waves take one class each.
 template <typename T, int MB, int CB, bool RM>
-__device__ __forceinline__ void fp4_run(const GemmShape& sh, const GemmEpi& e, int64_t ldx, const Fp4Shape& w4,
-                                        int kind, int cb0, int mb0, int slice, f32x4* red, const RowMeta* rm,
+__device__ __forceinline__ void fp4_run(const GemmShape& sh, const GemmEpi& e, int64_t ldx, const Fp4Shape& w4, int kind, int cb0, int mb0, int slice, f32x4* red, const RowMeta* rm,
                                         float* stage) {
   constexpr int XP = MB >= 4 ? 2 : 4;  // k-blocks of X in flight
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -276,29 +304,7 @@ __device__ __forceinline__ void fp4_run(const GemmShape& sh, const GemmEpi& e, i
       f32x4 v = red[((0 * MB + i) * JR + jj) * 64 + lane];
 #pragma unroll
       for (int w = 1; w < 4; ++w) v = v + red[((w * MB + i) * JR + jj) * 64 + lane];
-      float* tw = stage + wave * 256;
-      float* part = e.part + (int64_t)slice * sh.M * sh.N;
-      if (kind == EPI_F32) {
-        store_tile<T, EPI_F32>(sh, e, mb0 + i, blk, v, nullptr, tw, nullptr, f32x4{}, f32x4{}, lane);
-      } else if (kind == EPI_PARTIAL) {
-        store_tile<T, EPI_PARTIAL>(sh, e, mb0 + i, blk, v, part, tw, nullptr, f32x4{}, f32x4{}, lane);
-      } else if (kind == EPI_SWIGLU) {
-        store_tile<T, EPI_SWIGLU>(sh, e, mb0 + i, blk, v, nullptr, tw, nullptr, f32x4{}, f32x4{}, lane);
-      } else if (kind == EPI_QKV) {
-        f32x4 cs = f32x4{1.f, 1.f, 1.f, 1.f}, sn = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (blk < 2 * e.H * (e.hd / 16)) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int lr = 16 * i + 4 * (lane >> 4) + r;
-            if (16 * mb0 + lr < sh.M) {
-              const int64_t ti = (int64_t)rm[lr].pos * (e.hd / 2) + 8 * (blk % (e.hd / 16)) + (lane & 7);
-              cs[r] = e.rcos[ti];
-              sn[r] = e.rsin[ti];
-            }
-          }
-        }
-        store_tile<T, EPI_QKV>(sh, e, mb0 + i, blk, v, nullptr, tw, rm + 16 * i, cs, sn, lane);
-      }
+      store_output<T>(sh, e, kind, mb0 + i, blk, slice, v, stage + wave * 256, rm + 16 * i, lane);
     }
   }
 }
@@ -313,12 +319,7 @@ __global__ __launch_bounds__(256) void gemm_fp4_kernel(const GemmShape sh, const
   __shared__ RowMeta rm[16 * MB];
   __shared__ __attribute__((aligned(16))) float stage[4 * 256];
   const int mb0 = blockIdx.x * MB, b = blockIdx.y, slice = blockIdx.z;
-  if (kind == EPI_QKV && threadIdx.x < 16 * MB) {  // visible after the barrier that follows the k-loop
-    const int row = 16 * mb0 + threadIdx.x;
-    RowMeta t{-1, 0, -1};
-    if (row < sh.M) t = RowMeta{e.kvoff[row], e.pos[row], e.qrow[row]};
-    rm[threadIdx.x] = t;
-  }
+  if (kind == EPI_QKV) row_targets(sh, e, 16 * mb0, 16 * MB, rm);  // visible after the barrier behind the k-loop
   if (b < nbig) {
     fp4_run<T, MB, CBA, RM>(sh, e, ldx, w4, kind, b * CBA, mb0, slice, red, rm, stage);
   } else {
@@ -328,50 +329,188 @@ __global__ __launch_bounds__(256) void gemm_fp4_kernel(const GemmShape sh, const
   }
 }
 
+constexpr int FP4_ROWS_BYTES = 112 << 10;
+
+// Split products of up to 16 rows whose sum nobody else finishes: a workgroup
+// owns one column block and the whole reduction, S slices of four waves (one a
+// class) side by side, and the slices meet in LDS, not in a finishing launch.
+// Its share is short (35 KB of 4096 x 16), a quarter of the bf16 kernels'.  The
+// rows are staged in LDS, only the ones there are; a thread's first pieces are
+// requested before its weights, since loads return in order and the weights
+// need not be waited for there.
+template <typename T, int S, bool RM>
+__global__ __launch_bounds__(256 * S) void gemm_fp4_whole_kernel(const GemmShape sh, const GemmEpi e, int64_t ldx,
+                                                                 const Fp4Shape w4) {
+  constexpr int PF = 4, XU = 2;           // quads in flight; pieces of x a thread requests first
+  constexpr int J = sizeof(T) / 2;        // 16-byte pieces of eight values
+  extern __shared__ int4 xs[];
+  __shared__ f32x4 red[GEMM_MAX_SPLITS * 4 * 64];
+  __shared__ __attribute__((aligned(16))) float stage[256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), cls = wave & 3;
+  const int g = lane >> 4, r = min(lane & 15, sh.M - 1);  // rows past M repeat the last one; they are not stored
+  const int nk = cls < w4.kps ? (w4.kps - cls + 3) / 4 : 0, nq = (nk + 3) / 4;
+  // piece (kb, g, half) of row q goes to ((4 kb + g) J + half) M + q
+  const int total = sh.K / ET<T>::VEC * sh.M;
+  auto piece = [&](int i) {
+    const int q = i % sh.M, k = i / sh.M * ET<T>::VEC;
+    return RM ? ld16((const T*)sh.X + (int64_t)q * ldx + k) : ld16((const T*)sh.X + tiled_index<T>(sh.x_mtiles, q, k));
+  };
+  int4 xr[XU];
+#pragma unroll
+  for (int t = 0; t < XU; ++t)
+    if (tid + t * 256 * S < total) xr[t] = piece(tid + t * 256 * S);
+  int4 bc[PF];
+  uint32_t bs[PF];
+  const uint8_t* codes = nullptr;
+  const uint8_t* scales = nullptr;
+  auto load_w = [&](int slot, int q) {
+    bc[slot] = ld16_nt(codes + (int64_t)q * 1024);
+    bs[slot] = *reinterpret_cast<const uint32_t*>(scales + (int64_t)q * 64);
+  };
+  auto start = [&](int slice) {
+    const int64_t u = fp4_unit(w4, blockIdx.x, slice, cls);
+    codes = (const uint8_t*)sh.W + u * 1024 + lane * 16;
+    scales = (const uint8_t*)sh.W + w4.codes_bytes + u * 64 + (lane & 15) * 4;
+#pragma unroll
+    for (int t = 0; t < PF; ++t)
+      if (t < nq) load_w(t, t);
+  };
+  start(wave / 4);
+#pragma unroll
+  for (int t = 0; t < XU; ++t)
+    if (tid + t * 256 * S < total) xs[tid + t * 256 * S] = xr[t];
+  for (int i = tid + XU * 256 * S; i < total; i += 256 * S) xs[i] = piece(i);
+  __syncthreads();
+  for (int sl = wave / 4; sl < w4.splits; sl += S) {
+    if (sl >= S) start(sl);
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int4* x = xs + ((int64_t)(sl * w4.kps + cls) * 4 + g) * J * sh.M + r;
+    const int step = 16 * J * sh.M;  // four k-blocks on
+    for (int q0 = 0; q0 < nq; q0 += PF) {
+#pragma unroll
+      for (int t = 0; t < PF; ++t) {
+        if (q0 + t >= nq) break;  // wave-uniform
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = 4 * (q0 + t) + i;
+          if (k >= nk) break;
+          Frag32<T> xf, w;
+#pragma unroll
+          for (int h = 0; h < J; ++h) xf.v[h] = x[k * step + h * sh.M];
+          w.from_fp4(word(bc[t], i), fp4_scale((bs[t] >> (8 * i)) & 255));
+          acc = mfma32<T>(xf, w, acc);
+        }
+        if (q0 + t + PF < nq) load_w(t, q0 + t + PF);
+      }
+    }
+    red[(sl * 4 + cls) * 64 + lane] = acc;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  f32x4 v;
+  for (int sl = 0; sl < w4.splits; ++sl) {  // classes in class order, slices in slice order
+    f32x4 t = red[(sl * 4) * 64 + lane];
+#pragma unroll
+    for (int c = 1; c < 4; ++c) t = t + red[(sl * 4 + c) * 64 + lane];
+    v = sl == 0 ? t : v + t;
+  }
+  store_tile<T, EPI_F32>(sh, e, 0, blockIdx.x, v, nullptr, stage, nullptr, f32x4{}, f32x4{}, lane);
+}
+
+// FP4_WHOLE: the kernel above, where the rows fit LDS.  FP4_ROWS: blocks of rows
+// read where they lie (one block).  FP4_BLOCKS: from tiles.
+enum Fp4Route { FP4_BLOCKS, FP4_ROWS, FP4_WHOLE };
+Fp4Route fp4_route(int dtype, int M, int N, int K, int splits, int kind, int64_t ldx) {
+  // A workgroup's weights, 8.5 K bytes, come through one CU, and column blocks
+  // past one a CU wait for a second round.  One row, us, against the slices in
+  // workgroups of their own and a finishing launch (both kernels, without the gap
+  // between): 4096 x 4096 5.6 / 7.5, 11008 x 4096 9.2 / 11.6, 4096 x 1024 5.3 /
+  // 5.8, 13824 x 5120 13.8 / 14.7; 13824 x 256 7.4 / 5.8 (the launch saved is worth
+  // 2.5 us of the host's time), 13824 x 8176, four rows, 27.8 / 20.9.
+  const int64_t bytes = (int64_t)M * K * (dtype == DT_BF16 ? 2 : 4);
+  if (M <= 16 && splits > 1 && kind == EPI_F32 && bytes <= FP4_ROWS_BYTES && K <= 14336 && N / 16 <= 384)
+    return FP4_WHOLE;
+  return ldx > 0 ? FP4_ROWS : FP4_BLOCKS;
+}
+
 constexpr int FP4_CB_MAX = 8;
 constexpr int FP4_WGS = 256;
 
-template <typename T, int MB, int CBA, bool RM>
-void fp4_launch(const GemmShape& s, const GemmEpi& e, int64_t ldx, const Fp4Shape& w4, int kind, int runs, int nbig,
-                hipStream_t st, hipEvent_t ea, hipEvent_t eb) {
-  const dim3 grid((s.M + 16 * MB - 1) / (16 * MB), runs, s.splits);
-  if (ea || eb)
-    hipExtLaunchKernelGGL((gemm_fp4_kernel<T, MB, CBA, RM>), grid, dim3(256), 0, st, ea, eb, 0, s, e, ldx, w4, kind,
-                          nbig);
-  else
-    hipLaunchKernelGGL((gemm_fp4_kernel<T, MB, CBA, RM>), grid, dim3(256), 0, st, s, e, ldx, w4, kind, nbig);
+// Column runs of a slice: GEMM_WGS workgroups' worth, at most FP4_CB_MAX blocks
+// long; the first `big` runs have `run` blocks, the others one less.
+struct Fp4Runs {
+  int runs, run, big;
+};
+Fp4Runs fp4_runs(int nbc, int splits) {
+  Fp4Runs r;
+  r.runs = std::min(std::max((FP4_WGS + splits - 1) / splits, (nbc + FP4_CB_MAX - 1) / FP4_CB_MAX), nbc);
+  r.run = (nbc + r.runs - 1) / r.runs;
+  r.big = nbc - r.runs * (r.run - 1);
+  return r;
 }
 
-template <typename T, int MB, bool RM>
-void fp4_mb(const GemmShape& s, const GemmEpi& e, int64_t ldx, const Fp4Shape& w4, int kind, hipStream_t st,
-            hipEvent_t ea, hipEvent_t eb) {
-  const int nbc = s.N / 16;
-  const int runs = std::min(std::max((FP4_WGS + s.splits - 1) / s.splits, (nbc + FP4_CB_MAX - 1) / FP4_CB_MAX), nbc);
-  const int run = (nbc + runs - 1) / runs, nbig = nbc - runs * (run - 1);
-  switch (run) {
-    case 1: fp4_launch<T, MB, 1, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
-    case 2: fp4_launch<T, MB, 2, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
-    case 3: fp4_launch<T, MB, 3, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
-    case 4: fp4_launch<T, MB, 4, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
-    case 5: fp4_launch<T, MB, 5, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
-    case 6: fp4_launch<T, MB, 6, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
-    case 7: fp4_launch<T, MB, 7, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
-    default: fp4_launch<T, MB, 8, RM>(s, e, ldx, w4, kind, runs, nbig, st, ea, eb); break;
+struct Fp4Launch {
+  const GemmShape& s;
+  const GemmEpi& e;
+  int64_t ldx;
+  Fp4Shape w4;
+  int kind;
+  hipStream_t st;
+  hipEvent_t ea, eb;
+
+  template <typename... A, typename K>
+  void go(K kernel, dim3 grid, int threads, size_t lds, A... args) const {
+    if (ea || eb)
+      hipExtLaunchKernelGGL(kernel, grid, dim3(threads), lds, st, ea, eb, 0, args...);
+    else
+      hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, st, args...);
   }
-}
-
-template <typename T>
-void fp4_t(const GemmShape& s, const GemmEpi& e, int64_t ldx, const Fp4Shape& w4, int kind, hipStream_t st,
-           hipEvent_t ea, hipEvent_t eb) {
-  if (s.M <= 16 && ldx > 0)
-    fp4_mb<T, 1, true>(s, e, ldx, w4, kind, st, ea, eb);
-  else if (s.M <= 16)
-    fp4_mb<T, 1, false>(s, e, 0, w4, kind, st, ea, eb);
-  else if (s.M <= 32)
-    fp4_mb<T, 2, false>(s, e, 0, w4, kind, st, ea, eb);
-  else
-    fp4_mb<T, 4, false>(s, e, 0, w4, kind, st, ea, eb);
-}
+  // f(column blocks of a long run)
+  template <class F>
+  static void by_run(int run, F&& f) {
+    switch (run) {
+      case 1: f(std::integral_constant<int, 1>{}); break;
+      case 2: f(std::integral_constant<int, 2>{}); break;
+      case 3: f(std::integral_constant<int, 3>{}); break;
+      case 4: f(std::integral_constant<int, 4>{}); break;
+      case 5: f(std::integral_constant<int, 5>{}); break;
+      case 6: f(std::integral_constant<int, 6>{}); break;
+      case 7: f(std::integral_constant<int, 7>{}); break;
+      default: f(std::integral_constant<int, 8>{}); break;
+    }
+  }
+  template <typename T, int MB, bool RM>
+  void blocks() const {
+    const Fp4Runs r = fp4_runs(s.N / 16, s.splits);
+    const dim3 grid((s.M + 16 * MB - 1) / (16 * MB), r.runs, s.splits);
+    by_run(r.run, [&](auto cb) {
+      go(gemm_fp4_kernel<T, MB, decltype(cb)::value, RM>, grid, 256, 0, s, e, ldx, w4, kind, r.big);
+    });
+  }
+  template <typename T, bool RM>
+  void whole() const {
+    const dim3 grid(s.N / 16);
+    const size_t lds = (size_t)s.M * s.K * sizeof(T);
+    // sixteen waves a column block, eight where two workgroups a CU are wanted
+    if (s.splits >= 4 && s.N / 16 <= FP4_WGS)
+      go(gemm_fp4_whole_kernel<T, 4, RM>, grid, 1024, lds, s, e, ldx, w4);
+    else
+      go(gemm_fp4_whole_kernel<T, 2, RM>, grid, 512, lds, s, e, ldx, w4);
+  }
+  template <typename T>
+  void run(Fp4Route route) const {
+    if (route == FP4_WHOLE)
+      ldx > 0 ? whole<T, true>() : whole<T, false>();
+    else if (route == FP4_ROWS)
+      blocks<T, 1, true>();
+    else if (s.M <= 16)
+      blocks<T, 1, false>();
+    else if (s.M <= 32)
+      blocks<T, 2, false>();
+    else
+      blocks<T, 4, false>();
+  }
+};
 
 // Row-major x with a row stride into tiles, 16 bytes a thread; rows that do not
 // start at 16 bytes are read element by element.
@@ -449,12 +588,13 @@ void launch_gemm_fp4(int dtype, const GemmShape& s, const GemmEpi& e, int64_t ld
     (void)launch_gemm(dtype, u, e, st, ev_start, ev_stop);
     return;
   }
-  const bool finish = s.splits > 1 && e.kind != EPI_PARTIAL;
-  const int kind = finish ? EPI_PARTIAL : e.kind;
+  const Fp4Route route = fp4_route(dtype, s.M, s.N, s.K, s.splits, e.kind, ldx);
+  const bool finish = s.splits > 1 && e.kind != EPI_PARTIAL && route != FP4_WHOLE;
+  const Fp4Launch l{s, e, ldx, w4, finish ? (int)EPI_PARTIAL : e.kind, st, ev_start, finish ? nullptr : ev_stop};
   if (dtype == DT_BF16)
-    fp4_t<bf16_t>(s, e, ldx, w4, kind, st, ev_start, finish ? nullptr : ev_stop);
+    l.run<bf16_t>(route);
   else
-    fp4_t<float>(s, e, ldx, w4, kind, st, ev_start, finish ? nullptr : ev_stop);
+    l.run<float>(route);
   if (finish) launch_gemm_finish(dtype, s, e, st, ev_stop);
 }
 

@@ -116,18 +116,26 @@ constexpr int GROUP = FAN * CHUNK, SUPER = FAN * GROUP;  // positions
 constexpr int SUPER_WGS = 256;
 static_assert(WIN == KV4_MAX_DEPTH + 1, "the window holds every position of a tree");
 
-// Depth of a lane's node, and a lane's entry of one node's path.
+// Depth of a lane's node.
 __device__ __forceinline__ int node_depth(const Kv4Tree& t, int u) {
   uint32_t w = t.depth[0];
 #pragma unroll
   for (int i = 1; i < 8; ++i) w = u / 8 == i ? t.depth[i] : w;
   return (int)(w >> (4 * (u & 7))) & 15;
 }
-__device__ __forceinline__ int path_node(const uint32_t (&path)[4], int depth) {
-  uint32_t w = path[0];
+// u's ancestor-or-self at a lane's depth e (0 .. deep, u's own; others give 0):
+// every lane holds the parent of the node of its number, the walk from u is uniform.
+__device__ __forceinline__ int ancestor(const Kv4Tree& t, int u, int deep, int e, int lane) {
+  uint32_t w = t.parent[0];
 #pragma unroll
-  for (int i = 1; i < 4; ++i) w = depth / 4 == i ? path[i] : w;
-  return (int)(w >> (8 * (depth & 3))) & 255;
+  for (int i = 1; i < 16; ++i) w = lane / 4 == i ? t.parent[i] : w;
+  const int parent = (int)(w >> (8 * (lane & 3))) & 63;
+  int node = u, mine = 0;
+  for (int d = deep; d >= 0; --d) {
+    mine = e == d ? node : mine;
+    node = __builtin_amdgcn_readlane(parent, node);
+  }
+  return mine;
 }
 
 __device__ __forceinline__ float exp2_from(float a, float b) {  // 2^(a - b), 0 from nothing
@@ -507,8 +515,9 @@ __device__ __forceinline__ float pair_reduce(float x, float y, int lane) {
 // output; the shares of the 16 keys are then added over the lanes, halving the
 // dimensions a lane holds with each of the four steps: the lane ends with
 // dimensions HD/4 j + (HD/64) rev .., rev the bits 5, 4, 3, 2 of the lane.  The
-// partials are folded, for those dimensions, while the rows are in flight.
-template <typename T, int HD>
+// partials are folded, for those dimensions, while the rows are in flight, BATCH
+// a round trip, the first requested as soon as n is known.
+template <typename T, int HD, int BATCH>
 __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
   constexpr int DPL = HD / 64, DQ = HD / 4;
   const Kv4View& c = a.c;
@@ -520,64 +529,71 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
   const int kw = lane >> 2, sub = lane & 3;
   const int dim = DQ * sub + DPL * (8 * (lane >> 5) + 4 * ((lane >> 4) & 1) + 2 * ((lane >> 3) & 1) + ((lane >> 2) & 1));
   const int n = min(a.n_b[b], c.max_pages * c.ps);
-  const int P = n + ((a.tree.depth[u / 8] >> (4 * (u & 7))) & 15);
+  const int deep = (int)(a.tree.depth[u / 8] >> (4 * (u & 7))) & 15, P = n + deep;
   // this lane's window key
   const int p = P - WIN + 1 + kw;
-  const int at = p < n ? p : n + path_node(a.tree.path[u], min(max(p - n, 0), KV4_MAX_DEPTH));
-  const int64_t e = n >= 0 && p >= 0 ? kv4_slot(c, b, at) : (int64_t)-1;
-  const bool valid = e >= 0;
-  Frag32<T> qf[HD / 32];
-  load_query<T, HD>((const T*)a.q + row * a.ldq + hq * HD, sub, a.scale < 0.f, qf);
+  const int anc = ancestor(a.tree, u, deep, p - n, lane);
+  const int at = p < n ? p : n + anc;
+  const bool in = n >= 0 && p >= 0 && at < c.max_pages * c.ps;
+  const int page = in ? c.page_table[(int64_t)b * c.max_pages + (unsigned)at / (unsigned)c.ps] : -1;
   const int maxk = n < 0 ? -1 : n + a.deepest - WIN;
   const bool supers = maxk >= 0 && kv4_supers(maxk, a.blocks);
   const int lim = n < 0 ? -1 : P - WIN;  // last shared position of this query
   const int nu = lim < 0 ? 0 : lim / (supers ? SUPER : GROUP) + 1;
   const int64_t base = part_slot(a, b, h, 0, nq) + qi;
-  const uint32_t r = valid ? (uint32_t)(e / 32 + h * (c.ps * HD / 32)) : 0;
+  float2 bml[BATCH];
+  float bo[BATCH][DPL];
+  auto load_batch = [&](int g0) {  // past the last unit: the last again
+#pragma unroll
+    for (int t = 0; t < BATCH; ++t) {
+      const int64_t i = base + (int64_t)min(g0 + t, nu - 1) * nq;
+      bml[t] = *reinterpret_cast<const float2*>(a.part_ml + i * 2);
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) bo[t][d] = a.part_o[i * HD + dim + d];
+    }
+  };
+  if (nu > 0) load_batch(0);
+  Frag32<T> qf[HD / 32];
+  load_query<T, HD>((const T*)a.q + row * a.ldq + hq * HD, sub, a.scale < 0.f, qf);
+  const bool valid = (unsigned)page < (unsigned)c.n_pages;
+  const uint32_t r = valid ? (uint32_t)((int64_t)page * (c.page_stride / 32)) +
+                                 (h * c.ps + (unsigned)at % (unsigned)c.ps) * (HD / 32)
+                           : 0;
   Quarter<HD> k, v;
   k.load(c.codes, c.scales, r, sub);
   v.load(c.codes + (int64_t)c.H * c.ps * HD / 2, c.scales + (int64_t)c.H * c.ps * HD / 32, r, sub);
   float m = -CH_INF, l = 0.f, o[DPL], gm = -CH_INF, gl = 0.f, go[DPL];
 #pragma unroll
   for (int d = 0; d < DPL; ++d) o[d] = go[d] = 0.f;
-  // BATCH partials a round trip, folded in order
-  auto fold_units = [&](auto batch) {
-    constexpr int BATCH = decltype(batch)::value;
-    for (int g0 = 0; g0 < nu; g0 += BATCH) {
-      float2 bml[BATCH];
-      float bo[BATCH][DPL];
+  for (int g0 = 0; g0 < nu; g0 += BATCH) {
+    if (g0 > 0) load_batch(g0);
 #pragma unroll
-      for (int t = 0; t < BATCH; ++t) {
-        const int64_t at = base + (int64_t)min(g0 + t, nu - 1) * nq;
-        bml[t] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+    for (int t = 0; t < BATCH; ++t) {
+      if (g0 + t >= nu) break;
+      float x, y;
+      if (supers) {
+        if (fold(m, l, bml[t].x, bml[t].y, x, y)) {
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) bo[t][d] = a.part_o[at * HD + dim + d];
+          for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, bo[t][d], y);
+        }
+        continue;
       }
+      if (fold(gm, gl, bml[t].x, bml[t].y, x, y)) {  // groups make a super
 #pragma unroll
-      for (int t = 0; t < BATCH; ++t) {
-        if (g0 + t >= nu) break;
-        float x, y;
-        if (fold(gm, gl, bml[t].x, bml[t].y, x, y)) {  // groups make a super; a super is itself
+        for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, bo[t][d], y);
+      }
+      if (t % FAN == FAN - 1 || g0 + t == nu - 1) {
+        if (fold(m, l, gm, gl, x, y)) {
 #pragma unroll
-          for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, bo[t][d], y);
+          for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
         }
-        if (supers || t % FAN == FAN - 1 || g0 + t == nu - 1) {
-          if (fold(m, l, gm, gl, x, y)) {
+        gm = -CH_INF;
+        gl = 0.f;
 #pragma unroll
-            for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
-          }
-          gm = -CH_INF;
-          gl = 0.f;
-#pragma unroll
-          for (int d = 0; d < DPL; ++d) go[d] = 0.f;
-        }
+        for (int d = 0; d < DPL; ++d) go[d] = 0.f;
       }
     }
-  };
-  if (nu <= 4)  // uniform
-    fold_units(std::integral_constant<int, 4>{});
-  else
-    fold_units(std::integral_constant<int, 16>{});
+  }
   float acc = 0.f;
   float sc = fp4_scale(k.s);
 #pragma unroll
@@ -631,7 +647,13 @@ void kv4_attn_go(const Kv4AttnArgs& a, hipStream_t st) {
   // cost their start, 5 to 8 ns each, where a long table holds short sequences.
   const int y = std::min(a.units, std::max(1, 2048 / (x * a.c.B)));
   hipLaunchKernelGGL((kv4_shared<T, HD>), dim3(x, y, a.c.B), dim3(256), 0, st, a);
-  hipLaunchKernelGGL((kv4_window<T, HD>), dim3((a.Hq + 3) / 4, a.N, a.c.B), dim3(256), 0, st, a);
+  const dim3 grid((a.Hq + 3) / 4, a.N, a.c.B);
+  if (a.units <= 4)
+    hipLaunchKernelGGL((kv4_window<T, HD, 4>), grid, dim3(256), 0, st, a);
+  else if (a.units <= 8)
+    hipLaunchKernelGGL((kv4_window<T, HD, 8>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv4_window<T, HD, 32>), grid, dim3(256), 0, st, a);
 }
 
 }  // namespace

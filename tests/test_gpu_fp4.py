@@ -92,7 +92,10 @@ def check_product(x, w, y):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M,N,K", [(1, 16, 32), (1, 1024, 256), (1, 4096, 4096), (2, 48, 96), (5, 80, 544),
                                    (16, 512, 1088), (17, 64, 64), (33, 208, 2080), (64, 768, 256), (65, 4096, 512),
-                                   (129, 320, 1024), (300, 1040, 288), (130, 8256, 160)])
+                                   (129, 320, 1024), (300, 1040, 288), (130, 8256, 160),
+                                   # up to 16 rows: whole rows in LDS or a slice of them, one workgroup a column
+                                   # block or not, and rows too long for it
+                                   (1, 64, 8192), (7, 80, 2048), (16, 320, 4096), (13, 8256, 2048), (16, 8256, 4128)])
 def test_product(dtype, M, N, K):
     g = torch.Generator().manual_seed(M * 7 + N + K)
     x = (torch.randn(M, K, generator=g) * torch.exp(torch.randn(K, generator=g))).to(R.TYPES[dtype])
