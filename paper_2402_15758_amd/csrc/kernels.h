@@ -118,11 +118,14 @@ void launch_fp4_unpack_rows(int dtype, const void* packed, int N, int K, void* d
 // Row-major x [M][ldx] -> tiled.
 void launch_tile_strided(int dtype, const void* x, int64_t ldx, int M, int K, void* dst, int mtiles, hipStream_t st);
 // Whether launches of M rows run on the bf16 kernels over the unpacked matrix:
-// bf16, whole 64-column groups, more than FP4_DIRECT_ROWS rows.
-constexpr int FP4_DIRECT_ROWS = 128;
+// bf16, whole 64-column groups, more than FP4_DIRECT_ROWS rows.  Up to there the
+// weights are converted once a 64-row block, past it once, to memory (us, blocks /
+// unpacked; 4096 x 12288: 256 rows 37 / 55, 384 rows 55 / 73, 512 rows 73 / 75;
+// 4096 x 4096, 512 rows: 31 / 32).
+constexpr int FP4_DIRECT_ROWS = 512;
 bool gemm_fp4_unpacks(int dtype, int M, int N);
 // s.W: the packed matrix, s.splits = fp4_splits(N, K), all columns.  ldx > 0: X
-// is row-major (at most 16 rows, 16-byte aligned).  unpacked: room for the
+// is row-major (at most 32 rows, 16-byte aligned).  unpacked: room for the
 // bf16 matrix where gemm_fp4_unpacks, else nullptr.
 void launch_gemm_fp4(int dtype, const GemmShape& s, const GemmEpi& e, int64_t ldx, void* unpacked, hipStream_t st,
                      hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
