@@ -362,7 +362,8 @@ chimera_status chimera_gemm_static(int32_t dtype, const void* x, const void* w, 
  * captured into a HIP graph.  A workspace is scratch of one call: calls that
  * may run at the same time (other streams, other graphs) need their own. */
 
-/* A K x N matrix packed for chimera_gemm_fp4: N a multiple of 16, K of 32.
+/* A K x N matrix packed for chimera_gemm_fp4: N a multiple of 16, K of 32, both
+ * at most 2^20.
  * w is row-major [K][ldw] of `dtype`, ldw >= N, at any element; `packed` is
  * 16-byte aligned, chimera_fp4_bytes long, its layout the library's own.
  * chimera_fp4_unpack writes the values that `packed` stands for, rounded to

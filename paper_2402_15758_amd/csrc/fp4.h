@@ -90,3 +90,21 @@ __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = p[e];
 }
+
+// The caller's rows may start at any element: loads and stores of eight values
+// take 4-byte (fp32) or 2-byte (bf16) alignment.
+template <typename T>
+__device__ __forceinline__ void store8(T* p, uint32_t w, float scale);
+template <>
+__device__ __forceinline__ void store8<bf16_t>(bf16_t* p, uint32_t w, float scale) {
+  typedef int i4_any __attribute__((ext_vector_type(4), aligned(2)));
+  const int4 v = fp4_to_bf16x8(w, scale);
+  *reinterpret_cast<i4_any*>(p) = i4_any{v.x, v.y, v.z, v.w};
+}
+template <>
+__device__ __forceinline__ void store8<float>(float* p, uint32_t w, float scale) {
+  typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+  const f32x4 a = fp4_to_f32x4<0>(w, scale), b = fp4_to_f32x4<1>(w, scale);
+  *reinterpret_cast<f4_any*>(p) = f4_any{a[0], a[1], a[2], a[3]};
+  *reinterpret_cast<f4_any*>(p + 4) = f4_any{b[0], b[1], b[2], b[3]};
+}

@@ -141,9 +141,9 @@ struct Kv4View {
 // Rows r of K and V (k + r ld, v + r ld: [H][hd]) at position pos[r] of sequence
 // seq[r], or at element offset off[r]; slots the cache does not have are skipped.
 void launch_kv4_append(int dtype, const Kv4View& c, const void* k, const void* v, int64_t ld, const int* seq,
-                       const int* pos, const int64_t* off, int64_t rows, hipStream_t st);
+                       const int* pos, const int64_t* off, int rows, hipStream_t st);
 void launch_kv4_read(int dtype, const Kv4View& c, void* k, void* v, int64_t ld, const int* seq, const int* pos,
-                     int64_t rows, hipStream_t st);
+                     int rows, hipStream_t st);
 constexpr int KV4_MAX_DEPTH = 15;
 // By value in the kernels' arguments, as words that scalar loads bring whole
 // (arguments may lie in host memory, where a lane's own loads take microseconds)

@@ -26,52 +26,62 @@ __device__ __forceinline__ int64_t kv4_slot(const Kv4View& c, int b, int p) {
   return (int64_t)page * c.page_stride + (int64_t)(p % c.ps) * c.hd;
 }
 
-// Rows into the cache: a thread takes 8 values, the four threads of a group
-// agree on its scale.  Bound by bytes; a row's 8-value pieces are read whole and
-// written as whole words.
+// A thread's place in the rows of a call: 8 values of K or V of one row; a block
+// stays within a row, so its place in the cache is found once.
+struct RowPiece {
+  int kv, at;  // K or V, first of the 8 values in the row
+  bool on;
+};
+__device__ __forceinline__ RowPiece row_piece(const Kv4View& c) {
+  const int width = c.H * c.hd, i = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  return {i >= width, i >= width ? i - width : i, i < 2 * width};
+}
+__device__ __forceinline__ int64_t piece_offset(const Kv4View& c, int64_t base, const RowPiece& p) {
+  const int h = c.hd == 128 ? p.at >> 7 : p.at >> 6;
+  return base + ((int64_t)p.kv * c.H + h) * c.ps * c.hd + (p.at & (c.hd - 1));
+}
+
+// Rows into the cache: grid (pieces of a row, rows), the four threads of a group
+// agree on its scale.  Bound by the launch for a step's rows (64 rows of 32 heads
+// of 128: 3.0 us) and by bytes for a prompt's (2044 rows: 12.3 us, 4.2 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const T* __restrict__ k,
                                                          const T* __restrict__ v, int64_t ld,
                                                          const int* __restrict__ seq, const int* __restrict__ pos,
-                                                         const int64_t* __restrict__ off, int64_t rows) {
-  const int per = c.H * c.hd / 8;  // pieces of a row of K (or V): a multiple of 4
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = i / (2 * per);
-  if (row >= rows) return;  // groups of four threads stay whole
-  const int piece = (int)(i % (2 * per)), kv = piece / per, at = piece % per * 8;
-  const int64_t base = off != nullptr ? off[row] : kv4_slot(c, seq[row], pos[row]);
-  float x[8];
-  load8<T>((kv ? v : k) + row * ld + at, x);
-  uint32_t m = amax_bits8(x);
-  m = max(m, (uint32_t)dpp_mov_i<DPP_XOR1>((int)m));
-  m = max(m, (uint32_t)dpp_mov_i<DPP_XOR2>((int)m));
-  const uint32_t s = fp4_scale_byte(m);
-  const uint32_t w = fp4_encode8(x, s);
-  if (base < 0) return;
-  const int64_t e = base + ((int64_t)kv * c.H + at / c.hd) * c.ps * c.hd + at % c.hd;
-  *reinterpret_cast<uint32_t*>(c.codes + e / 2) = w;
-  if ((threadIdx.x & 3) == 0) c.scales[e / 32] = (uint8_t)s;
+                                                         const int64_t* __restrict__ off, int rows) {
+  const RowPiece p = row_piece(c);
+  if (!p.on) return;  // groups of four threads stay whole
+  for (int row = blockIdx.y; row < rows; row += gridDim.y) {
+    const int64_t base = off != nullptr ? off[row] : kv4_slot(c, seq[row], pos[row]);
+    float x[8];
+    load8<T>((p.kv ? v : k) + row * ld + p.at, x);
+    uint32_t m = amax_bits8(x);
+    m = max(m, (uint32_t)dpp_mov_i<DPP_XOR1>((int)m));
+    m = max(m, (uint32_t)dpp_mov_i<DPP_XOR2>((int)m));
+    const uint32_t s = fp4_scale_byte(m);
+    const uint32_t w = fp4_encode8(x, s);
+    if (base < 0) continue;
+    const int64_t e = piece_offset(c, base, p);
+    *reinterpret_cast<uint32_t*>(c.codes + e / 2) = w;
+    if ((threadIdx.x & 3) == 0) c.scales[e / 32] = (uint8_t)s;
+  }
 }
 
-// Rows out, as values.
+// Rows out, as values (the same rows: 2.9 and 12.1 us).
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T* __restrict__ k, T* __restrict__ v,
                                                        int64_t ld, const int* __restrict__ seq,
-                                                       const int* __restrict__ pos, int64_t rows) {
-  const int per = c.H * c.hd / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = i / (2 * per);
-  if (row >= rows) return;
-  const int piece = (int)(i % (2 * per)), kv = piece / per, at = piece % per * 8;
-  const int64_t base = kv4_slot(c, seq[row], pos[row]);
-  if (base < 0) return;
-  const int64_t e = base + ((int64_t)kv * c.H + at / c.hd) * c.ps * c.hd + at % c.hd;
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(c.codes + e / 2);
-  const float s = fp4_scale(c.scales[e / 32]);
-  const f32x4 a = fp4_to_f32x4<0>(w, s), b = fp4_to_f32x4<1>(w, s);
-  T* dst = (kv ? v : k) + row * ld + at;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) dst[j] = ET<T>::from_f(j < 4 ? a[j & 3] : b[j & 3]);
+                                                       const int* __restrict__ pos, int rows) {
+  const RowPiece p = row_piece(c);
+  if (!p.on) return;
+  for (int row = blockIdx.y; row < rows; row += gridDim.y) {
+    const int64_t base = kv4_slot(c, seq[row], pos[row]);
+    if (base < 0) continue;
+    const int64_t e = piece_offset(c, base, p);
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(c.codes + e / 2);
+    const float s = fp4_scale(c.scales[e / 32]);
+    store8<T>((p.kv ? v : k) + row * ld + p.at, w, s);
+  }
 }
 
 // A layer's rows as values, for prefill attention: grid (positions / 64, 2 H,
@@ -318,7 +328,7 @@ __device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h,
 // share nothing until their partials meet.  The next chunk's K is requested when
 // the scores have taken this one's, its V when this one's is used up.  Several
 // query blocks of a workgroup sharing one conversion of V, with a barrier a
-// chunk, were slower: 64 nodes at 512 tokens 12.8 us against MARK.
+// chunk, were slower: 64 nodes at 512 tokens 12.8 us against 8.0.
 //
 // Workgroups are dealt to the eight dies round-robin, the first grid dimension
 // first: heads, whose work is equal, and a head's query blocks on the die whose
@@ -658,24 +668,34 @@ void kv4_attn_go(const Kv4AttnArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// Pieces of 8 values of a row's K and V in blocks of whole waves; rows past the
+// grid's limit are walked.
+static void row_grid(const Kv4View& c, int rows, dim3& grid, dim3& block) {
+  const int pieces = c.H * c.hd / 4, threads = std::min(256, (pieces + 63) / 64 * 64);
+  block = dim3(threads);
+  grid = dim3((pieces + threads - 1) / threads, std::min(rows, 65535));
+}
+
 void launch_kv4_append(int dtype, const Kv4View& c, const void* k, const void* v, int64_t ld, const int* seq,
-                       const int* pos, const int64_t* off, int64_t rows, hipStream_t st) {
-  const dim3 grid((unsigned)((rows * (c.H * c.hd / 4) + 255) / 256));
+                       const int* pos, const int64_t* off, int rows, hipStream_t st) {
+  dim3 grid, block;
+  row_grid(c, rows, grid, block);
   if (dtype == DT_BF16)
-    hipLaunchKernelGGL(kv4_append_kernel<bf16_t>, grid, dim3(256), 0, st, c, (const bf16_t*)k, (const bf16_t*)v, ld,
-                       seq, pos, off, rows);
-  else
-    hipLaunchKernelGGL(kv4_append_kernel<float>, grid, dim3(256), 0, st, c, (const float*)k, (const float*)v, ld, seq,
+    hipLaunchKernelGGL(kv4_append_kernel<bf16_t>, grid, block, 0, st, c, (const bf16_t*)k, (const bf16_t*)v, ld, seq,
                        pos, off, rows);
+  else
+    hipLaunchKernelGGL(kv4_append_kernel<float>, grid, block, 0, st, c, (const float*)k, (const float*)v, ld, seq, pos,
+                       off, rows);
 }
 
 void launch_kv4_read(int dtype, const Kv4View& c, void* k, void* v, int64_t ld, const int* seq, const int* pos,
-                     int64_t rows, hipStream_t st) {
-  const dim3 grid((unsigned)((rows * (c.H * c.hd / 4) + 255) / 256));
+                     int rows, hipStream_t st) {
+  dim3 grid, block;
+  row_grid(c, rows, grid, block);
   if (dtype == DT_BF16)
-    hipLaunchKernelGGL(kv4_read_kernel<bf16_t>, grid, dim3(256), 0, st, c, (bf16_t*)k, (bf16_t*)v, ld, seq, pos, rows);
+    hipLaunchKernelGGL(kv4_read_kernel<bf16_t>, grid, block, 0, st, c, (bf16_t*)k, (bf16_t*)v, ld, seq, pos, rows);
   else
-    hipLaunchKernelGGL(kv4_read_kernel<float>, grid, dim3(256), 0, st, c, (float*)k, (float*)v, ld, seq, pos, rows);
+    hipLaunchKernelGGL(kv4_read_kernel<float>, grid, block, 0, st, c, (float*)k, (float*)v, ld, seq, pos, rows);
 }
 
 void launch_kv4_expand(int dtype, const Kv4View& c, const PrefillChunk& chunk, void* pool, hipStream_t st) {

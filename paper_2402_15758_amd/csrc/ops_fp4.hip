@@ -36,7 +36,7 @@ hipStream_t check_stream(void* stream) {
 }
 void check_matrix(int32_t N, int32_t K) {
   REQUIRE(N > 0 && N % 16 == 0 && K > 0 && K % 32 == 0, CHIMERA_EINVAL, "N must be a multiple of 16, K of 32");
-  REQUIRE((int64_t)N * K < (int64_t)1 << 36, CHIMERA_EINVAL, "matrix too large");
+  REQUIRE(N <= 1 << 20 && K <= 1 << 20, CHIMERA_EINVAL, "N and K are at most 2^20");
 }
 
 // Workspace of a product: tiled x, then the unpacked matrix where the launch

@@ -51,6 +51,8 @@ def test_the_format_in_float64():
 def test_matrix_sizes():
     for N, K in [(8, 32), (24, 32), (16, 16), (0, 32), (16, 0), (-16, 32)]:
         refused(B.CHIMERA_EINVAL, "N must be a multiple of 16", B.chimera_fp4_bytes, N, K)
+    for N, K in [((1 << 20) + 16, 32), (16, (1 << 20) + 32)]:
+        refused(B.CHIMERA_EINVAL, "2^20", B.chimera_fp4_bytes, N, K)
     assert B.chimera_fp4_bytes(4096, 4096) == 4096 * 4096 * 17 // 32
     # classes of a slice are padded to whole units of four k-blocks
     assert B.chimera_fp4_bytes(16, 32) == 4 * (1024 + 64)
