@@ -96,7 +96,7 @@ _PROTOS = {
     "chimera_kv4_append": [ctypes.POINTER(chimera_kv4), I32, P, P, I64, P, P, I32, P],
     "chimera_kv4_read": [ctypes.POINTER(chimera_kv4), I32, P, P, I32, P, P, I64, P],
     "chimera_kv4_attn_bytes": [ctypes.POINTER(chimera_kv4), I32, I32, PI64],
-    "chimera_kv4_attn": [ctypes.POINTER(chimera_kv4), I32, P, I64, P, I32, PI32, I32, ctypes.c_float, P, I64, P, I64,
+    "chimera_kv4_attn": [ctypes.POINTER(chimera_kv4), I32, P, I64, P, I32, P, I32, ctypes.c_float, P, I64, P, I64,
                          P],
 }
 
@@ -334,10 +334,12 @@ def chimera_kv4_attn_bytes(cache: chimera_kv4, n_heads: int, n_nodes: int) -> in
 def chimera_kv4_attn(cache: chimera_kv4, dtype: int, q_ptr: int, ldq: int, n_ptr: int, n_heads: int, parent,
                      n_nodes: int, scale: float, out_ptr: int, ldo: int, ws_ptr: int, ws_bytes: int, stream: int):
     """parent: a contiguous numpy int32 array of n_nodes entries, or None for a chain."""
-    if parent is not None and len(parent) != n_nodes:
-        raise ValueError("parent needs n_nodes entries")
-    _check(lib().chimera_kv4_attn(ctypes.byref(cache), dtype, q_ptr, ldq, n_ptr, n_heads, _i32p(parent), n_nodes,
-                                  scale, out_ptr, ldo, ws_ptr, ws_bytes, stream))
+    if parent is not None:
+        if parent.shape != (n_nodes,) or parent.dtype != "int32" or not parent.flags.c_contiguous:
+            raise ValueError("parent is a contiguous int32 array of n_nodes entries")
+        parent = parent.__array_interface__["data"][0]
+    _check(lib().chimera_kv4_attn(ctypes.byref(cache), dtype, q_ptr, ldq, n_ptr, n_heads, parent, n_nodes, scale,
+                                  out_ptr, ldo, ws_ptr, ws_bytes, stream))
 
 
 def chimera_ctx_free(ctx: int):

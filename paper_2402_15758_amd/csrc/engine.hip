@@ -433,6 +433,7 @@ void verify_layers(chimera_ctx* c, const VerifyRows& r, hipStream_t st, bool tim
       f.c = kv4_layer(kv, l, r.B);
       f.blocks = kv4_attn_blocks(r.B, H, H, r.N);
       f.units = kv4_attn_units((int64_t)kv->max_pages * kv->ps, f.blocks);
+      f.one = kv4_attn_one((int64_t)kv->max_pages * kv->ps);
       f.part_ml = f.part_o + (int64_t)r.B * f.units * r.N * hdim;
       f.o_mtiles = r.mtiles;
       launch_kv4_attn(dt, f, st);

@@ -168,6 +168,7 @@ struct Kv4AttnArgs {
   int Hq, N;
   int deepest;              // node depth
   int blocks, units;        // kv4_attn_blocks, kv4_attn_units
+  int one;                  // kv4_attn_one
   int o_mtiles;             // > 0: out is tiled, with this many 16-row tiles
   float scale;
   float* part_o;            // [B][H][units][N Hq / H][hd]
@@ -179,6 +180,8 @@ struct Kv4AttnArgs {
 int kv4_attn_blocks(int B, int Hq, int H, int N);
 int kv4_attn_units(int64_t cap, int blocks);
 int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int H, int hd, int N);
+// Whether a cache of cap positions a sequence is attended to in one launch.
+bool kv4_attn_one(int64_t cap);
 void launch_kv4_attn(int dtype, const Kv4AttnArgs& a, hipStream_t st);
 
 // ---- elementwise / norms ------------------------------------------------------

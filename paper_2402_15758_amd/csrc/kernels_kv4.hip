@@ -316,6 +316,109 @@ __device__ __forceinline__ void pv_half(const f32x4 (&s)[4], int kp, const T* v,
   }
 }
 
+// x of the lanes with bit B clear and y of those with it set, each summed over
+// the pair of lanes that differ in bit B.
+template <int B>
+__device__ __forceinline__ float pair_reduce(float x, float y, int lane) {
+  if constexpr (B == 5) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else if constexpr (B == 4) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else {
+    const bool up = (lane >> B) & 1;
+    const float keep = up ? y : x, give = up ? x : y;
+    if constexpr (B == 3) return keep + dpp_mov<DPP_ROR8>(give);
+    // lane ^ 4: mirrored within 8 (lane ^ 7), then within 4 (lane ^ 3)
+    return keep + dpp_mov<0x1B>(dpp_mov<DPP_MIRROR8>(give));
+  }
+}
+
+// The window of one query (node u, head hq of sequence b), a wave.  Lane 4 k + j
+// takes quarter j of window key k, of K for the score and of V for its share of
+// the output; the shares of the 16 keys are then added over the lanes, halving
+// the dimensions a lane holds with each of the four steps: the lane ends with
+// dimensions HD/4 j + (HD/64) rev .., rev the bits 5, 4, 3, 2 of the lane.
+// request(dim) may ask for what the shared pass left, as soon as n is known;
+// shared(dim, m, l, o) hands it over, for those dimensions, while the window's
+// rows are in flight.
+template <typename T, int HD, class Request, class Shared>
+__device__ __forceinline__ void window_query(const Kv4AttnArgs& a, int b, int u, int hq, int n, int lane,
+                                             Request&& request, Shared&& shared) {
+  constexpr int DPL = HD / 64, DQ = HD / 4;
+  const Kv4View& c = a.c;
+  const int h = hq / (a.Hq / c.H);
+  const int64_t row = (int64_t)b * a.N + u;
+  const int kw = lane >> 2, sub = lane & 3;
+  const int dim = DQ * sub + DPL * (8 * (lane >> 5) + 4 * ((lane >> 4) & 1) + 2 * ((lane >> 3) & 1) + ((lane >> 2) & 1));
+  const int deep = (int)(a.tree.depth[u / 8] >> (4 * (u & 7))) & 15, P = n + deep;
+  // this lane's window key
+  const int p = P - WIN + 1 + kw;
+  const int anc = ancestor(a.tree, u, deep, p - n, lane);
+  const int at = p < n ? p : n + anc;
+  const bool in = n >= 0 && p >= 0 && at < c.max_pages * c.ps;
+  const int page = in ? c.page_table[(int64_t)b * c.max_pages + (unsigned)at / (unsigned)c.ps] : -1;
+  request(dim);
+  Frag32<T> qf[HD / 32];
+  load_query<T, HD>((const T*)a.q + row * a.ldq + hq * HD, sub, a.scale < 0.f, qf);
+  const bool valid = (unsigned)page < (unsigned)c.n_pages;
+  const uint32_t r = valid ? (uint32_t)((int64_t)page * (c.page_stride / 32)) +
+                                 (h * c.ps + (unsigned)at % (unsigned)c.ps) * (HD / 32)
+                           : 0;
+  Quarter<HD> k, v;
+  k.load(c.codes, c.scales, r, sub);
+  v.load(c.codes + (int64_t)c.H * c.ps * HD / 2, c.scales + (int64_t)c.H * c.ps * HD / 32, r, sub);
+  float m = -CH_INF, l = 0.f, o[DPL];
+#pragma unroll
+  for (int d = 0; d < DPL; ++d) o[d] = 0.f;
+  shared(dim, m, l, o);
+  float acc = 0.f;
+  float sc = fp4_scale(k.s);
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) {
+    const f32x4 x0 = fp4_to_f32x4<0>(k.w[i], sc), x1 = fp4_to_f32x4<1>(k.w[i], sc);
+    const T* q = reinterpret_cast<const T*>(qf[i].v);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) acc = fmaf(ET<T>::to_f(q[t]), t < 4 ? x0[t & 3] : x1[t & 3], acc);
+  }
+  acc = acc + dpp_mov<DPP_XOR1>(acc);
+  acc = acc + dpp_mov<DPP_XOR2>(acc);
+  const float s = valid ? acc * (fabsf(a.scale) * LOG2E) : -CH_INF;
+  const float mn = fmaxf(m, wave_max(s));
+  const float alpha = __ballot(valid) != 0 ? exp2_from(m, mn) : 1.f;
+  const float pe = valid ? __builtin_amdgcn_exp2f(s - mn) : 0.f;
+  l = l * alpha + wave_sum(sub == 0 ? pe : 0.f);
+  if (!valid) v.clear();
+  sc = fp4_scale(v.s);
+  float w[DQ];
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) {
+    const f32x4 x0 = fp4_to_f32x4<0>(v.w[i], sc), x1 = fp4_to_f32x4<1>(v.w[i], sc);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      w[8 * i + t] = pe * x0[t];
+      w[8 * i + 4 + t] = pe * x1[t];
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < DQ / 2; ++d) w[d] = pair_reduce<5>(w[d], w[d + DQ / 2], lane);
+#pragma unroll
+  for (int d = 0; d < DQ / 4; ++d) w[d] = pair_reduce<4>(w[d], w[d + DQ / 4], lane);
+#pragma unroll
+  for (int d = 0; d < DQ / 8; ++d) w[d] = pair_reduce<3>(w[d], w[d + DQ / 8], lane);
+#pragma unroll
+  for (int d = 0; d < DQ / 16; ++d) w[d] = pair_reduce<2>(w[d], w[d + DQ / 16], lane);
+#pragma unroll
+  for (int d = 0; d < DPL; ++d) {
+    const float y = l == 0.f ? 0.f : (o[d] * alpha + w[d]) / l;  // 0: no visible key
+    if (a.o_mtiles > 0)
+      store_tiled<T>((T*)a.out, a.o_mtiles, (int)row, hq * HD + dim + d, y);
+    else
+      ((T*)a.out)[row * a.ldo + hq * HD + dim + d] = ET<T>::from_f(y);
+  }
+}
+
 // Partials of sequence b, cache head h, unit (group or super): one a query.
 __device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h, int unit, int nq) {
   return (((int64_t)b * a.c.H + h) * a.units + unit) * nq;
@@ -335,7 +438,10 @@ __device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h,
 // L2 has its keys (where H is a multiple of 8).  With the groups first, die i
 // took group i of every head (8 ragged sequences of 1024 to 4096 tokens, single
 // queries: 60 us instead of 37).
-template <typename T, int HD>
+//
+// ONE: a cache that holds a single group.  The workgroup goes on with its queries'
+// windows, from the partials in LDS: one launch, and no partial in memory.
+template <typename T, int HD, bool ONE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 3 : 2))) void kv4_shared(
     const Kv4AttnArgs a) {
   constexpr int VP = v_pitch<T, HD>(), OP = HD + 4, QP = HD + 16 / sizeof(T);  // row pitches: V, partials, queries
@@ -358,9 +464,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
   if (wave == 0)
     load_query<T, HD>((const T*)a.q + ((int64_t)b * a.N + u) * a.ldq + (h * gq + qi % gq) * HD, g, a.scale < 0.f, qf);
   const int maxk = n < 0 ? -1 : n + a.deepest - WIN;  // last position any query treats as shared
-  if (maxk < 0) return;                               // uniform
-  const bool supers = kv4_supers(maxk, a.blocks);
-  const int nu = maxk / (supers ? SUPER : GROUP) + 1, per = supers ? FAN : 1;  // chunks a wave
+  if (!ONE && maxk < 0) return;                       // uniform
+  const bool supers = !ONE && kv4_supers(maxk, a.blocks);
+  const int nu = ONE ? 1 : maxk / (supers ? SUPER : GROUP) + 1, per = supers ? FAN : 1;  // chunks a wave
   const int lim = n + node_depth(a.tree, u) - WIN;                             // this column's last shared position
   const uint8_t* vcodes = cv.codes + (int64_t)cv.H * cv.ps * HD / 2;
   const uint8_t* vscales = cv.scales + (int64_t)cv.H * cv.ps * HD / 32;
@@ -388,7 +494,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
 
   for (int unit = blockIdx.y; unit < nu; unit += gridDim.y) {
     const int c0 = (unit * FAN + wave) * per;
-    const int nc = min(per, maxk / CHUNK - c0 + 1);  // chunks with shared keys; may be <= 0
+    const int nc = maxk < 0 ? 0 : min(per, maxk / CHUNK - c0 + 1);  // chunks with shared keys; may be <= 0
     float m = -CH_INF, l = 0.f;
     f32x4 o[HD / 16];
 #pragma unroll
@@ -482,8 +588,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
       }
     }
     __syncthreads();
-    const int64_t base = part_slot(a, b, h, unit, nq) + q0;
     const int mine = min(nq - q0, 16);
+    if constexpr (ONE) {
+      constexpr int DPL = HD / 64;
+      for (int q = wave; q < mine; q += FAN) {  // wave-uniform
+        auto shared = [&](int dim, float& M, float& L, float (&O)[DPL]) {
+#pragma unroll
+          for (int w = 0; w < FAN; ++w) {
+            float x, y;
+            if (fold(M, L, ml[w][q][0], ml[w][q][1], x, y)) {
+#pragma unroll
+              for (int d = 0; d < DPL; ++d) O[d] = fold_value(O[d], x, stage_[w].o[q * OP + dim + d], y);
+            }
+          }
+        };
+        window_query<T, HD>(a, b, (q0 + q) / gq, h * gq + (q0 + q) % gq, n, lane, [](int) {}, shared);
+      }
+      return;
+    }
+    const int64_t base = part_slot(a, b, h, unit, nq) + q0;
     for (int i = tid; i < mine * (HD / 4); i += 256) {
       const int q = i / (HD / 4), d = i % (HD / 4) * 4;
       float M = -CH_INF, L = 0.f;
@@ -501,59 +624,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
   }
 }
 
-// x of the lanes with bit B clear and y of those with it set, each summed over
-// the pair of lanes that differ in bit B.
-template <int B>
-__device__ __forceinline__ float pair_reduce(float x, float y, int lane) {
-  if constexpr (B == 5) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  } else if constexpr (B == 4) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  } else {
-    const bool up = (lane >> B) & 1;
-    const float keep = up ? y : x, give = up ? x : y;
-    if constexpr (B == 3) return keep + dpp_mov<DPP_ROR8>(give);
-    // lane ^ 4: mirrored within 8 (lane ^ 7), then within 4 (lane ^ 3)
-    return keep + dpp_mov<0x1B>(dpp_mov<DPP_MIRROR8>(give));
-  }
-}
-
-// The window: grid (ceil(Hq / 4), N, B), a wave per query.  Lane 4 k + j takes
-// quarter j of window key k, of K for the score and of V for its share of the
-// output; the shares of the 16 keys are then added over the lanes, halving the
-// dimensions a lane holds with each of the four steps: the lane ends with
-// dimensions HD/4 j + (HD/64) rev .., rev the bits 5, 4, 3, 2 of the lane.  The
-// partials are folded, for those dimensions, while the rows are in flight, BATCH
-// a round trip, the first requested as soon as n is known.
+// grid (ceil(Hq / 4), N, B): the window after the shared pass's partials, BATCH of
+// them a round trip.
 template <typename T, int HD, int BATCH>
 __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
-  constexpr int DPL = HD / 64, DQ = HD / 4;
+  constexpr int DPL = HD / 64;
   const Kv4View& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hq = 4 * blockIdx.x + wave, u = blockIdx.y, b = blockIdx.z;
   if (hq >= a.Hq) return;  // wave-uniform
   const int gq = a.Hq / c.H, h = hq / gq, nq = a.N * gq, qi = u * gq + hq % gq;
-  const int64_t row = (int64_t)b * a.N + u;
-  const int kw = lane >> 2, sub = lane & 3;
-  const int dim = DQ * sub + DPL * (8 * (lane >> 5) + 4 * ((lane >> 4) & 1) + 2 * ((lane >> 3) & 1) + ((lane >> 2) & 1));
   const int n = min(a.n_b[b], c.max_pages * c.ps);
-  const int deep = (int)(a.tree.depth[u / 8] >> (4 * (u & 7))) & 15, P = n + deep;
-  // this lane's window key
-  const int p = P - WIN + 1 + kw;
-  const int anc = ancestor(a.tree, u, deep, p - n, lane);
-  const int at = p < n ? p : n + anc;
-  const bool in = n >= 0 && p >= 0 && at < c.max_pages * c.ps;
-  const int page = in ? c.page_table[(int64_t)b * c.max_pages + (unsigned)at / (unsigned)c.ps] : -1;
   const int maxk = n < 0 ? -1 : n + a.deepest - WIN;
   const bool supers = maxk >= 0 && kv4_supers(maxk, a.blocks);
-  const int lim = n < 0 ? -1 : P - WIN;  // last shared position of this query
+  // last shared position of this query
+  const int lim = n < 0 ? -1 : n + ((int)(a.tree.depth[u / 8] >> (4 * (u & 7))) & 15) - WIN;
   const int nu = lim < 0 ? 0 : lim / (supers ? SUPER : GROUP) + 1;
   const int64_t base = part_slot(a, b, h, 0, nq) + qi;
   float2 bml[BATCH];
   float bo[BATCH][DPL];
-  auto load_batch = [&](int g0) {  // past the last unit: the last again
+  auto load_batch = [&](int g0, int dim) {  // past the last unit: the last again
 #pragma unroll
     for (int t = 0; t < BATCH; ++t) {
       const int64_t i = base + (int64_t)min(g0 + t, nu - 1) * nq;
@@ -562,92 +652,44 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
       for (int d = 0; d < DPL; ++d) bo[t][d] = a.part_o[i * HD + dim + d];
     }
   };
-  if (nu > 0) load_batch(0);
-  Frag32<T> qf[HD / 32];
-  load_query<T, HD>((const T*)a.q + row * a.ldq + hq * HD, sub, a.scale < 0.f, qf);
-  const bool valid = (unsigned)page < (unsigned)c.n_pages;
-  const uint32_t r = valid ? (uint32_t)((int64_t)page * (c.page_stride / 32)) +
-                                 (h * c.ps + (unsigned)at % (unsigned)c.ps) * (HD / 32)
-                           : 0;
-  Quarter<HD> k, v;
-  k.load(c.codes, c.scales, r, sub);
-  v.load(c.codes + (int64_t)c.H * c.ps * HD / 2, c.scales + (int64_t)c.H * c.ps * HD / 32, r, sub);
-  float m = -CH_INF, l = 0.f, o[DPL], gm = -CH_INF, gl = 0.f, go[DPL];
+  auto request = [&](int dim) {
+    if (nu > 0) load_batch(0, dim);
+  };
+  auto shared = [&](int dim, float& m, float& l, float (&o)[DPL]) {
+    float gm = -CH_INF, gl = 0.f, go[DPL];
 #pragma unroll
-  for (int d = 0; d < DPL; ++d) o[d] = go[d] = 0.f;
-  for (int g0 = 0; g0 < nu; g0 += BATCH) {
-    if (g0 > 0) load_batch(g0);
+    for (int d = 0; d < DPL; ++d) go[d] = 0.f;
+    for (int g0 = 0; g0 < nu; g0 += BATCH) {
+      if (g0 > 0) load_batch(g0, dim);
 #pragma unroll
-    for (int t = 0; t < BATCH; ++t) {
-      if (g0 + t >= nu) break;
-      float x, y;
-      if (supers) {
-        if (fold(m, l, bml[t].x, bml[t].y, x, y)) {
+      for (int t = 0; t < BATCH; ++t) {
+        if (g0 + t >= nu) break;
+        float x, y;
+        if (supers) {
+          if (fold(m, l, bml[t].x, bml[t].y, x, y)) {
 #pragma unroll
-          for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, bo[t][d], y);
+            for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, bo[t][d], y);
+          }
+          continue;
         }
-        continue;
-      }
-      if (fold(gm, gl, bml[t].x, bml[t].y, x, y)) {  // groups make a super
+        if (fold(gm, gl, bml[t].x, bml[t].y, x, y)) {  // groups make a super
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, bo[t][d], y);
-      }
-      if (t % FAN == FAN - 1 || g0 + t == nu - 1) {
-        if (fold(m, l, gm, gl, x, y)) {
-#pragma unroll
-          for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
+          for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, bo[t][d], y);
         }
-        gm = -CH_INF;
-        gl = 0.f;
+        if (t % FAN == FAN - 1 || g0 + t == nu - 1) {
+          if (fold(m, l, gm, gl, x, y)) {
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) go[d] = 0.f;
+            for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
+          }
+          gm = -CH_INF;
+          gl = 0.f;
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) go[d] = 0.f;
+        }
       }
     }
-  }
-  float acc = 0.f;
-  float sc = fp4_scale(k.s);
-#pragma unroll
-  for (int i = 0; i < HD / 32; ++i) {
-    const f32x4 x0 = fp4_to_f32x4<0>(k.w[i], sc), x1 = fp4_to_f32x4<1>(k.w[i], sc);
-    const T* q = reinterpret_cast<const T*>(qf[i].v);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) acc = fmaf(ET<T>::to_f(q[t]), t < 4 ? x0[t & 3] : x1[t & 3], acc);
-  }
-  acc = acc + dpp_mov<DPP_XOR1>(acc);
-  acc = acc + dpp_mov<DPP_XOR2>(acc);
-  const float s = valid ? acc * (fabsf(a.scale) * LOG2E) : -CH_INF;
-  const float mn = fmaxf(m, wave_max(s));
-  const float alpha = __ballot(valid) != 0 ? exp2_from(m, mn) : 1.f;
-  const float pe = valid ? __builtin_amdgcn_exp2f(s - mn) : 0.f;
-  l = l * alpha + wave_sum(sub == 0 ? pe : 0.f);
-  if (!valid) v.clear();
-  sc = fp4_scale(v.s);
-  float w[DQ];
-#pragma unroll
-  for (int i = 0; i < HD / 32; ++i) {
-    const f32x4 x0 = fp4_to_f32x4<0>(v.w[i], sc), x1 = fp4_to_f32x4<1>(v.w[i], sc);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      w[8 * i + t] = pe * x0[t];
-      w[8 * i + 4 + t] = pe * x1[t];
-    }
-  }
-#pragma unroll
-  for (int d = 0; d < DQ / 2; ++d) w[d] = pair_reduce<5>(w[d], w[d + DQ / 2], lane);
-#pragma unroll
-  for (int d = 0; d < DQ / 4; ++d) w[d] = pair_reduce<4>(w[d], w[d + DQ / 4], lane);
-#pragma unroll
-  for (int d = 0; d < DQ / 8; ++d) w[d] = pair_reduce<3>(w[d], w[d + DQ / 8], lane);
-#pragma unroll
-  for (int d = 0; d < DQ / 16; ++d) w[d] = pair_reduce<2>(w[d], w[d + DQ / 16], lane);
-#pragma unroll
-  for (int d = 0; d < DPL; ++d) {
-    const float y = l == 0.f ? 0.f : (o[d] * alpha + w[d]) / l;  // 0: no visible key
-    if (a.o_mtiles > 0)
-      store_tiled<T>((T*)a.out, a.o_mtiles, (int)row, hq * HD + dim + d, y);
-    else
-      ((T*)a.out)[row * a.ldo + hq * HD + dim + d] = ET<T>::from_f(y);
-  }
+  };
+  window_query<T, HD>(a, b, u, hq, n, lane, request, shared);
 }
 
 template <typename T, int HD>
@@ -656,7 +698,11 @@ void kv4_attn_go(const Kv4AttnArgs& a, hipStream_t st) {
   // A workgroup walks the units of its place.  Three a CU are resident; more only
   // cost their start, 5 to 8 ns each, where a long table holds short sequences.
   const int y = std::min(a.units, std::max(1, 2048 / (x * a.c.B)));
-  hipLaunchKernelGGL((kv4_shared<T, HD>), dim3(x, y, a.c.B), dim3(256), 0, st, a);
+  if (a.one) {
+    hipLaunchKernelGGL((kv4_shared<T, HD, true>), dim3(x, 1, a.c.B), dim3(256), 0, st, a);
+    return;
+  }
+  hipLaunchKernelGGL((kv4_shared<T, HD, false>), dim3(x, y, a.c.B), dim3(256), 0, st, a);
   const dim3 grid((a.Hq + 3) / 4, a.N, a.c.B);
   if (a.units <= 4)
     hipLaunchKernelGGL((kv4_window<T, HD, 4>), grid, dim3(256), 0, st, a);
@@ -715,6 +761,8 @@ int kv4_attn_units(int64_t cap, int blocks) {
   const int64_t supers = (cap + SUPER - 1) / SUPER, groups = (cap + GROUP - 1) / GROUP;
   return (int)std::max(supers, std::min<int64_t>(groups, FAN * (int64_t)((SUPER_WGS + blocks - 1) / blocks)));
 }
+
+bool kv4_attn_one(int64_t cap) { return cap <= GROUP; }
 
 int64_t kv4_attn_bytes(int B, int64_t cap, int Hq, int H, int hd, int N) {
   return (int64_t)B * kv4_attn_units(cap, kv4_attn_blocks(B, Hq, H, N)) * N * Hq * (hd + 2) * 4;

@@ -276,6 +276,7 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
     const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
     a.blocks = kv4_attn_blocks(cache->batch, n_heads, cache->n_heads, n_nodes);
     a.units = kv4_attn_units(cap, a.blocks);
+    a.one = kv4_attn_one(cap);
     a.part_o = (float*)ws;
     a.part_ml = a.part_o + (int64_t)cache->batch * a.units * n_nodes * n_heads * cache->head_dim;
     launch_kv4_attn(dtype, a, st);

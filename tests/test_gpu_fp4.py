@@ -308,6 +308,27 @@ def test_a_query_does_not_depend_on_its_company(dtype):
         assert torch.equal(one.view(3, H * hd), whole[:, u]), u
 
 
+@pytest.mark.parametrize("dtype,hd,n", [("bf16", 128, 40), ("bf16", 128, 200), ("f32", 64, 130), ("bf16", 64, 2500)])
+def test_bits_do_not_depend_on_the_table_or_the_batch(dtype, hd, n):
+    """The work is dealt by its amount and by the table's length (one launch, groups,
+    supers): a short and a long table, one sequence and a batch of 300 of it."""
+    H, page, nodes = 2, 16, 3
+    parents = R.tree(nodes, 2)
+    c = R.Cache([n], nodes, H, hd, page, dtype, 41, gap=0).to("cuda")
+    q = queries(1, nodes, 2 * H, hd, dtype, 13).cuda()
+    want = attend(c, q, [n], parents, 0.1)
+    short = c.table
+    c.table = torch.cat((short, torch.full((1, 1000), -1, dtype=torch.int32, device="cuda")), 1)
+    assert torch.equal(attend(c, q, [n], parents, 0.1), want)
+    for table in (short, c.table):
+        c.table = table.repeat(300, 1)
+        lens = [n] * 300
+        lens[7] = -1
+        out = attend(c, q.repeat(300, 1, 1, 1), lens, parents, 0.1).view(300, -1)
+        keep = torch.arange(300, device="cuda") != 7
+        assert bool((out[keep] == want.view(1, -1)).all()) and bool((out[7] == 0).all())
+
+
 def test_attention_ignores_what_it_does_not_see():
     """Bad pages, positions past the table, and NaN in rows of other branches and
     behind the sequence."""
