@@ -203,7 +203,8 @@ __device__ __forceinline__ void row_targets(const GemmShape& sh, const GemmEpi& 
 // One workgroup's run of CB column blocks from cb0, rows 16 mb0 .. 16 (mb0 +
 // MB) - 1 of one slice; the four waves take one class each.
 template <typename T, int MB, int CB, bool RM>
-__device__ __forceinline__ void fp4_run(const GemmShape& sh, const GemmEpi& e, int64_t ldx, const Fp4Shape& w4, int kind, int cb0, int mb0, int slice, f32x4* red, const RowMeta* rm,
+__device__ __forceinline__ void fp4_run(const GemmShape& sh, const GemmEpi& e, int64_t ldx, const Fp4Shape& w4,
+                                        int kind, int cb0, int mb0, int slice, f32x4* red, const RowMeta* rm,
                                         float* stage) {
   constexpr int XP = MB >= 4 ? 2 : 4;  // k-blocks of X in flight
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -318,6 +319,13 @@ __device__ __forceinline__ void fp4_run(const GemmShape& sh, const GemmEpi& e, i
 // column blocks, the others CBA - 1.  mapped: the row blocks of a run go to one
 // die (dealt round-robin by linear id), whose L2 then has their weights (256 rows,
 // 4096 x 12288: 43.0 -> 37.4 us).
+//
+// A quad of weights (1 KiB of codes a wave) is requested while the quad before it is
+// converted, straight from memory: nothing of W is read twice by a workgroup.  Up
+// to 16 rows it is bound by that stream (1 row of 22016 x 4096 12.4 us, 3.9 TB/s);
+// from 64 rows on by each CU's intake of its activations (64 rows of 12288 x 4096
+// 15.8 us, 22016 x 4096 20), which longer runs of columns would take in less often
+// but do not fit the registers with.
 template <typename T, int MB, int CBA, bool RM>
 __global__ __launch_bounds__(256) void gemm_fp4_kernel(const GemmShape sh, const GemmEpi e, int64_t ldx,
                                                        const Fp4Shape w4, int kind, int nbig, int mapped) {
@@ -352,7 +360,8 @@ constexpr int FP4_ROWS_BYTES = 112 << 10;
 // Its share is short (35 KB of 4096 x 16), a quarter of the bf16 kernels'.  The
 // rows are staged in LDS, only the ones there are; a thread's first pieces are
 // requested before its weights, since loads return in order and the weights
-// need not be waited for there.
+// need not be waited for there.  One row of 4096 x 4096 4.5 us with its launch in a
+// graph (floor 1.7): a start, a round trip for rows and weights and two barriers.
 template <typename T, int S, bool RM>
 __global__ __launch_bounds__(256 * S) void gemm_fp4_whole_kernel(const GemmShape sh, const GemmEpi e, int64_t ldx,
                                                                  const Fp4Shape w4) {
@@ -451,7 +460,7 @@ Fp4Route fp4_route(int dtype, int M, int N, int K, int splits, int kind, int64_t
 constexpr int FP4_CB_MAX = 8;
 constexpr int FP4_WGS = 256;
 
-// Column runs of a slice: GEMM_WGS workgroups' worth, at most FP4_CB_MAX blocks
+// Column runs of a slice: FP4_WGS workgroups' worth, at most FP4_CB_MAX blocks
 // long; the first `big` runs have `run` blocks, the others one less.
 struct Fp4Runs {
   int runs, run, big;

@@ -433,6 +433,11 @@ __device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h,
 // query blocks of a workgroup sharing one conversion of V, with a barrier a
 // chunk, were slower: 64 nodes at 512 tokens 12.8 us against 8.0.
 //
+// Eight single queries of 1024 to 4096 tokens, 32 heads: 26 us, 3.4 TB/s of cache;
+// its loads alone take 21 us, and without them the conversions and the softmax
+// (485 instructions a chunk) 23.  One of 32768 tokens with 8 cache heads: 15 us, a
+// wave a SIMD and its chain of four chunks.
+//
 // Workgroups are dealt to the eight dies round-robin, the first grid dimension
 // first: heads, whose work is equal, and a head's query blocks on the die whose
 // L2 has its keys (where H is a multiple of 8).  With the groups first, die i
@@ -625,7 +630,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
 }
 
 // grid (ceil(Hq / 4), N, B): the window after the shared pass's partials, BATCH of
-// them a round trip.
+// them a round trip.  Dependent round trips (n, page, rows) bound it: 64 nodes of 32
+// heads 5.4 us, 8192 queries 12, one with 32 partials 11.
 template <typename T, int HD, int BATCH>
 __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
   constexpr int DPL = HD / 64;

@@ -378,6 +378,109 @@ def test_extreme_scores():
     assert torch.isnan(attend(c, q.cuda(), lens, None, 1.0)).all()
 
 
+# ---- sizes past 31 and 32 bits, the widest staging, the smallest numbers -------------
+@pytest.mark.parametrize("dtype,M,N,K", [("bf16", 14, 320, 4096), ("f32", 7, 336, 4096), ("bf16", 4, 64, 14336)])
+def test_product_of_the_longest_staged_rows(dtype, M, N, K):
+    """112 KiB of rows in LDS, next to the workgroup's sums."""
+    g = torch.Generator().manual_seed(M)
+    x = torch.randn(M, K, generator=g).to(R.TYPES[dtype])
+    w = weights(K, N, dtype, M + 1)
+    check_product(x, w, product(x.cuda(), pack(w.cuda(), dtype), N, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 40])
+def test_product_of_the_smallest_weights(dtype, M):
+    """Groups at the smallest scale, whose smallest values are subnormal."""
+    g = torch.Generator().manual_seed(M)
+    x = (torch.randn(M, 64, generator=g) * 2.0 ** 100).to(R.TYPES[dtype])
+    w = (torch.randint(-7, 8, (64, 16), generator=g).float() * 2.0 ** -127).to(R.TYPES[dtype])
+    check_product(x, w, product(x.cuda(), pack(w.cuda(), dtype), 16, dtype))
+
+
+def test_product_with_a_matrix_past_32_bits():
+    """131072 x 40000: over 2^32 values, 2.8 GB packed; first and last columns."""
+    N, K = 40000, 131072
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.empty(K, N, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    x = torch.randn(600, K, generator=g, device="cuda").bfloat16()
+    p = pack(w, "bf16")
+    cols = [w[:, :16].cpu(), w[:, -16:].cpu()]
+    del w
+    for M in (1, 40, 600):
+        y = product(x[:M], p, N, "bf16")
+        check_product(x[:M].cpu(), cols[0], y[:, :16])
+        check_product(x[:M].cpu(), cols[1], y[:, -16:])
+    u = unpack(p, N, K, "bf16")
+    assert same(u[:, -16:], held_w(cols[1]))
+    del u, p, x, y
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_pool_past_32_bits(dtype):
+    """A cache of 140000 pages, over 2^31 groups of values (39 GB): rows in its
+    first and its last pages."""
+    lens, nodes, H, hd, page = [700, 90], 4, 8, 128, 256
+    n_pages = 140000
+    parents = R.tree(nodes, 2)
+    assert n_pages * 2 * H * page * hd // 32 > 2 ** 31
+    nb = B.chimera_kv4_bytes(n_pages, page, H, hd)
+    pool = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 2], [n_pages // 2, n_pages - 3, -1]], dtype=torch.int32,
+                         device="cuda")
+    c = R.Cache(lens, nodes, H, hd, page, dtype, 3)
+    kv = c.kv
+    c.pool, c.table, c.n_pages = pool, table, n_pages
+    for b in range(2):
+        x = kv[b].cuda()
+        rows, D = x.shape[0], H * hd
+        seq = torch.full((rows,), b, dtype=torch.int32, device="cuda")
+        pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+        B.chimera_kv4_append(c.struct(), DT[dtype], x.data_ptr(), x[:, 1].data_ptr(), 2 * D, seq.data_ptr(),
+                             pos.data_ptr(), rows, stream())
+        out = torch.empty_like(x)
+        B.chimera_kv4_read(c.struct(), DT[dtype], seq.data_ptr(), pos.data_ptr(), rows, out.data_ptr(),
+                           out[:, 1].data_ptr(), 2 * D, stream())
+        assert same(out, R.held(kv[b]))
+    q = queries(2, nodes, 2 * H, hd, dtype, 6)
+    want, tol = R.attention(q, kv, lens, parents, 0.1)
+    check_attention(attend(c, q.cuda(), lens, parents, 0.1), want, tol)
+    del pool
+    c.pool = None
+    torch.cuda.empty_cache()
+
+
+def test_many_rows_and_many_sequences():
+    """More rows than a grid's second dimension holds, and a batch at its limit."""
+    H, hd, page, B_ = 1, 64, 4, 65535
+    table = torch.arange(B_, dtype=torch.int32, device="cuda").view(B_, 1)
+    nb = B.chimera_kv4_bytes(B_, page, H, hd)
+    c = R.Cache([1], 1, H, hd, page, "bf16", 1)
+    c.pool, c.table, c.n_pages = torch.zeros(nb, dtype=torch.uint8, device="cuda"), table, B_
+    rows = 2 * B_
+    x = torch.randn(rows, hd, generator=torch.Generator().manual_seed(5)).bfloat16()
+    seq = torch.arange(rows, dtype=torch.int32, device="cuda") % B_
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") // B_
+    xd = x.cuda()
+    B.chimera_kv4_append(c.struct(), 1, xd.data_ptr(), xd.data_ptr(), hd, seq.data_ptr(), pos.data_ptr(), rows,
+                         stream())
+    out = torch.empty(2, rows, hd, dtype=torch.bfloat16, device="cuda")
+    B.chimera_kv4_read(c.struct(), 1, seq.data_ptr(), pos.data_ptr(), rows, out[0].data_ptr(), out[1].data_ptr(), hd,
+                       stream())
+    h = R.held(x)
+    assert same(out[0], h) and same(out[1], h)
+    # one committed token and the new one; the two rows' weights by hand
+    q = queries(B_, 1, 1, hd, "bf16", 2)
+    got = attend(c, q.cuda(), [1] * B_, None, 0.125).double().cpu()
+    k = h.view(2, B_, hd)
+    s = torch.stack([(q.view(B_, hd).double() * k[i]).sum(-1) * 0.125 for i in range(2)])
+    want = (torch.softmax(s, 0).unsqueeze(-1) * k).sum(0)
+    ds = (hd + 8) * 2.0 ** -23 * 0.125 * (q.view(B_, hd).double().abs() * k.abs().amax(0)).sum(-1, keepdim=True)
+    top = k.abs().amax((0, 2)).unsqueeze(-1)
+    assert bool(((got - want).abs() <= 2.0 ** -8 * 1.01 * want.abs() + 2 * (2 * ds + 2.0 ** -15) * top).all())
+
+
 # ---- together, as a decode step uses them ------------------------------------------
 def test_a_layer_step_captured_and_replayed():
     """Projections from 4-bit weights, rows into the cache, attention over it and

@@ -187,6 +187,30 @@ def test_cache_holds_rounded_rows_and_compacts_them():
             x.close()
 
 
+def test_typical_decoding_and_trigram_cache():
+    """The other decoding modes over both 4-bit formats: replayed and eager typical
+    steps agree, and a lookup cache leaves greedy verification lossless; fewer
+    prompts than places, and a session used again."""
+    w = synth.make_weights(SMALL, std=0.06)
+    ps = prompts([70, 33], SMALL.vocab, 11)
+    kw = dict(weight_format="fp4", kv_format="fp4")
+    want = greedy(SMALL, w, ps, 24, **kw)
+    s = Session(SMALL, w, synth.TREES["T32"], max_batch=3, max_len=512, **kw)
+    s.trigram_cache(1 << 12)
+    for _ in range(2):
+        assert s.generate(ps, 24)[0] == want
+    s.trigram_cache(0)
+    typical = []
+    for graph in (True, False, True):
+        s.set_decoding(True, temperature=0.8, seed=5)
+        s.set_graph(graph)
+        typical.append(run(s, ps, 5))
+    for r in typical[1:]:
+        for x, y in zip(typical[0][1] + typical[0][2] + typical[0][3], r[1] + r[2] + r[3]):
+            assert np.array_equal(x, y)
+    s.close()
+
+
 def test_formats_and_sizes():
     with pytest.raises(ValueError):
         Session(SMALL, None, (), kv_format="int8")
