@@ -629,12 +629,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
   }
 }
 
-// grid (ceil(Hq / 4), N, B): the window after the shared pass's partials, BATCH of
-// them a round trip.  Dependent round trips (n, page, rows) bound it: 64 nodes of 32
-// heads 5.4 us, 8192 queries 12, one with 32 partials 11.
-template <typename T, int HD, int BATCH>
-__global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
-  constexpr int DPL = HD / 64;
+constexpr int WINDOW_BATCH = 32;  // partials of a query a wave holds at most
+
+// 16 bytes a lane, 1 KiB a wave, from memory into LDS.
+__device__ __forceinline__ void dma_1k(const float* src, float* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+// grid (ceil(Hq / 4), N, B): the window after the shared pass's partials, a wave a
+// query.  The partials go straight to LDS, `batch` of them a round trip, and are
+// folded in a short loop: unrolled over registers, the code of 32 was 27 KB, and
+// most of the time went into fetching it (WINDOW_FIGURES).
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a, int batch) {
+  constexpr int DPL = HD / 64, LANES = HD / 4, PER = 64 / LANES;  // lanes of a partial, partials of a load
+  extern __shared__ __attribute__((aligned(16))) float parts[];   // [4][batch][HD], batch a multiple of FAN
   const Kv4View& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hq = 4 * blockIdx.x + wave, u = blockIdx.y, b = blockIdx.z;
@@ -647,52 +657,50 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a) {
   const int lim = n < 0 ? -1 : n + ((int)(a.tree.depth[u / 8] >> (4 * (u & 7))) & 15) - WIN;
   const int nu = lim < 0 ? 0 : lim / (supers ? SUPER : GROUP) + 1;
   const int64_t base = part_slot(a, b, h, 0, nq) + qi;
-  float2 bml[BATCH];
-  float bo[BATCH][DPL];
-  auto load_batch = [&](int g0, int dim) {  // past the last unit: the last again
-#pragma unroll
-    for (int t = 0; t < BATCH; ++t) {
-      const int64_t i = base + (int64_t)min(g0 + t, nu - 1) * nq;
-      bml[t] = *reinterpret_cast<const float2*>(a.part_ml + i * 2);
-#pragma unroll
-      for (int d = 0; d < DPL; ++d) bo[t][d] = a.part_o[i * HD + dim + d];
-    }
+  float* const mine = parts + wave * batch * HD;
+  float2 bml = float2{-CH_INF, 0.f};  // lane t: partial t of the batch
+  auto load_batch = [&](int g0) {     // past the last partial: the last again
+    bml = reinterpret_cast<const float2*>(a.part_ml)[base + (int64_t)min(g0 + lane, nu - 1) * nq];
+    const int count = min(nu - g0, batch);
+#pragma unroll 1
+    for (int i = 0; i < count; i += PER)
+      dma_1k(a.part_o + (base + (int64_t)min(g0 + i + lane / LANES, nu - 1) * nq) * HD + 4 * (lane % LANES),
+             mine + i * HD);
   };
-  auto request = [&](int dim) {
-    if (nu > 0) load_batch(0, dim);
+  auto request = [&](int) {
+    if (nu > 0) load_batch(0);
   };
   auto shared = [&](int dim, float& m, float& l, float (&o)[DPL]) {
     float gm = -CH_INF, gl = 0.f, go[DPL];
 #pragma unroll
     for (int d = 0; d < DPL; ++d) go[d] = 0.f;
-    for (int g0 = 0; g0 < nu; g0 += BATCH) {
-      if (g0 > 0) load_batch(g0, dim);
+    for (int g0 = 0; g0 < nu; g0 += batch) {
+      if (g0 > 0) load_batch(g0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const int count = min(nu - g0, batch);
+#pragma unroll 1
+      for (int t = 0; t < count; ++t) {
+        const float m2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(bml.x), t));
+        const float l2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(bml.y), t));
+        float x, y, o2[DPL];
 #pragma unroll
-      for (int t = 0; t < BATCH; ++t) {
-        if (g0 + t >= nu) break;
-        float x, y;
-        if (supers) {
-          if (fold(m, l, bml[t].x, bml[t].y, x, y)) {
+        for (int d = 0; d < DPL; ++d) o2[d] = mine[t * HD + dim + d];
+        if (fold(gm, gl, m2, l2, x, y)) {
 #pragma unroll
-            for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, bo[t][d], y);
-          }
-          continue;
+          for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, o2[d], y);
         }
-        if (fold(gm, gl, bml[t].x, bml[t].y, x, y)) {  // groups make a super
+        // four groups make a super; a super by itself is one already
+        if (!supers && t % FAN != FAN - 1 && g0 + t != nu - 1) continue;
+        if (fold(m, l, gm, gl, x, y)) {
 #pragma unroll
-          for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, bo[t][d], y);
+          for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
         }
-        if (t % FAN == FAN - 1 || g0 + t == nu - 1) {
-          if (fold(m, l, gm, gl, x, y)) {
+        gm = -CH_INF;
+        gl = 0.f;
 #pragma unroll
-            for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
-          }
-          gm = -CH_INF;
-          gl = 0.f;
-#pragma unroll
-          for (int d = 0; d < DPL; ++d) go[d] = 0.f;
-        }
+        for (int d = 0; d < DPL; ++d) go[d] = 0.f;
       }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next batch comes
     }
   };
   window_query<T, HD>(a, b, u, hq, n, lane, request, shared);
@@ -710,12 +718,8 @@ void kv4_attn_go(const Kv4AttnArgs& a, hipStream_t st) {
   }
   hipLaunchKernelGGL((kv4_shared<T, HD, false>), dim3(x, y, a.c.B), dim3(256), 0, st, a);
   const dim3 grid((a.Hq + 3) / 4, a.N, a.c.B);
-  if (a.units <= 4)
-    hipLaunchKernelGGL((kv4_window<T, HD, 4>), grid, dim3(256), 0, st, a);
-  else if (a.units <= 8)
-    hipLaunchKernelGGL((kv4_window<T, HD, 8>), grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((kv4_window<T, HD, 32>), grid, dim3(256), 0, st, a);
+  const int batch = std::min(WINDOW_BATCH, (a.units + FAN - 1) / FAN * FAN);
+  hipLaunchKernelGGL((kv4_window<T, HD>), grid, dim3(256), (size_t)4 * batch * HD * sizeof(float), st, a, batch);
 }
 
 }  // namespace
