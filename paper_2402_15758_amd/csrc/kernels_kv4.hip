@@ -419,6 +419,10 @@ __device__ __forceinline__ void window_query(const Kv4AttnArgs& a, int b, int u,
   }
 }
 
+__device__ __forceinline__ float lane_value(float v, int lane) {  // uniform
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
 // Partials of sequence b, cache head h, unit (group or super): one a query.
 __device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h, int unit, int nq) {
   return (((int64_t)b * a.c.H + h) * a.units + unit) * nq;
@@ -638,9 +642,11 @@ __device__ __forceinline__ void dma_1k(const float* src, float* lds) {
 }
 
 // grid (ceil(Hq / 4), N, B): the window after the shared pass's partials, a wave a
-// query.  The partials go straight to LDS, `batch` of them a round trip, and are
-// folded in a short loop: unrolled over registers, the code of 32 was 27 KB, and
-// most of the time went into fetching it (WINDOW_FIGURES).
+// query.  The partials go straight to LDS, `batch` of them a round trip.  Unrolled
+// over registers, 32 of them were 27 KB of code and folds of dependent exponentials;
+// now the lanes find all factors at once and a short loop multiplies and adds (one
+// query of 32768 tokens, 32 partials: 12.4 -> 7.1 us).  Dependent round trips (n,
+// page, rows) bound it: 64 nodes of 32 heads 5.4 us, 8192 queries 12.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a, int batch) {
   constexpr int DPL = HD / 64, LANES = HD / 4, PER = 64 / LANES;  // lanes of a partial, partials of a load
@@ -662,7 +668,7 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a, int batch
   auto load_batch = [&](int g0) {     // past the last partial: the last again
     bml = reinterpret_cast<const float2*>(a.part_ml)[base + (int64_t)min(g0 + lane, nu - 1) * nq];
     const int count = min(nu - g0, batch);
-#pragma unroll 1
+#pragma unroll 2
     for (int i = 0; i < count; i += PER)
       dma_1k(a.part_o + (base + (int64_t)min(g0 + i + lane / LANES, nu - 1) * nq) * HD + 4 * (lane % LANES),
              mine + i * HD);
@@ -671,34 +677,71 @@ __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a, int batch
     if (nu > 0) load_batch(0);
   };
   auto shared = [&](int dim, float& m, float& l, float (&o)[DPL]) {
-    float gm = -CH_INF, gl = 0.f, go[DPL];
-#pragma unroll
-    for (int d = 0; d < DPL; ++d) go[d] = 0.f;
     for (int g0 = 0; g0 < nu; g0 += batch) {
       if (g0 > 0) load_batch(g0);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      const int count = min(nu - g0, batch);
-#pragma unroll 1
-      for (int t = 0; t < count; ++t) {
-        const float m2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(bml.x), t));
-        const float l2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(bml.y), t));
-        float x, y, o2[DPL];
+      const int count = min(nu - g0, batch), step = supers ? 1 : FAN;
+      // The folds' factors hang on running maxima alone: every lane finds those of
+      // its partial.  top: the maximum of a partial, of a super's groups then.
+      const bool have = lane < count && bml.y != 0.f;
+      const uint64_t on = __ballot(have);
+      float top = have ? bml.x : -CH_INF, gx = 0.f, gy = 0.f;
+      if (!supers) {
+        float run = fmaxf(top, __shfl_up(top, 1, FAN));
+        run = fmaxf(run, __shfl_up(run, 2, FAN));
+        const float before = __shfl_up(run, 1, FAN);
+        gx = lane % FAN == 0 ? 0.f : exp2_from(before, run);
+        gy = __builtin_amdgcn_exp2f(top - run);
+        top = __shfl(run, FAN - 1, FAN);
+      }
+      float run = top;
+      for (int s = step; s < WINDOW_BATCH; s *= 2) {
+        const float v = __shfl_up(run, s);
+        run = lane >= s ? fmaxf(run, v) : run;
+      }
+      run = fmaxf(run, m);
+      const float prev = __shfl_up(run, step);
+      const float x = exp2_from(lane < step ? m : prev, run), y = __builtin_amdgcn_exp2f(top - run);
+      m = lane_value(run, count - 1);
+      float gl = l, go[DPL];  // supers: all there is; groups: a super's, none at first
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) o2[d] = mine[t * HD + dim + d];
-        if (fold(gm, gl, m2, l2, x, y)) {
-#pragma unroll
-          for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], x, o2[d], y);
-        }
-        // four groups make a super; a super by itself is one already
-        if (!supers && t % FAN != FAN - 1 && g0 + t != nu - 1) continue;
-        if (fold(m, l, gm, gl, x, y)) {
-#pragma unroll
-          for (int d = 0; d < DPL; ++d) o[d] = fold_value(o[d], x, go[d], y);
-        }
-        gm = -CH_INF;
+      for (int d = 0; d < DPL; ++d) go[d] = o[d];
+      if (!supers) {
         gl = 0.f;
 #pragma unroll
         for (int d = 0; d < DPL; ++d) go[d] = 0.f;
+      }
+#pragma unroll 1
+      for (int t0 = 0; t0 < count; t0 += FAN) {
+        float o2[FAN][DPL];
+#pragma unroll
+        for (int i = 0; i < FAN; ++i)
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) o2[i][d] = mine[(t0 + i) * HD + dim + d];
+        const uint32_t here = (uint32_t)(on >> t0) & ((1 << FAN) - 1);  // uniform, as all that follows
+#pragma unroll
+        for (int i = 0; i < FAN; ++i) {
+          if (((here >> i) & 1) == 0) continue;
+          const float l2 = lane_value(bml.y, t0 + i);
+          const float xt = lane_value(supers ? x : gx, t0 + i), yt = lane_value(supers ? y : gy, t0 + i);
+          gl = fold_value(gl, xt, l2, yt);
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) go[d] = fold_value(go[d], xt, o2[i][d], yt);
+        }
+        if (supers || here == 0) continue;  // supers: gl and go are the running sums
+        const float xt = lane_value(x, t0), yt = lane_value(y, t0);
+        l = fold_value(l, xt, gl, yt);
+        gl = 0.f;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) {
+          o[d] = fold_value(o[d], xt, go[d], yt);
+          go[d] = 0.f;
+        }
+      }
+      if (supers) {
+        l = gl;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) o[d] = go[d];
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next batch comes
     }

@@ -451,6 +451,30 @@ def test_a_pool_past_32_bits(dtype):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("H,n", [(8, 34000), (1, 34000)])
+def test_more_partials_than_a_wave_holds(H, n):
+    """33 supers of a query, and 133 groups, the last of either cut short; a stretch
+    of unknown pages in the middle."""
+    hd, page = 64, 64
+    kv = (torch.randn(n + 1, 2, H, hd, generator=torch.Generator().manual_seed(H)) * 0.7).bfloat16()
+    pages = n // page + 1
+    c = R.Cache([1], 1, H, hd, page, "bf16", 1)
+    c.n_pages = pages
+    c.table = torch.randperm(pages, generator=torch.Generator().manual_seed(2)).to(torch.int32).view(1, -1).cuda()
+    c.pool = torch.zeros(B.chimera_kv4_bytes(pages, page, H, hd), dtype=torch.uint8, device="cuda")
+    x = kv.cuda()
+    seq = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    pos = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    B.chimera_kv4_append(c.struct(), 1, x.data_ptr(), x[:, 1].data_ptr(), 2 * H * hd, seq.data_ptr(), pos.data_ptr(),
+                         n + 1, stream())
+    q = queries(1, 1, 2 * H, hd, "bf16", 3)
+    for lost in (False, True):
+        if lost:
+            c.table[0, 40:200] = -1  # positions 2560 .. 12799: whole supers and groups
+        want, tol = R.attention(q, [kv], [n], [-1], 0.2, seen=lambda b, p: not lost or not 2560 <= p < 12800)
+        check_attention(attend(c, q.cuda(), [n], None, 0.2), want, tol)
+
+
 def test_many_rows_and_many_sequences():
     """More rows than a grid's second dimension holds, and a batch at its limit."""
     H, hd, page, B_ = 1, 64, 4, 65535
