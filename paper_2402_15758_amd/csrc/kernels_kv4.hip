@@ -272,20 +272,23 @@ __device__ __forceinline__ void chunk_weights(f32x4 (&s)[4], float scale2, uint6
 }
 
 // O^T += V^T P^T over the 32 keys of half kp, staged as rows v.  A weight enters
-// the bf16 MFMA as two terms, hi = bf16(p) and bf16(p - hi): 16 bits of it, a
-// rounding of 2^-17, next to the 2^-9 of a bf16 output; 4-bit values are exact.
+// the bf16 MFMA as three terms, hi = bf16(p), mid = bf16(p - hi) and the rest: all
+// 24 bits of the float, and 4-bit values are exact, so every product is.
 template <typename T, int HD>
 __device__ __forceinline__ void pv_half(const f32x4 (&s)[4], int kp, const T* v, int g, int c16, f32x4 (&o)[HD / 16]) {
   constexpr int VP = v_pitch<T, HD>();
   if constexpr (sizeof(T) == 2) {
-    uint32_t ph[4], pl[4];
+    uint32_t ph[4], pm[4], pl[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float a0 = s[2 * kp + q / 2][2 * (q % 2)], a1 = s[2 * kp + q / 2][2 * (q % 2) + 1];
       ph[q] = cvt_pk_bf16(a0, a1);
-      pl[q] = cvt_pk_bf16(a0 - __uint_as_float(ph[q] << 16), a1 - __uint_as_float(ph[q] & 0xffff0000u));
+      const float r0 = a0 - __uint_as_float(ph[q] << 16), r1 = a1 - __uint_as_float(ph[q] & 0xffff0000u);
+      pm[q] = cvt_pk_bf16(r0, r1);
+      pl[q] = cvt_pk_bf16(r0 - __uint_as_float(pm[q] << 16), r1 - __uint_as_float(pm[q] & 0xffff0000u));
     }
     const int4 hf = int4{(int)ph[0], (int)ph[1], (int)ph[2], (int)ph[3]};
+    const int4 mf = int4{(int)pm[0], (int)pm[1], (int)pm[2], (int)pm[3]};
     const int4 lf = int4{(int)pl[0], (int)pl[1], (int)pl[2], (int)pl[3]};
     const T* vrow = v + (4 * g + (c16 >> 2)) * VP + 4 * (c16 & 3);
 #pragma unroll
@@ -299,6 +302,8 @@ __device__ __forceinline__ void pv_half(const f32x4 (&s)[4], int kp, const T* v,
       }
       o[d2] = mfma_kb<T>(vf[0], hf, o[d2]);
       o[d2 + 1] = mfma_kb<T>(vf[1], hf, o[d2 + 1]);
+      o[d2] = mfma_kb<T>(vf[0], mf, o[d2]);
+      o[d2 + 1] = mfma_kb<T>(vf[1], mf, o[d2 + 1]);
       o[d2] = mfma_kb<T>(vf[0], lf, o[d2]);
       o[d2 + 1] = mfma_kb<T>(vf[1], lf, o[d2 + 1]);
     }
@@ -618,7 +623,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
       return;
     }
     const int64_t base = part_slot(a, b, h, unit, nq) + q0;
-    for (int i = tid; i < mine * (HD / 4); i += 256) {
+    int first = tid;
+    asm volatile("" : "+v"(first));  // what follows from it takes no registers of the chunks' loop
+    for (int i = first; i < mine * (HD / 4); i += 256) {
       const int q = i / (HD / 4), d = i % (HD / 4) * 4;
       float M = -CH_INF, L = 0.f;
       f32x4 O = f32x4{0.f, 0.f, 0.f, 0.f};
