@@ -417,7 +417,11 @@ chimera_status chimera_kv4_read(const chimera_kv4* cache, int32_t dtype, const i
  * sequence b; head h reads the cache's head h / (n_heads / cache->n_heads).
  * n_b[b] tokens are committed; node u's own K and V lie at position n_b[b] + u.
  * It sees positions 0 .. n_b[b] - 1 and those of its ancestors and itself:
- * out = softmax(scale q K^T) V over them, in float32, rounded once.
+ * out = softmax(scale q K^T) V over them, in float32, rounded once.  A score whose
+ * q K^T, or scale times it in base 2, passes 2^128 is an infinity: a negative one
+ * weighs nothing, a row with a positive one or with nothing else becomes NaN.  V is
+ * summed before the division by the weights' sum, so rows become infinite or NaN
+ * where the sum of its magnitudes passes 2^128.  |scale| is at most 2^127.
  * parent (host, n_nodes entries, nullable): the tree, parent[0] = -1 and a
  * parent before its child, at most 15 levels below the root; NULL is a chain.
  * n_b[b] < 0 marks an empty place in the batch: its rows become zeros.  Positions

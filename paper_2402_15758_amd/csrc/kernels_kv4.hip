@@ -247,7 +247,10 @@ __device__ __forceinline__ int2 ld_tr16(const void* p) {
 // One chunk's scores become weights and its (m, l).  s: S^T, lane (g, c16) holding
 // query c16 and keys 16 kb + 4 g + r.  vis: the chunk's keys that the query sees;
 // ALL: every key, for every query of the wave (the masked path computes the same
-// values then).  scale2 >= 0.
+// values then).  scale2 >= 0.  A scaled score past the float's range is an infinity:
+// a chunk of nothing but negative ones (UNKNOWN, l == 1) counts for nothing next to
+// any other score, a positive one makes the row NaN.
+constexpr float UNKNOWN = -__FLT_MAX__;  // the maximum of scores of -inf
 template <bool ALL>
 __device__ __forceinline__ void chunk_weights(f32x4 (&s)[4], float scale2, uint64_t vis, int g, float& m, float& l) {
   const uint64_t mine = ALL ? 0 : vis >> (4 * g);
@@ -257,7 +260,7 @@ __device__ __forceinline__ void chunk_weights(f32x4 (&s)[4], float scale2, uint6
 #pragma unroll
     for (int r = 0; r < 4; ++r) mc = fmaxf(mc, ALL || ((mine >> (16 * kb + r)) & 1) ? s[kb][r] : -CH_INF);
   mc = rows_max(mc);
-  m = ALL || vis != 0 ? mc * scale2 : -CH_INF;
+  m = ALL || vis != 0 ? fmaxf(mc * scale2, UNKNOWN) : -CH_INF;
   float ls = 0.f;
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
@@ -269,6 +272,10 @@ __device__ __forceinline__ void chunk_weights(f32x4 (&s)[4], float scale2, uint6
       ls = ls + p;
     }
   l = rows_sum(ls);
+  if (__ballot(fabsf(m) >= __FLT_MAX__) != 0) {
+    l = m == UNKNOWN ? l + 1.f : l;
+    l = m == CH_INF ? __builtin_nanf("") : l;
+  }
 }
 
 // O^T += V^T P^T over the 32 keys of half kp, staged as rows v.  A weight enters
@@ -396,6 +403,7 @@ __device__ __forceinline__ void window_query(const Kv4AttnArgs& a, int b, int u,
   const float alpha = __ballot(valid) != 0 ? exp2_from(m, mn) : 1.f;
   const float pe = valid ? __builtin_amdgcn_exp2f(s - mn) : 0.f;
   l = l * alpha + wave_sum(sub == 0 ? pe : 0.f);
+  if (mn == UNKNOWN) l = __builtin_nanf("");  // nothing but scores of -inf
   if (!valid) v.clear();
   sc = fp4_scale(v.s);
   float w[DQ];

@@ -253,7 +253,8 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
     REQUIRE(ldq * es % 16 == 0, CHIMERA_EINVAL, "rows of q must start at multiples of 16 bytes");
     check_aligned(q, "q");
     check_aligned(ws, "workspace");
-    REQUIRE(std::isfinite(scale), CHIMERA_EINVAL, "scale must be finite");
+    REQUIRE(std::isfinite(scale) && std::fabs(scale) <= 0x1p127f, CHIMERA_EINVAL,
+            "scale must be finite, at most 2^127 in magnitude");  // times log2(e) it still is
     Kv4AttnArgs a{};
     for (int u = 0; u < n_nodes; ++u) {
       const int p = parent ? parent[u] : u - 1;

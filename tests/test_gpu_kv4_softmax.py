@@ -1,6 +1,5 @@
 """The 4-bit attention's weights: their precision, and scores at the ends of the
 float's range."""
-import numpy as np
 import pytest
 import torch
 
@@ -80,3 +79,67 @@ def test_weights_keep_all_bits_of_a_float(hd, n, first, table):
     want = ((b - c) / (1 + b + c)).unsqueeze(1)
     tol = torch.finfo(torch.bfloat16).eps / 2 * want.abs() + 4 * 2.0 ** -23
     assert bool(((out - want).abs() <= tol).all()), float(((out - want).abs() / tol).max())
+
+
+def rows(n, low, high, dtype, seed):
+    """Keys whose score with queries() passes the float's range downwards (low)
+    or upwards (high), positions of them; the others have ordinary scores."""
+    g = torch.Generator().manual_seed(seed)
+    k, v = (torch.randn(n + 1, 1, 64, generator=g) for _ in range(2))
+    k[:, :, :32] = 0
+    k[low, :, 0], k[high, :, 0] = -6.0, 6.0
+    return k.to(dtype), v.to(dtype)
+
+
+def queries(first, dtype, seed):
+    q = torch.randn(8, 64, generator=torch.Generator().manual_seed(seed)) * 0.7
+    q[:, 0] = first
+    return q.to(dtype)
+
+
+def without(q, k, v, n, gone, scale):
+    """The formula over the keys that are not `gone` (fp4_ref's form and tolerance)."""
+    kv = torch.stack((k, v), 1)
+    k0 = kv.clone()
+    k0[:, 0, :, 0] = 0  # the others' share of the first dimension: nothing
+    q0 = q.clone()
+    q0[:, 0] = 0
+    gone = set(gone)
+    want, tol = R.attention(q0.view(1, 1, *q.shape), [k0], [n], [-1], scale, seen=lambda b, p: p not in gone)
+    return want[0, 0], tol[0, 0]
+
+
+# tokens, table, copies of the eight queries: one launch, groups, supers
+SIZES = [(200, 0, 1), (700, 0, 1), (1500, 200, 1), (18750, 0, 32)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,table,copies", SIZES)
+@pytest.mark.parametrize("first,scale", [(2.0 ** 127, 0.125), (2.0 ** 60, 2.0 ** 80), (-(2.0 ** 127), -0.125)])
+def test_scores_of_minus_infinity_weigh_nothing(dtype, n, table, copies, first, scale):
+    """A key, a chunk, several of them, a stretch up to the window and some of the
+    window's keys, whose score (or scaled score) is below the float's range."""
+    q = queries(first, dtype, 1)
+    if scale > 1:  # the others' scaled scores stay ordinary
+        q[:, 1:] = (q[:, 1:].float() * 2.0 ** -80).to(dtype)
+    for stretch in ([7], range(64), range(64, 128), range(192), range(0, n - 15), range(n - 5, n - 2), range(3, n)):
+        low = list(stretch)
+        k, v = rows(n, low, [], dtype, n)
+        if scale < 0:
+            k[:, :, 0] = -k[:, :, 0].abs()  # q < 0 and scale < 0: the same scores
+        want, tol = without(q, k, v, n, low, scale)
+        out = Filled(k, v, table=table).attend(q.repeat(copies, 1), n, scale).double().view(copies, 8, 64)
+        assert bool(((out - want).abs() <= tol + 1e-30).all()), (low[0], len(low))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,table,copies", SIZES)
+@pytest.mark.parametrize("first,scale", [(2.0 ** 127, 0.125), (2.0 ** 60, 2.0 ** 80)])
+def test_scores_past_the_range_are_never_dropped_in_silence(dtype, n, table, copies, first, scale):
+    """A positive one, or nothing but negative ones: NaN."""
+    q = queries(first, dtype, 2)
+    for low, high in (([], [5]), ([], range(64)), (range(64), [70]), ([], [n - 3]), (range(n + 1), []),
+                      (range(n - 20), range(n - 20, n + 1)), (range(200), range(100, 101))):
+        k, v = rows(n, list(low), list(high), dtype, n)
+        out = Filled(k, v, table=table).attend(q.repeat(copies, 1), n, scale)
+        assert bool(torch.isnan(out).all()), (len(low), len(high))
