@@ -360,7 +360,9 @@ chimera_status chimera_gemm_static(int32_t dtype, const void* x, const void* w, 
  * says otherwise; the stream must belong to it (CHIMERA_EINVAL).  The calls
  * only enqueue kernels: they allocate nothing, do not synchronise, and may be
  * captured into a HIP graph.  A workspace is scratch of one call: calls that
- * may run at the same time (other streams, other graphs) need their own. */
+ * may run at the same time (other streams, other graphs) need their own.  The
+ * size a query names also holds for calls of fewer rows (chimera_gemm_fp4), and
+ * of fewer nodes or sequences (chimera_kv4_attn), all else the same. */
 
 /* A K x N matrix packed for chimera_gemm_fp4: N a multiple of 16, K of 32, both
  * at most 2^20.

@@ -175,6 +175,7 @@ struct Kv4AttnArgs {
   float* part_ml;           // [B][H][units][N Hq / H][2]
   Kv4Tree tree;
 };
+constexpr int KV4_SUPER_WGS = 256;  // blocks x supers from which on supers are dealt, not groups
 // Blocks of 16 queries of all sequences and cache heads; slots for partials of
 // a sequence and cache head over positions 0 .. cap - 1; bytes of all partials.
 int kv4_attn_blocks(int B, int Hq, int H, int N);

@@ -123,7 +123,6 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(const Kv4View c, const 
 // ---------------------------------------------------------------------------
 constexpr int CHUNK = 64, WIN = 16, FAN = 4;
 constexpr int GROUP = FAN * CHUNK, SUPER = FAN * GROUP;  // positions
-constexpr int SUPER_WGS = 256;
 static_assert(WIN == KV4_MAX_DEPTH + 1, "the window holds every position of a tree");
 
 // Depth of a lane's node.
@@ -174,7 +173,7 @@ __device__ __forceinline__ f32x4 fold_value(f32x4 o, float x, f32x4 o2, float y)
 // 15.0 us and a window of 7.1; as 1024 groups 14.2 and 18.3).  blocks: B x H x
 // blocks of 16 queries.
 __host__ __device__ __forceinline__ bool kv4_supers(int maxk, int blocks) {
-  return (int64_t)blocks * (maxk / SUPER + 1) >= SUPER_WGS;
+  return (int64_t)blocks * (maxk / SUPER + 1) >= KV4_SUPER_WGS;
 }
 
 // A lane's quarter of a row: dimensions HD/4 g .. HD/4 (g + 1) - 1, eight codes
@@ -827,9 +826,9 @@ void launch_kv4_expand(int dtype, const Kv4View& c, const PrefillChunk& chunk, v
 int kv4_attn_blocks(int B, int Hq, int H, int N) { return B * H * ((N * (Hq / H) + 15) / 16); }
 
 int kv4_attn_units(int64_t cap, int blocks) {
-  // groups are left only by sequences of fewer than SUPER_WGS / blocks supers
+  // groups are left only by sequences of fewer than KV4_SUPER_WGS / blocks supers
   const int64_t supers = (cap + SUPER - 1) / SUPER, groups = (cap + GROUP - 1) / GROUP;
-  return (int)std::max(supers, std::min<int64_t>(groups, FAN * (int64_t)((SUPER_WGS + blocks - 1) / blocks)));
+  return (int)std::max(supers, std::min<int64_t>(groups, FAN * (int64_t)((KV4_SUPER_WGS + blocks - 1) / blocks)));
 }
 
 bool kv4_attn_one(int64_t cap) { return cap <= GROUP; }

@@ -44,6 +44,7 @@ void check_matrix(int32_t N, int32_t K) {
 struct GemmWs {
   int64_t x = 0, w = 0, part = 0;
   bool rows;  // x is read where it lies
+  int64_t bytes() const { return x + w + part; }
 };
 GemmWs gemm_ws(int32_t dtype, int32_t M, int32_t N, int32_t K, bool readable) {
   GemmWs s;
@@ -101,6 +102,16 @@ void check_rows(const chimera_kv4* c, int32_t dtype, const void* k, const void* 
   REQUIRE((int64_t)rows * c->n_heads * c->head_dim / 4 < (int64_t)1 << 38, CHIMERA_EINVAL, "too many rows");
 }
 
+void check_queries(const chimera_kv4* c, int32_t n_heads, int32_t n_nodes) {
+  check_cache(c);
+  REQUIRE(n_heads >= 1 && n_heads <= 1024 && n_heads % c->n_heads == 0, CHIMERA_EINVAL,
+          "n_heads must be a multiple of the cache's heads, at most 1024");
+  REQUIRE(n_nodes >= 1 && n_nodes <= 64, CHIMERA_EINVAL, "n_nodes in [1, 64]");
+}
+int64_t attn_bytes(const chimera_kv4* c, int batch, int32_t n_heads, int32_t n_nodes) {
+  return kv4_attn_bytes(batch, (int64_t)c->max_pages * c->page_size, n_heads, c->n_heads, c->head_dim, n_nodes);
+}
+
 }  // namespace
 
 extern "C" {
@@ -148,8 +159,9 @@ chimera_status chimera_gemm_fp4_bytes(int32_t dtype, int32_t M, int32_t N, int32
     check_dtype(dtype);
     REQUIRE(M >= 1 && M <= FP4_MAX_ROWS, CHIMERA_EINVAL, "M in [1, 4096]");
     check_matrix(N, K);
-    const GemmWs s = gemm_ws(dtype, M, N, K, false);
-    *bytes = s.x + s.w + s.part;
+    // fewer rows may leave more partials, where the more run on a kernel that sums them
+    *bytes = 0;
+    for (int m = 1; m <= M; ++m) *bytes = std::max(*bytes, gemm_ws(dtype, m, N, K, false).bytes());
   });
 }
 
@@ -165,8 +177,8 @@ chimera_status chimera_gemm_fp4(int32_t dtype, const void* x, int64_t ldx, const
     const int64_t es = (int64_t)esize(dtype);
     const bool readable = ((uintptr_t)x & 15) == 0 && (M == 1 || ldx * es % 16 == 0);
     const GemmWs s = gemm_ws(dtype, M, N, K, readable);
-    REQUIRE(s.x + s.w + s.part == 0 || ws != nullptr, CHIMERA_EINVAL, "null workspace");
-    REQUIRE(ws_bytes >= s.x + s.w + s.part, CHIMERA_ENOMEM, "workspace too small");
+    REQUIRE(s.bytes() == 0 || ws != nullptr, CHIMERA_EINVAL, "null workspace");
+    REQUIRE(ws_bytes >= s.bytes(), CHIMERA_ENOMEM, "workspace too small");
     check_aligned(ws, "workspace");
     hipStream_t st = check_stream(stream);
     char* base = (char*)ws;
@@ -229,13 +241,15 @@ chimera_status chimera_kv4_read(const chimera_kv4* cache, int32_t dtype, const i
 
 chimera_status chimera_kv4_attn_bytes(const chimera_kv4* cache, int32_t n_heads, int32_t n_nodes, int64_t* bytes) {
   return guard([&] {
-    check_cache(cache);
+    check_queries(cache, n_heads, n_nodes);
     REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
-    REQUIRE(n_heads >= 1 && n_heads <= 1024 && n_heads % cache->n_heads == 0, CHIMERA_EINVAL,
-            "n_heads must be a multiple of the cache's heads, at most 1024");
-    REQUIRE(n_nodes >= 1 && n_nodes <= 64, CHIMERA_EINVAL, "n_nodes in [1, 64]");
-    *bytes = kv4_attn_bytes(cache->batch, (int64_t)cache->max_pages * cache->page_size, n_heads, cache->n_heads,
-                            cache->head_dim, n_nodes);
+    // Fewer queries may leave groups where more leave supers (kv4_attn_units), until
+    // a batch has a workgroup's worth of blocks for every super; then its size rules.
+    const int B = cache->batch;
+    *bytes = 0;
+    for (int n = 1; n <= n_nodes; ++n)
+      for (int b = 1; b <= B; b = b < KV4_SUPER_WGS || b == B ? b + 1 : B)
+        *bytes = std::max(*bytes, attn_bytes(cache, b, n_heads, n));
   });
 }
 
@@ -244,10 +258,9 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
                                 int64_t ldo, void* ws, int64_t ws_bytes, void* stream) {
   return guard([&] {
     check_dtype(dtype);
-    int64_t need = 0;
-    if (const chimera_status s = chimera_kv4_attn_bytes(cache, n_heads, n_nodes, &need)) throw Err(s, g_err);
+    check_queries(cache, n_heads, n_nodes);
     REQUIRE(q && n_b && out && ws, CHIMERA_EINVAL, "null argument");
-    REQUIRE(ws_bytes >= need, CHIMERA_ENOMEM, "workspace too small");
+    REQUIRE(ws_bytes >= attn_bytes(cache, cache->batch, n_heads, n_nodes), CHIMERA_ENOMEM, "workspace too small");
     const int64_t es = (int64_t)esize(dtype), width = (int64_t)n_heads * cache->head_dim;
     REQUIRE(ldq >= width && ldo >= width, CHIMERA_EINVAL, "row stride below n_heads * head_dim");
     REQUIRE(ldq * es % 16 == 0, CHIMERA_EINVAL, "rows of q must start at multiples of 16 bytes");
