@@ -216,8 +216,9 @@ typedef struct {
   int64_t steps;
   double ms_draft, ms_verify, ms_tail, ms_gemm_verify;  /* sums over the steps */
   int64_t gemm_verify_launches;
-  double gemm_verify_bytes; /* algorithmic bytes of those launches: weights + activations in/out */
-  double verify_bytes;      /* algorithmic bytes of the verify passes: weights, KV read and write */
+  /* algorithmic bytes, in 4-bit formats 17/32 of a byte a value (no padding of the packed layout, no unpacking) */
+  double gemm_verify_bytes; /* of those launches: weights + activations in/out */
+  double verify_bytes;      /* of the verify passes: weights, KV read and write */
   double ms_draft_median, ms_verify_median, ms_step_median; /* per-step medians (step: first to last stamp) */
 } chimera_profile;
 chimera_status chimera_profile_enable(chimera_ctx* ctx, int32_t enable);

@@ -611,11 +611,12 @@ void launch_gemm_fp4(int dtype, const GemmShape& s, const GemmEpi& e, int64_t ld
                      hipEvent_t ev_start, hipEvent_t ev_stop) {
   const Fp4Shape w4 = fp4_shape(s.N, s.K, s.splits);
   if (unpacked != nullptr) {
-    hipLaunchKernelGGL((fp4_unpack_kernel<bf16_t, false>), dim3(unit_blocks(w4)), dim3(256), 0, st,
-                       (const uint8_t*)s.W, w4, (bf16_t*)unpacked, (int64_t)0);
+    const Fp4Launch first{s, e, 0, w4, e.kind, st, ev_start, nullptr};  // the events span both launches
+    first.go(fp4_unpack_kernel<bf16_t, false>, dim3(unit_blocks(w4)), 256, 0, (const uint8_t*)s.W, w4,
+             (bf16_t*)unpacked, (int64_t)0);
     GemmShape u = s;
     u.W = unpacked;
-    (void)launch_gemm(dtype, u, e, st, ev_start, ev_stop);
+    (void)launch_gemm(dtype, u, e, st, nullptr, ev_stop);
     return;
   }
   const Fp4Route route = fp4_route(dtype, s.M, s.N, s.K, s.splits, e.kind, ldx);

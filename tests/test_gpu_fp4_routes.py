@@ -153,3 +153,26 @@ def test_engine_at_7b_width():
     s = Session(cfg, w, synth.TREES["T64"], max_batch=2, max_len=1024, **kw)
     assert s.generate(ps, 24)[0] == want
     s.close()
+
+
+def test_profiled_products_count_the_unpacking():
+    """640 verify rows at 7B width: with 4-bit weights the products' time holds the
+    unpacking (0.8 GB written over two layers, 0.1 ms at the card's peak rate next to
+    some 0.5 ms of products), which the same kernels over bf16 weights do not have."""
+    cfg = dataclasses.replace(synth.LLAMA7B, n_layers=2)
+    w = synth.make_weights(cfg, device="cuda")
+    ps = prompts([20] * 20, cfg.vocab, 7)
+    ms = {}
+    for fmt in ("fp4", "native"):
+        s = Session(cfg, w, synth.TREES["T32"], max_batch=20, max_len=128, weight_format=fmt)
+        s.set_graph(False)
+        s.profile(True)
+        s.prefill(ps)
+        times = []
+        for _ in range(8):
+            s.step()
+            times.append(s.profile_read().ms_gemm_verify)
+            s.profile(True)
+        ms[fmt] = sorted(times)[len(times) // 2]
+        s.close()
+    assert ms["fp4"] > ms["native"] + 0.08, ms
