@@ -25,6 +25,7 @@
 namespace {
 
 constexpr int DIES = 8;  // each with an L2 of its own
+constexpr int FP4_WGS = 256;  // a workgroup a CU
 
 // Where the units of a packed matrix lie.
 struct Fp4Shape {
@@ -352,7 +353,8 @@ __global__ __launch_bounds__(256) void gemm_fp4_kernel(const GemmShape sh, const
   }
 }
 
-constexpr int FP4_ROWS_BYTES = 112 << 10;
+constexpr int FP4_ROWS_BYTES = 112 << 10;     // rows of the kernel below, next to its sums in LDS
+constexpr int FP4_TWO_ROWS_BYTES = 47 << 10;  // with two workgroups on a CU
 
 // Split products of up to 16 rows whose sum nobody else finishes: a workgroup
 // owns one column block and the whole reduction, S slices of four waves (one a
@@ -360,7 +362,7 @@ constexpr int FP4_ROWS_BYTES = 112 << 10;
 // Its share is short (35 KB of 4096 x 16), a quarter of the bf16 kernels'.  The
 // rows are staged in LDS, only the ones there are; a thread's first pieces are
 // requested before its weights, since loads return in order and the weights
-// need not be waited for there.  One row of 4096 x 4096 4.5 us with its launch in a
+// need not be waited for there.  One row of 4096 x 4096 5.4 us with its launch in a
 // graph (floor 1.7): a start, a round trip for rows and weights and two barriers.
 template <typename T, int S, bool RM>
 __global__ __launch_bounds__(256 * S) void gemm_fp4_whole_kernel(const GemmShape sh, const GemmEpi e, int64_t ldx,
@@ -444,21 +446,34 @@ __global__ __launch_bounds__(256 * S) void gemm_fp4_whole_kernel(const GemmShape
 // FP4_WHOLE: the kernel above, where the rows fit LDS.  FP4_ROWS: blocks of rows
 // read where they lie (at most 32).  FP4_BLOCKS: from tiles.
 enum Fp4Route { FP4_BLOCKS, FP4_ROWS, FP4_WHOLE };
+// Whether a workgroup a column block is the faster form of such a product, against
+// the slices in workgroups of their own and a finishing launch.  The first takes as
+// long as K weights and M K activations take through one CU, whatever N; the second
+// 1.2 us longer to start, and then K N through all CUs.  So up to a column block a CU
+// the first wins where K (A + B M - N) stays below C; past that, with a second
+// block's rows beside the first's in LDS, where K (A + M) stays below C N.  The
+// constants fit 1800 measured sizes (N 16 to 8176, K 1024 to 57344, 1 to 16 rows,
+// weights from memory, calls in a graph), where the form taken is 0.2% (bf16) and
+// 0.4% (fp32) slower than the better one on average and 8% and 21% at most.  bf16,
+// us, workgroup a block / slices: 1 row of 2048 x 256 3.5 / 3.9, 4096 x 256 5.0 / 4.5,
+// 4096 x 4096 5.4 / 6.8, 8192 x 2048 6.7 / 6.6, 28672 x 4096 17.2 / 17.1, 57344 x 4096
+// 30.7 / 26.5, 8192 x 5120 8.9 / 9.7, 13824 x 5120 14.2 / 12.3; 16 rows of 1024 x 2048
+// 4.2 / 4.9, 2560 x 2048 6.6 / 6.2; 4 rows of 8192 x 5120 (one block's rows) 15.9 / 9.8.
+bool fp4_whole_pays(int dtype, int64_t M, int64_t N, int64_t K) {
+  const bool bf = dtype == DT_BF16;
+  const int64_t bytes = M * K * (bf ? 2 : 4);
+  if (N <= 16 * FP4_WGS) {
+    if (bytes > FP4_ROWS_BYTES) return false;
+    return bf ? K * (3000 + 200 * M - N) < 10000000 && K <= 8 * N + 2048 : K * (3400 + 250 * M - N) < 4000000;
+  }
+  return bytes <= FP4_TWO_ROWS_BYTES && (bf ? K * (2 + M) < 7 * N : K * (4 + M) < 2 * N);
+}
 Fp4Route fp4_route(int dtype, int M, int N, int K, int splits, int kind, int64_t ldx) {
-  // A workgroup's weights, 8.5 K bytes, come through one CU, and column blocks
-  // past one a CU wait for a second round.  One row, us, against the slices in
-  // workgroups of their own and a finishing launch (both kernels, without the gap
-  // between): 4096 x 4096 5.6 / 7.5, 11008 x 4096 9.2 / 11.6, 4096 x 1024 5.3 /
-  // 5.8, 13824 x 5120 13.8 / 14.7; 13824 x 256 7.4 / 5.8 (the launch saved is worth
-  // 2.5 us of the host's time), 13824 x 8176, four rows, 27.8 / 20.9.
-  const int64_t bytes = (int64_t)M * K * (dtype == DT_BF16 ? 2 : 4);
-  if (M <= 16 && splits > 1 && kind == EPI_F32 && bytes <= FP4_ROWS_BYTES && K <= 14336 && N / 16 <= 384)
-    return FP4_WHOLE;
+  if (M <= 16 && splits > 1 && kind == EPI_F32 && fp4_whole_pays(dtype, M, N, K)) return FP4_WHOLE;
   return ldx > 0 ? FP4_ROWS : FP4_BLOCKS;
 }
 
 constexpr int FP4_CB_MAX = 8;
-constexpr int FP4_WGS = 256;
 
 // Column runs of a slice: FP4_WGS workgroups' worth, at most FP4_CB_MAX blocks
 // long; the first `big` runs have `run` blocks, the others one less.

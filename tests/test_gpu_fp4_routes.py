@@ -176,3 +176,29 @@ def test_profiled_products_count_the_unpacking():
         ms[fmt] = sorted(times)[len(times) // 2]
         s.close()
     assert ms["fp4"] > ms["native"] + 0.08, ms
+
+
+@pytest.mark.parametrize("dtype,N,K", [("bf16", 4096, 7168), ("bf16", 4096, 34816), ("bf16", 8176, 1536),
+                                       ("bf16", 5120, 4096), ("bf16", 2048, 8192), ("bf16", 16, 4096),
+                                       ("bf16", 16, 2048), ("f32", 4096, 7168), ("f32", 256, 1024),
+                                       ("f32", 4112, 1024)])
+def test_a_workgroup_a_column_block_has_the_bits_of_slices(dtype, N, K):
+    """Row counts on both sides of the choice (8 and 4 rows of 7168 values are the
+    most that LDS holds), with and without room between the rows."""
+    g = torch.Generator().manual_seed(K)
+    t = R.TYPES[dtype]
+    big = torch.randn(17, K + 8, generator=g).to(t).cuda()
+    w = weights(K, N, dtype, 5)
+    p = pack(w.cuda(), dtype)
+    d = 1 if dtype == "bf16" else 0
+    for src in (big[:, :K].contiguous(), big[:, :K]):
+        ref = None
+        for M in (17, 16, 12, 9, 8, 7, 5, 4, 3, 2, 1):
+            need = B.chimera_gemm_fp4_bytes(d, M, N, K)
+            ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+            y = torch.full((M + 1, N), 123.0, device="cuda")
+            B.chimera_gemm_fp4(d, src.data_ptr(), src.stride(0), p.data_ptr(), M, N, K, y.data_ptr(), N, ws.data_ptr(),
+                               need, stream())
+            ref = y[:M].clone() if ref is None else ref
+            assert torch.equal(y[:M], ref[:M]) and bool((y[M] == 123).all()), M
+    check_product(big[:, :K].cpu(), w, ref)
