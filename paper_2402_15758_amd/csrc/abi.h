@@ -9,7 +9,8 @@
 
 #include "chimera.h"
 
-extern thread_local std::string g_err;
+// The library's own: a program or another library may have a g_err too.
+extern thread_local __attribute__((visibility("hidden"))) std::string g_err;
 
 namespace {
 

@@ -1,4 +1,7 @@
 """The 4-bit operators' limits and sizes, on the host: nothing is launched."""
+import subprocess
+
+import numpy as np
 import pytest
 
 from paper_2402_15758_amd import binding as B
@@ -52,10 +55,16 @@ def test_an_attentions_workspace_holds_for_fewer_queries(H, Hq, pages, page):
         assert n == 1 or ws >= size[b, n - 1]
         assert b == 1 or ws >= size[batches[batches.index(b) - 1], n]
     tree = [-1] + [0] * 63
-    import numpy as np
     for top_b, top_n in ((8, 49), (9, 64), (300, 33), (1, 64)):
         for b in range(1, top_b + 1):
             for n in (1, 2, 15, 16, 17, 32, 33, 48, 49, 64):
                 if n <= top_n:
                     size_passes(B.CHIMERA_EINVAL, (b, n), B.chimera_kv4_attn, c(b), 1, P + 2, w, P, Hq,
                                 np.array(tree[:n], dtype=np.int32), n, 0.1, P, w, P, size[top_b, top_n], None)
+
+
+def test_the_error_message_is_the_librarys_own():
+    """Its name is none that a program or another library could take over."""
+    names = subprocess.run(["nm", "-D", "--defined-only", B.LIB_PATH], capture_output=True, text=True,
+                           check=True).stdout
+    assert "chimera_last_error" in names and "g_err" not in names
