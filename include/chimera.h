@@ -51,8 +51,9 @@ typedef enum {
 typedef enum { CHIMERA_F32 = 0, CHIMERA_BF16 = 1 } chimera_dtype;
 /* Added to chimera_config.dtype: the target layers' matrices (wq .. w_down) are
  * rounded to the 4-bit format of the 4-bit operators below as they are loaded
- * (groups along d_in) and held in it, 17/64 of their bytes in bf16.  Tensors are
- * given as without it; embeddings, the LM head and the draft keep the dtype.  A
+ * (groups along d_in) and held in it, 17/64 of their bytes in bf16 and the packed
+ * layout's padding (2.6% more at the 7B and 13B shapes).  Tensors are given as
+ * without it; embeddings, the LM head and the draft keep the dtype.  A
  * bf16 model has the bits of the same model loaded with the rounded matrices. */
 enum { CHIMERA_WEIGHTS_FP4 = 0x100 };
 
@@ -115,7 +116,9 @@ chimera_status chimera_kv_create(chimera_model* m, int32_t max_batch, int32_t ma
  * operators below): each layer is a 4-bit paged cache of its own, 17/64 of the
  * bytes in bf16, and one layer's K and V as values, which prefill attention
  * reads.  Every position's K and V are rounded as they are written, in prefill
- * and in steps, so the model is the one whose attention reads those values;
+ * and in steps, so the model is the one whose attention reads those values.
+ * Prefill sums its attention in another order than steps do, so a token's bits may
+ * depend on which of the two it went through;
  * everything else is as with chimera_kv_create (greedy verification is lossless
  * against greedy decoding over the same kind of cache).  chimera_kv_read gives
  * the values held.  The compaction check refuses such a cache
@@ -368,7 +371,9 @@ chimera_status chimera_gemm_static(int32_t dtype, const void* x, const void* w, 
 /* A K x N matrix packed for chimera_gemm_fp4: N a multiple of 16, K of 32, both
  * at most 2^20.
  * w is row-major [K][ldw] of `dtype`, ldw >= N, at any element; `packed` is
- * 16-byte aligned, chimera_fp4_bytes long, its layout the library's own.
+ * 16-byte aligned, chimera_fp4_bytes long, its layout the library's own: 17/32 of a
+ * byte a value, padded where a slice of the reduction is no multiple of 512 values
+ * (4096 x 4096 not at all, 11008 x 4096 by 12%, K = 256 to twice that).
  * chimera_fp4_unpack writes the values that `packed` stands for, rounded to
  * `dtype` (bf16: exactly). */
 chimera_status chimera_fp4_bytes(int32_t N, int32_t K, int64_t* bytes);

@@ -12,6 +12,9 @@
 // the class, kb = kps s + w + 4 (4 q + i).  Lane l's 16 bytes are the words of
 // k-blocks i = 0..3, each with k = 32 kb + 8 (l >> 4) + 0..7 of column 16 c +
 // (l & 15): 1 KiB contiguous a load.  Its scales are 64 bytes, four (i) a column.
+// A class's last quad is whole too, and its padding (zeros) is stored and streamed:
+// nothing where a slice is a multiple of 512 values, 12% at 11008 x 4096 (four slices
+// of 86 k-blocks), 20% at 5120 x 5120, 4% at 13824 x 5120, 100% at K = 256.
 #include <hip/hip_ext.h>
 
 #include <algorithm>
@@ -61,7 +64,9 @@ __device__ __forceinline__ Fp4Src fp4_source(int kind, int c, int cl, int H, int
   return {0, 16 * c + cl};
 }
 
-// One wave a unit; a group's 32 values lie in the four lanes of a column.
+// One wave a unit; a group's 32 values lie in the four lanes of a column.  A lane
+// reads an element of each of its rows, 16 columns of a row side by side: 4096 x
+// 22016 of bf16 62 us, 3.7 TB/s; weights are packed once.
 template <typename T>
 __global__ __launch_bounds__(256) void fp4_pack_kernel(const T* __restrict__ s0, const T* __restrict__ s1,
                                                        const T* __restrict__ s2, int64_t ldw, int kind, int H, int hd,
@@ -96,8 +101,9 @@ __global__ __launch_bounds__(256) void fp4_pack_kernel(const T* __restrict__ s0,
   if (lane < 16) reinterpret_cast<uint32_t*>(dst + sh.codes_bytes + unit * 64)[lane] = sc;
 }
 
-// The values: row-major [K][N] (ROWS), or bf16 in the layout of the bf16
-// kernels (kernels_gemm.hip), N rounded up to whole 64-column groups.
+// The values: row-major [K][N] (ROWS; 4096 x 22016 96 us, stores of 16 columns a
+// row), or bf16 in the layout of the bf16 kernels (kernels_gemm.hip; N a multiple of
+// 64).
 template <typename T, bool ROWS>
 __global__ __launch_bounds__(256) void fp4_unpack_kernel(const uint8_t* __restrict__ src, const Fp4Shape sh,
                                                          T* __restrict__ dst, int64_t ldw) {
@@ -323,10 +329,11 @@ __device__ __forceinline__ void fp4_run(const GemmShape& sh, const GemmEpi& e, i
 //
 // A quad of weights (1 KiB of codes a wave) is requested while the quad before it is
 // converted, straight from memory: nothing of W is read twice by a workgroup.  Up
-// to 16 rows it is bound by that stream (1 row of 22016 x 4096 12.4 us, 3.9 TB/s);
-// from 64 rows on by each CU's intake of its activations (64 rows of 12288 x 4096
-// 15.8 us, 22016 x 4096 20), which longer runs of columns would take in less often
-// but do not fit the registers with.
+// to 16 rows it is bound by that stream (1 row of 4096 x 22016 11.7 us, 4.1 TB/s);
+// from 64 rows on by each CU's intake of its activations (64 rows of 4096 x 22016
+// 23.5 us, of 4096 x 12288 with their tiling 18.4; 2.5 TB/s of memory, the MFMA busy
+// 16% and the VALU 12% of the time), which longer runs of columns would take in less
+// often but do not fit the registers with.
 template <typename T, int MB, int CBA, bool RM>
 __global__ __launch_bounds__(256) void gemm_fp4_kernel(const GemmShape sh, const GemmEpi e, int64_t ldx,
                                                        const Fp4Shape w4, int kind, int nbig, int mapped) {

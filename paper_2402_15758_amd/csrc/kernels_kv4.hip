@@ -43,7 +43,7 @@ __device__ __forceinline__ int64_t piece_offset(const Kv4View& c, int64_t base, 
 
 // Rows into the cache: grid (pieces of a row, rows), the four threads of a group
 // agree on its scale.  Bound by the launch for a step's rows (64 rows of 32 heads
-// of 128: 3.0 us) and by bytes for a prompt's (2044 rows: 12.3 us, 4.2 TB/s).
+// of 128: 3.0 us) and by bytes for a prompt's (2044 rows: 42 MB in 12.2 us, 3.5 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const T* __restrict__ k,
                                                          const T* __restrict__ v, int64_t ld,
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const 
   }
 }
 
-// Rows out, as values (the same rows: 2.9 and 12.1 us).
+// Rows out, as values (the same rows: 3.0 and 11.8 us).
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T* __restrict__ k, T* __restrict__ v,
                                                        int64_t ld, const int* __restrict__ seq,
@@ -170,7 +170,7 @@ __device__ __forceinline__ f32x4 fold_value(f32x4 o, float x, f32x4 o2, float y)
 
 // Whether a sequence's shared positions 0 .. maxk are dealt in supers: where
 // those alone give every CU a workgroup (32768 tokens, 8 cache heads, 256 of them:
-// 15.0 us and a window of 7.1; as 1024 groups 14.2 and 18.3).  blocks: B x H x
+// 15.8 us and a window of 7.3; as 1024 groups 14.2 and 18.3).  blocks: B x H x
 // blocks of 16 queries.
 __host__ __device__ __forceinline__ bool kv4_supers(int maxk, int blocks) {
   return (int64_t)blocks * (maxk / SUPER + 1) >= KV4_SUPER_WGS;
@@ -451,10 +451,11 @@ __device__ __forceinline__ int64_t part_slot(const Kv4AttnArgs& a, int b, int h,
 // query blocks of a workgroup sharing one conversion of V, with a barrier a
 // chunk, were slower: 64 nodes at 512 tokens 12.8 us against 8.0.
 //
-// Eight single queries of 1024 to 4096 tokens, 32 heads: 26 us, 3.4 TB/s of cache;
-// its loads alone take 21 us, and without them the conversions and the softmax
-// (485 instructions a chunk) 23.  One of 32768 tokens with 8 cache heads: 15 us, a
-// wave a SIMD and its chain of four chunks.
+// Eight single queries of 1024 to 4096 tokens, 32 heads: 28 us, 3.2 TB/s of cache.
+// Its loads alone took 21 us, and without them the conversions and the softmax (some
+// 520 VALU instructions a chunk) as long; over the pass the VALU is busy 31% and the
+// MFMA 12% of the time: chains of three waves a SIMD, ragged lengths.  One query of
+// 32768 tokens with 8 cache heads: 16 us, a wave a SIMD and its chain of four chunks.
 //
 // Workgroups are dealt to the eight dies round-robin, the first grid dimension
 // first: heads, whose work is equal, and a head's query blocks on the die whose
@@ -661,8 +662,9 @@ __device__ __forceinline__ void dma_1k(const float* src, float* lds) {
 // query.  The partials go straight to LDS, `batch` of them a round trip.  Unrolled
 // over registers, 32 of them were 27 KB of code and folds of dependent exponentials;
 // now the lanes find all factors at once and a short loop multiplies and adds (one
-// query of 32768 tokens, 32 partials: 12.4 -> 7.1 us).  Dependent round trips (n,
-// page, rows) bound it: 64 nodes of 32 heads 5.4 us, 8192 queries 12.
+// query of 32768 tokens, 32 partials: 12.4 -> 7.3 us).  Dependent round trips (n,
+// page, rows) bound it: 64 nodes of 32 heads 5.8 us, 8192 queries 12.2 (the VALU busy
+// 16% and 46% of the time).
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_window(const Kv4AttnArgs a, int batch) {
   constexpr int DPL = HD / 64, LANES = HD / 4, PER = 64 / LANES;  // lanes of a partial, partials of a load
