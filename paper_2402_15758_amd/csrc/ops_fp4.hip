@@ -159,9 +159,10 @@ chimera_status chimera_gemm_fp4_bytes(int32_t dtype, int32_t M, int32_t N, int32
     check_dtype(dtype);
     REQUIRE(M >= 1 && M <= FP4_MAX_ROWS, CHIMERA_EINVAL, "M in [1, 4096]");
     check_matrix(N, K);
-    // fewer rows may leave more partials, where the more run on a kernel that sums them
-    *bytes = 0;
-    for (int m = 1; m <= M; ++m) *bytes = std::max(*bytes, gemm_ws(dtype, m, N, K, false).bytes());
+    // Fewer rows may leave more partials, where the more run on a kernel that sums
+    // them: the route changes with whole 64-row blocks, and grows within one.
+    *bytes = gemm_ws(dtype, M, N, K, false).bytes();
+    for (int m = (M - 1) / 64 * 64; m > 0; m -= 64) *bytes = std::max(*bytes, gemm_ws(dtype, m, N, K, false).bytes());
   });
 }
 
@@ -243,13 +244,18 @@ chimera_status chimera_kv4_attn_bytes(const chimera_kv4* cache, int32_t n_heads,
   return guard([&] {
     check_queries(cache, n_heads, n_nodes);
     REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
-    // Fewer queries may leave groups where more leave supers (kv4_attn_units), until
-    // a batch has a workgroup's worth of blocks for every super; then its size rules.
-    const int B = cache->batch;
+    // Fewer queries may leave groups where more leave supers: kv4_attn_units falls
+    // with ceil(KV4_SUPER_WGS / blocks), and the size grows where that stays.
     *bytes = 0;
-    for (int n = 1; n <= n_nodes; ++n)
-      for (int b = 1; b <= B; b = b < KV4_SUPER_WGS || b == B ? b + 1 : B)
+    for (int n = 1; n <= n_nodes; ++n) {
+      const int per = kv4_attn_blocks(1, n_heads, cache->n_heads, n);
+      if (n < n_nodes && kv4_attn_blocks(1, n_heads, cache->n_heads, n + 1) == per) continue;
+      for (int b = cache->batch; b > 0;) {
         *bytes = std::max(*bytes, attn_bytes(cache, b, n_heads, n));
+        const int factor = (KV4_SUPER_WGS + b * per - 1) / (b * per);
+        b = std::min(b - 1, (KV4_SUPER_WGS - 1) / (per * factor));  // the most sequences with a larger one
+      }
+    }
   });
 }
 
