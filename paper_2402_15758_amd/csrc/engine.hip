@@ -300,7 +300,7 @@ struct Gemm {
   }
   // Partials that a run_layer launch of kind EPI_PARTIAL leaves.
   int layer_partials(int M, int N, int K, int x_mtiles) const {
-    return c->m->w4 && !gemm_fp4_unpacks(c->m->dt, M, N) ? fp4_splits(N, K) : gemm_partials(c->m->dt, M, N, K, x_mtiles);
+    return c->m->w4 && !gemm_fp4_unpacks(c->m->dt, M, N, K) ? fp4_splits(N, K) : gemm_partials(c->m->dt, M, N, K, x_mtiles);
   }
 
   void run(const void* X, int x_mtiles, int M, const void* W, int N, int K, GemmEpi e, int nb_off = 0,
@@ -332,7 +332,7 @@ struct Gemm {
     }
     // the kernels record the events at their own start and end
     if (w4) {
-      launch_gemm_fp4(c->m->dt, s, e, 0, gemm_fp4_unpacks(c->m->dt, M, N) ? c->w4_wide : nullptr, st,
+      launch_gemm_fp4(c->m->dt, s, e, 0, gemm_fp4_unpacks(c->m->dt, M, N, K) ? c->w4_wide : nullptr, st,
                       ev ? ev->a : nullptr, ev ? ev->b : nullptr);
       return;
     }
@@ -807,15 +807,22 @@ void carve_ctx(chimera_ctx* c, Arena& a) {
   auto layer_rows = [&](size_t M, int N, int Kd, int kind) {
     int64_t rows = gemm_partial_rows(m->dt, (int)M, N, Kd, kind);
     if (m->w4 && (kind == EPI_PARTIAL || fp4_splits(N, Kd) > 1)) {
-      const int64_t direct = gemm_fp4_unpacks(m->dt, (int)M, N) ? FP4_DIRECT_ROWS : (int64_t)M;
+      const int64_t direct = gemm_fp4_unpacks(m->dt, (int)M, N, Kd) ? gemm_fp4_direct_rows(N, Kd) : (int64_t)M;
       rows = std::max(rows, (int64_t)fp4_splits(N, Kd) * direct);
     }
     return rows;
   };
   c->parts = a.arr<float>(d * std::max(layer_rows(Px, (int)d, hdim, EPI_PARTIAL),
                                        layer_rows(Px, (int)d, (int)F, EPI_PARTIAL)));
-  if (m->w4 && gemm_fp4_unpacks(m->dt, (int)Px, (int)d))
-    c->w4_wide = a.take(d * std::max<size_t>(3 * hdim, 2 * F) * es);
+  size_t wide = 0;  // the largest matrix that a launch reads unpacked
+  auto unpacked = [&](size_t N, size_t Kd) {
+    if (m->w4 && gemm_fp4_unpacks(m->dt, (int)Px, (int)N, (int)Kd)) wide = std::max(wide, N * Kd);
+  };
+  unpacked(3 * hdim, d);
+  unpacked(d, hdim);
+  unpacked(2 * F, d);
+  unpacked(d, F);
+  if (wide > 0) c->w4_wide = a.take(wide * es);
   // split-K scratch: the most that a launch of this context leaves to a
   // finishing pass (partials are indexed with the full packed width)
   size_t scr = 1;

@@ -118,12 +118,18 @@ void launch_fp4_unpack_rows(int dtype, const void* packed, int N, int K, void* d
 // Row-major x [M][ldx] -> tiled.
 void launch_tile_strided(int dtype, const void* x, int64_t ldx, int M, int K, void* dst, int mtiles, hipStream_t st);
 // Whether launches of M rows run on the bf16 kernels over the unpacked matrix:
-// bf16, whole 64-column groups, more than FP4_DIRECT_ROWS rows.  Up to there the
-// weights are converted once a 64-row block, past it once, to memory (us, blocks /
-// unpacked; 4096 x 12288: 256 rows 37 / 55, 384 rows 55 / 73, 512 rows 73 / 75;
-// 4096 x 4096, 512 rows: 31 / 32).
-constexpr int FP4_DIRECT_ROWS = 512;
-bool gemm_fp4_unpacks(int dtype, int M, int N);
+// bf16, whole 64-column groups, more than gemm_fp4_direct_rows.  Up to there the
+// weights are converted once a 64-row block, past it once, to memory, which is a
+// launch more and 2.5 bytes a weight moved; what a small matrix leaves to the bf16
+// kernels does not fill the card.  us, blocks / unpacked (with the tiling, in a
+// graph), at 384, 448, 512, 640, 768 and 1024 rows: 4096 x 22016 110 / 115, 127 / 115,
+// 146 / 117, 190 / 155, 218 / 180, 294 / 196; 11008 x 4096 64 / 75, 79 / 78, 80 / 80,
+// 103 / 110, 120 / 114, 156 / 127; 4096 x 4096 36 / 39, 41 / 39, 42 / 42, 54 / 56, 62 /
+// 60, 82 / 68; 1024 x 8192 19 / 26, 22 / 27, 23 / 28, 29 / 33, 32 / 33, 43 / 36; 2048 x
+// 1024 17 / 22, 19 / 22, 19 / 22, 22 / 25, 25 / 27, 30 / 29; 2048 and 4096 rows of 256 x
+// 1024 12 / 13 and 24 / 17.
+int gemm_fp4_direct_rows(int N, int K);
+bool gemm_fp4_unpacks(int dtype, int M, int N, int K);
 // s.W: the packed matrix, s.splits = fp4_splits(N, K), all columns.  ldx > 0: X
 // is row-major (at most 32 rows, 16-byte aligned).  unpacked: room for the
 // bf16 matrix where gemm_fp4_unpacks, else nullptr.

@@ -651,4 +651,10 @@ void launch_gemm_fp4(int dtype, const GemmShape& s, const GemmEpi& e, int64_t ld
   if (finish) launch_gemm_finish(dtype, s, e, st, ev_stop);
 }
 
-bool gemm_fp4_unpacks(int dtype, int M, int N) { return dtype == DT_BF16 && N % 64 == 0 && M > FP4_DIRECT_ROWS; }
+int gemm_fp4_direct_rows(int N, int K) {
+  const int64_t weights = (int64_t)N * K;
+  return weights >= 12 << 20 ? 384 : (weights >= 1 << 20 ? 768 : 2048);
+}
+bool gemm_fp4_unpacks(int dtype, int M, int N, int K) {
+  return dtype == DT_BF16 && N % 64 == 0 && M > gemm_fp4_direct_rows(N, K);
+}

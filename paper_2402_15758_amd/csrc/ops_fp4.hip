@@ -49,7 +49,7 @@ struct GemmWs {
 GemmWs gemm_ws(int32_t dtype, int32_t M, int32_t N, int32_t K, bool readable) {
   GemmWs s;
   const int64_t es = (int64_t)esize(dtype);
-  const bool unpack = gemm_fp4_unpacks(dtype, M, N);
+  const bool unpack = gemm_fp4_unpacks(dtype, M, N, K);
   // A launch saved against reads of 64 bytes a row: at 64 rows 4096 x 22016 29.8 us
   // and 28.1 with the tiling launch, 4096 x 12288 22.0 and 20.0, 4096 x 4096 10.8
   // and 11.1.

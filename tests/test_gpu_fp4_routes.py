@@ -42,14 +42,17 @@ def product(x, p, N, K):
 
 
 def borders(N, K, top):
-    """Row counts where a launch takes another route: around 512 rows, and where more
-    rows need less (the kernel that sums the slices itself)."""
+    """Row counts where a launch takes another route: around those from which on the
+    matrix is unpacked, and where more rows need less (the kernel that sums the slices
+    itself)."""
     need = {M: least_workspace(1, M, N, K) for M in [*range(64, top + 1, 64), *range(65, top + 1, 64)]}
     drops = [M for M in range(65, top + 1, 64) if need[M] < need[M - 1]]
-    return sorted({512, 513, 600, top} | {M + i for M in drops for i in (-1, 0)})
+    near = [M for M in (384, 385, 512, 513, 600, 768, 769, 2048, 2049) if M <= top]
+    return sorted({*near, top} | {M + i for M in drops for i in (-1, 0)})
 
 
-@pytest.mark.parametrize("N,K", [(1024, 2048), (2048, 4096), (4096, 1024), (64, 1024), (48, 2048), (4096, 4096)])
+@pytest.mark.parametrize("N,K", [(1024, 2048), (2048, 4096), (4096, 1024), (64, 1024), (48, 2048), (4096, 4096),
+                                 (12288, 1024)])
 def test_many_rows_have_the_bits_of_one(N, K):
     top = 3000
     g = torch.Generator().manual_seed(N + K)
@@ -86,11 +89,11 @@ def test_many_rows_have_the_bits_of_the_bf16_product(N, K):
         assert torch.equal(product(x[:M], p, N, K), ref[:M]), M
 
 
-@pytest.mark.parametrize("lens,tree,batch", [([900, 40, 700, 513], "T64", 4), ([30 + 7 * i for i in range(20)], "T32", 20)])
-def test_engine_launches_past_512_rows_with_split_reductions(lens, tree, batch):
-    """Prefill chunks of over 512 rows, and a verify pass of 640, over unpacked
+@pytest.mark.parametrize("lens,tree,batch", [([900, 40, 700, 513], "T64", 4), ([30 + 7 * i for i in range(26)], "T32", 26)])
+def test_engine_unpacks_with_split_reductions(lens, tree, batch):
+    """Prefill chunks of over 768 rows, and a verify pass of 832, over unpacked
     matrices: the bits of the rounded model."""
-    cfg = dataclasses.replace(SMALL, d_model=1024, n_heads=8, d_ffn=4096, n_layers=2)
+    cfg = dataclasses.replace(SMALL, d_model=1280, n_heads=10, d_ffn=4096, n_layers=2)
     w = synth.make_weights(cfg, std=0.04)
     ps = prompts(lens, cfg.vocab, 5)
     outs = []
