@@ -459,9 +459,9 @@ enum Fp4Route { FP4_BLOCKS, FP4_ROWS, FP4_WHOLE };
 // 1.2 us longer to start, and then K N through all CUs.  So up to a column block a CU
 // the first wins where K (A + B M - N) stays below C; past that, with a second
 // block's rows beside the first's in LDS, where K (A + M) stays below C N.  The
-// constants fit 1800 measured sizes (N 16 to 8176, K 1024 to 57344, 1 to 16 rows,
+// constants fit 1534 measured sizes (N 16 to 8176, K 1024 to 57344, 1 to 16 rows,
 // weights from memory, calls in a graph), where the form taken is 0.2% (bf16) and
-// 0.4% (fp32) slower than the better one on average and 8% and 21% at most.  bf16,
+// 0.6% (fp32) slower than the better one on average and 9% and 21% at most.  bf16,
 // us, workgroup a block / slices: 1 row of 2048 x 256 3.5 / 3.9, 4096 x 256 5.0 / 4.5,
 // 4096 x 4096 5.4 / 6.8, 8192 x 2048 6.7 / 6.6, 28672 x 4096 17.2 / 17.1, 57344 x 4096
 // 30.7 / 26.5, 8192 x 5120 8.9 / 9.7, 13824 x 5120 14.2 / 12.3; 16 rows of 1024 x 2048
