@@ -444,6 +444,123 @@ chimera_status chimera_kv4_attn(const chimera_kv4* cache, int32_t dtype, const v
                                 int32_t n_heads, const int32_t* parent, int32_t n_nodes, float scale, void* out,
                                 int64_t ldo, void* ws, int64_t ws_bytes, void* stream);
 
+/* ---- a plain paged cache ------------------------------------------------------
+ * The operators of a decoding layer over a K/V cache of float32 or bf16 values,
+ * and the verification of drafted tokens by their probabilities.  The conventions
+ * of the 4-bit operators hold: device pointers of the current device unless a
+ * declaration says otherwise, kernels only enqueued, no allocation and no
+ * synchronisation, capturable; a workspace is scratch of one call, and its size
+ * holds for calls of fewer rows, sequences or nodes too, all else the same. */
+
+/* The cache (a host struct; a call copies it).  pool: 16-byte aligned,
+ * chimera_paged_bytes long, rows of head_dim values of `dtype` in the order
+ * [page][K | V][head][slot].  page_table (device, [batch][max_pages]): position p
+ * of sequence b lies in slot p % page_size of page page_table[b][p / page_size].
+ * Entries whose positions a call does not touch may hold anything; a page id
+ * outside 0 .. n_pages - 1 is a page that the cache does not have.  head_dim is 64
+ * or 128, page_size at most 256, a pool at most 2^31 rows. */
+typedef struct {
+  void* pool;
+  int64_t pool_bytes;
+  const int32_t* page_table;
+  int32_t batch, max_pages, n_pages, page_size, n_heads, head_dim;
+  int32_t dtype;
+} chimera_paged;
+chimera_status chimera_paged_bytes(int32_t n_pages, int32_t page_size, int32_t n_heads, int32_t head_dim, int32_t dtype,
+                                   int64_t* bytes);
+
+/* Rotary positions (a host struct).  The first rot_dim dimensions of a head turn,
+ * in pairs (i, i + rot_dim / 2) (CHIMERA_ROPE_HALF) or (2i, 2i + 1)
+ * (CHIMERA_ROPE_PAIRS); the others pass.  Pair i at position p turns by p theta_i,
+ * theta_i = base^(-2i / rot_dim), and is multiplied by gain.  For contexts past
+ * those a model was trained on: CHIMERA_ROPE_LINEAR divides theta by factor;
+ * CHIMERA_ROPE_RAMP multiplies it by w + (1 - w) / factor, w = clamp((t - low) /
+ * (high - low), 0, 1), t = original_positions theta / (2 pi) the turns within the
+ * original context.  A table of (cos, sin) for positions 0 .. max_positions - 1 is
+ * laid out once: chimera_rope_bytes long, 16-byte aligned, angles in 64 bits. */
+enum { CHIMERA_ROPE_HALF = 0, CHIMERA_ROPE_PAIRS = 1 };
+enum { CHIMERA_ROPE_NONE = 0, CHIMERA_ROPE_LINEAR = 1, CHIMERA_ROPE_RAMP = 2 };
+typedef struct {
+  int32_t rot_dim, layout, max_positions;
+  float base;
+  int32_t scaling;
+  float factor;
+  int32_t original_positions;
+  float low, high, gain;
+} chimera_rope;
+chimera_status chimera_rope_bytes(const chimera_rope* rope, int64_t* bytes);
+chimera_status chimera_rope_table(const chimera_rope* rope, void* table, int64_t table_bytes, void* stream);
+
+/* Rows into the cache.  Row r of q, k and v (r ld further on, at any element, heads
+ * of head_dim values of `dtype`) belongs to position pos[r] of sequence seq[r].
+ * Each head x of q and k becomes x (mean(x^2) + eps)^(-1/2) gain where q_gain or
+ * k_gain (float32 [head_dim], nullable) is given, then turns as `rope` says (NULL:
+ * not; `table`: what chimera_rope_table wrote for it), in float32, and is rounded
+ * once, to the cache's dtype: q into row r of q_out (ldo apart, at any element), k
+ * into the cache, and v as it is.  q NULL with n_heads 0 writes K and V alone.
+ * q_out may be q itself (same dtype and stride); other outputs must not overlap
+ * inputs.  A row whose sequence (-1 marks padding), position (within the table of
+ * the rotation, too) or page there is not is skipped, its row of q_out left as it
+ * was.  Rows of one call must name distinct slots: a slot named twice ends with a
+ * mixture of its rows. */
+chimera_status chimera_paged_append(const chimera_paged* cache, int32_t dtype, const void* q, const void* k, const void* v,
+                                    int64_t ld, int32_t n_heads, const int32_t* seq, const int32_t* pos, int32_t rows,
+                                    const chimera_rope* rope, const void* table, const float* q_gain,
+                                    const float* k_gain, float eps, void* q_out, int64_t ldo, void* stream);
+
+/* Attention of new tokens over the cache, causal.  Rows row0[b] .. row0[b + 1] - 1
+ * of q and out (row strides ldq, ldo; [n_heads][head_dim] of the cache's dtype) are
+ * sequence b's new tokens at positions n_b[b], n_b[b] + 1, ..., their own K and V in
+ * the cache already; row0 (device, [batch + 1], not decreasing, at most `rows`) may
+ * be NULL: rows == batch then, one row a sequence.  Rows outside row0[0] ..
+ * row0[batch] - 1 are left as they were.  Head h reads the cache's head h / (n_heads /
+ * cache->n_heads).  The row at position p sees positions 0 .. p; with window > 0 only
+ * those above p - window and the first `sinks`.  out = softmax(scale q K^T) V over
+ * them.
+ * Scores, softmax and sums are float32, the weights rounded once to bf16 where the
+ * cache is, the result rounded once.  A score whose q K^T, or scale times it in base 2, passes 2^128 is an infinity: a negative one
+ * weighs nothing, a row with a positive one or with nothing else becomes NaN.  |scale|
+ * is at most 2^127.  Positions that the cache does not have are not seen; a row that
+ * sees none becomes zeros, and so do the rows of a sequence whose n_b is negative.
+ * Nothing that a row does not see reaches it, infinities and NaN included.  n_b is at
+ * most 2^30.  q: rows at multiples of 16 bytes; out at any element; ws: 16-byte
+ * aligned, chimera_paged_attn_bytes long.  Equal calls give equal bits; a row's last
+ * bits may depend on the other rows of its call. */
+chimera_status chimera_paged_attn_bytes(const chimera_paged* cache, int32_t n_heads, int32_t rows, int64_t* bytes);
+chimera_status chimera_paged_attn(const chimera_paged* cache, const void* q, int64_t ldq, int32_t n_heads,
+                                  const int32_t* row0, const int32_t* n_b, int32_t rows, int32_t window, int32_t sinks,
+                                  float scale, void* out, int64_t ldo, void* ws, int64_t ws_bytes, void* stream);
+
+/* Drafted tokens verified against the target's probabilities, and the next token:
+ * sampling from the target at `temperature`, whatever was drafted.  tokens ([batch]
+ * [n_nodes]) are the nodes of a tree (parent: host, n_nodes entries, parent[0] = -1
+ * and a parent before its child; NULL: a chain); node 0 is the last committed token.
+ * Row b n_nodes + i of logits (ld apart, [vocab] of `dtype`) gives p = softmax(logits
+ * / temperature) of the token after node i.  u ([batch][n_nodes], in [0, 1)) are the
+ * random numbers: u[0] draws the next token, u[i] tests node i.
+ *  - draft NULL: the children of a node were chosen (the draft's best).  They are
+ *    tested in the order of their ids; child c is accepted where u[c] (1 - the mass of
+ *    the siblings rejected before it) < p(its token).  Where all are rejected the next
+ *    token comes from p without them, normalised.
+ *  - draft given, a chain: node i + 1's token was drawn from q = softmax(draft row i /
+ *    temperature).  It is accepted where u[i + 1] q(token) < p(token), else the next
+ *    token comes from max(p - q, 0), normalised.
+ * After a node without children it comes from p.  It is the least v for which the
+ * weights of 0 .. v add up to more than u[0] of their sum.  All of it is computed in
+ * 64 bits.  Results: n_new [batch] tokens, new_tokens [batch][K + 1] (K the tree's
+ * depth): the accepted ones in order of depth, then the next; path_nodes [batch][K +
+ * 1] (nullable): the accepted nodes from the root; entries past n_new are -1.
+ * A node whose token is not in 0 .. vocab - 1 is not there (padding of ragged trees),
+ * and a sequence whose node 0 is negative is an empty place: n_new 0.  A row on the
+ * path with a NaN, a +inf or nothing but -inf has no distribution: the walk ends
+ * there with the next token -1.  ws: 16-byte aligned, chimera_accept_bytes long
+ * (drawn: whether draft is given). */
+chimera_status chimera_accept_bytes(int32_t batch, int32_t n_nodes, int32_t vocab, int32_t drawn, int64_t* bytes);
+chimera_status chimera_accept(int32_t dtype, const void* logits, int64_t ld, const void* draft, int64_t ldd, int32_t vocab,
+                              const int32_t* tokens, const int32_t* parent, int32_t n_nodes, int32_t batch,
+                              float temperature, const double* u, int32_t* new_tokens, int32_t* n_new,
+                              int32_t* path_nodes, void* ws, int64_t ws_bytes, void* stream);
+
 const char* chimera_last_error(void);
 void chimera_ctx_free(chimera_ctx* ctx);
 void chimera_kv_free(chimera_kv* kv);

@@ -14,6 +14,8 @@ CHIMERA_WEIGHTS_FP4 = 0x100
 CHIMERA_DECODE_GREEDY, CHIMERA_DECODE_TYPICAL = 0, 1
 CHIMERA_DRAFT_CHAIN, CHIMERA_DRAFT_BRANCH = 0, 1
 DBG_VERIFY_LOGITS, DBG_DRAFT_LOGITS, DBG_TREE_TOKENS, DBG_DRAFT_LISTS, DBG_SEQ_LEN, DBG_TOKENS = range(6)
+CHIMERA_ROPE_HALF, CHIMERA_ROPE_PAIRS = 0, 1
+CHIMERA_ROPE_NONE, CHIMERA_ROPE_LINEAR, CHIMERA_ROPE_RAMP = 0, 1, 2
 CHIMERA_MAX_PIPELINED_STEPS = 64
 CHIMERA_OK, CHIMERA_EINVAL, CHIMERA_ENOMEM, CHIMERA_ECAPACITY, CHIMERA_EHIP, CHIMERA_ESTATE = 0, -1, -2, -3, -4, -5
 STATUS = {0: "OK", -1: "EINVAL", -2: "ENOMEM", -3: "ECAPACITY", -4: "EHIP", -5: "ESTATE"}
@@ -49,6 +51,20 @@ class chimera_kv4(ctypes.Structure):
     _fields_ = [("pool", ctypes.c_void_p), ("pool_bytes", ctypes.c_int64), ("page_table", ctypes.c_void_p),
                 ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class chimera_paged(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("pool_bytes", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class chimera_rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("max_positions", ctypes.c_int32),
+                ("base", ctypes.c_float), ("scaling", ctypes.c_int32), ("factor", ctypes.c_float),
+                ("original_positions", ctypes.c_int32), ("low", ctypes.c_float), ("high", ctypes.c_float),
+                ("gain", ctypes.c_float)]
 
 
 _lib = None
@@ -96,6 +112,16 @@ _PROTOS = {
     "chimera_kv4_append": [ctypes.POINTER(chimera_kv4), I32, P, P, I64, P, P, I32, P],
     "chimera_kv4_read": [ctypes.POINTER(chimera_kv4), I32, P, P, I32, P, P, I64, P],
     "chimera_kv4_attn_bytes": [ctypes.POINTER(chimera_kv4), I32, I32, PI64],
+    "chimera_paged_bytes": [I32, I32, I32, I32, I32, PI64],
+    "chimera_rope_bytes": [ctypes.POINTER(chimera_rope), PI64],
+    "chimera_rope_table": [ctypes.POINTER(chimera_rope), P, I64, P],
+    "chimera_paged_append": [ctypes.POINTER(chimera_paged), I32, P, P, P, I64, I32, P, P, I32,
+                             ctypes.POINTER(chimera_rope), P, P, P, ctypes.c_float, P, I64, P],
+    "chimera_paged_attn_bytes": [ctypes.POINTER(chimera_paged), I32, I32, PI64],
+    "chimera_paged_attn": [ctypes.POINTER(chimera_paged), P, I64, I32, P, P, I32, I32, I32, ctypes.c_float, P, I64, P,
+                           I64, P],
+    "chimera_accept_bytes": [I32, I32, I32, I32, PI64],
+    "chimera_accept": [I32, P, I64, P, I64, I32, P, P, I32, I32, ctypes.c_float, P, P, P, P, P, I64, P],
     "chimera_kv4_attn": [ctypes.POINTER(chimera_kv4), I32, P, I64, P, I32, P, I32, ctypes.c_float, P, I64, P, I64,
                          P],
 }
@@ -334,12 +360,70 @@ def chimera_kv4_attn_bytes(cache: chimera_kv4, n_heads: int, n_nodes: int) -> in
 def chimera_kv4_attn(cache: chimera_kv4, dtype: int, q_ptr: int, ldq: int, n_ptr: int, n_heads: int, parent,
                      n_nodes: int, scale: float, out_ptr: int, ldo: int, ws_ptr: int, ws_bytes: int, stream: int):
     """parent: a contiguous numpy int32 array of n_nodes entries, or None for a chain."""
-    if parent is not None:
-        if parent.shape != (n_nodes,) or parent.dtype != "int32" or not parent.flags.c_contiguous:
-            raise ValueError("parent is a contiguous int32 array of n_nodes entries")
-        parent = parent.__array_interface__["data"][0]
+    parent = _parent(parent, n_nodes)
     _check(lib().chimera_kv4_attn(ctypes.byref(cache), dtype, q_ptr, ldq, n_ptr, n_heads, parent, n_nodes, scale,
                                   out_ptr, ldo, ws_ptr, ws_bytes, stream))
+
+
+def _parent(parent, n_nodes: int):
+    if parent is None:
+        return None
+    if parent.shape != (n_nodes,) or parent.dtype != "int32" or not parent.flags.c_contiguous:
+        raise ValueError("parent is a contiguous int32 array of n_nodes entries")
+    return parent.__array_interface__["data"][0]
+
+
+def chimera_paged_bytes(n_pages: int, page_size: int, n_heads: int, head_dim: int, dtype: int) -> int:
+    out = I64()
+    _check(lib().chimera_paged_bytes(n_pages, page_size, n_heads, head_dim, dtype, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_rope_bytes(rope: chimera_rope) -> int:
+    out = I64()
+    _check(lib().chimera_rope_bytes(ctypes.byref(rope), ctypes.byref(out)))
+    return out.value
+
+
+def chimera_rope_table(rope: chimera_rope, table_ptr: int, table_bytes: int, stream: int):
+    _check(lib().chimera_rope_table(ctypes.byref(rope), table_ptr, table_bytes, stream))
+
+
+def chimera_paged_append(cache: chimera_paged, dtype: int, q_ptr, k_ptr: int, v_ptr: int, ld: int, n_heads: int,
+                         seq_ptr: int, pos_ptr: int, rows: int, rope, table_ptr, q_gain_ptr, k_gain_ptr, eps: float,
+                         q_out_ptr, ldo: int, stream: int):
+    """rope: a chimera_rope, or None for rows that do not turn (table_ptr None too)."""
+    _check(lib().chimera_paged_append(ctypes.byref(cache), dtype, q_ptr, k_ptr, v_ptr, ld, n_heads, seq_ptr, pos_ptr,
+                                      rows, None if rope is None else ctypes.byref(rope), table_ptr, q_gain_ptr,
+                                      k_gain_ptr, eps, q_out_ptr, ldo, stream))
+
+
+def chimera_paged_attn_bytes(cache: chimera_paged, n_heads: int, rows: int) -> int:
+    out = I64()
+    _check(lib().chimera_paged_attn_bytes(ctypes.byref(cache), n_heads, rows, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_paged_attn(cache: chimera_paged, q_ptr: int, ldq: int, n_heads: int, row0_ptr, n_ptr: int, rows: int,
+                       window: int, sinks: int, scale: float, out_ptr: int, ldo: int, ws_ptr, ws_bytes: int,
+                       stream: int):
+    _check(lib().chimera_paged_attn(ctypes.byref(cache), q_ptr, ldq, n_heads, row0_ptr, n_ptr, rows, window, sinks,
+                                    scale, out_ptr, ldo, ws_ptr, ws_bytes, stream))
+
+
+def chimera_accept_bytes(batch: int, n_nodes: int, vocab: int, drawn: bool) -> int:
+    out = I64()
+    _check(lib().chimera_accept_bytes(batch, n_nodes, vocab, 1 if drawn else 0, ctypes.byref(out)))
+    return out.value
+
+
+def chimera_accept(dtype: int, logits_ptr: int, ld: int, draft_ptr, ldd: int, vocab: int, tokens_ptr: int, parent,
+                   n_nodes: int, batch: int, temperature: float, u_ptr: int, new_tokens_ptr: int, n_new_ptr: int,
+                   path_nodes_ptr, ws_ptr: int, ws_bytes: int, stream: int):
+    """parent: a contiguous numpy int32 array of n_nodes entries, or None for a chain."""
+    _check(lib().chimera_accept(dtype, logits_ptr, ld, draft_ptr, ldd, vocab, tokens_ptr, _parent(parent, n_nodes),
+                                n_nodes, batch, temperature, u_ptr, new_tokens_ptr, n_new_ptr, path_nodes_ptr, ws_ptr,
+                                ws_bytes, stream))
 
 
 def chimera_ctx_free(ctx: int):

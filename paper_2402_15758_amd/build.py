@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libchimera.so")
 SOURCES = ["kernels_gemm_wide.hip", "kernels_gemm.hip", "kernels_gemm_rows.hip", "kernels_attn.hip", "kernels_misc.hip",
-           "kernels_fp4.hip", "kernels_kv4.hip", "ops_fp4.hip", "engine.hip"]
+           "kernels_fp4.hip", "kernels_kv4.hip", "ops_fp4.hip", "kernels_paged.hip", "kernels_paged_attn.hip",
+           "kernels_accept.hip", "ops_paged.hip", "engine.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,36 @@
+// Verification of drafted tokens by their probabilities (kernels_accept.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+// A tree of up to 64 nodes by value, a byte a parent (the root's: 0), as words that
+// scalar loads bring whole.
+struct AcceptTree {
+  uint32_t parent[16];
+  void set(int u, int p) { parent[u / 4] |= (uint32_t)(u == 0 ? 0 : p) << (8 * (u % 4)); }
+};
+
+struct AcceptArgs {
+  const void* logits;       // [B N][ld]
+  int64_t ld;
+  const void* draft;        // [B N][ldd], nullptr: the tokens were chosen
+  int64_t ldd;
+  const int* tokens;        // [B][N]
+  const double* u;          // [B][N]
+  int B, N, V, K;           // K: the tree's depth
+  double inv_T;
+  int* new_tokens;          // [B][K + 1]
+  int* n_new;               // [B]
+  int* path;                // [B][K + 1], nullptr: not wanted
+  int parts;                // of a row
+  // scratch: each part's maximum and sum of exp((z - maximum) inv_T), target rows
+  // then draft rows; the residual's parts
+  float* part_m;            // [2][B N][parts]
+  double* part_s;
+  double* resid;            // [B][parts]
+  AcceptTree tree;
+};
+constexpr int ACCEPT_PART = 4096;  // entries of a part
+int64_t accept_bytes(int B, int N, int V, bool drawn);
+void accept_carve(AcceptArgs& a, void* ws);
+void launch_accept(int dtype, const AcceptArgs& a, hipStream_t st);

@@ -1,0 +1,243 @@
+// Rows into a paged K/V cache (paged.h): queries and keys normalised head by head
+// and rotated by their position on the way, and the rotation's table.
+#include "common.h"
+#include "paged.h"
+
+namespace {
+
+// ---- the rotation's table ----------------------------------------------------------
+// table[p][i] = gain (cos, sin)(p theta_i), angles in 64 bits and rounded once: at
+// position 2^20 a 32-bit angle is off by up to 0.06.  A thread an entry; 33024
+// positions of 64 pairs take TIME us, once a model.
+__global__ __launch_bounds__(256) void rope_table_kernel(const RopeArgs r, float2* __restrict__ table, int64_t n) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= n) return;
+  const int64_t p = e / r.pairs;
+  const int i = (int)(e - p * r.pairs);
+  double th = pow((double)r.base, -(double)(2 * i) / (double)(2 * r.pairs));
+  if (r.scaling == 1) {
+    th = th / (double)r.factor;
+  } else if (r.scaling == 2) {
+    // turns that the original context holds: many keep theta, few divide it
+    const double t = (double)r.original * th / 6.283185307179586476925;
+    const double w = fmin(fmax((t - (double)r.low) / ((double)r.high - (double)r.low), 0.0), 1.0);
+    th = th * (w + (1.0 - w) / (double)r.factor);
+  }
+  double s, c;
+  sincos((double)p * th, &s, &c);
+  table[e] = float2{(float)(c * (double)r.gain), (float)(s * (double)r.gain)};
+}
+
+// ---- rows --------------------------------------------------------------------------
+// Four values at any element, or 16 (8) bytes at once where they are aligned.
+template <bool VEC>
+__device__ __forceinline__ void load4(const float* p, float* x) {
+  if constexpr (VEC) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = p[i];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load4(const bf16_t* p, float* x) {
+  if constexpr (VEC) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
+    x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = bf2f(p[i]);
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(float* p, const float* x) {
+  if constexpr (VEC) {
+    *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = x[i];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(bf16_t* p, const float* x) {
+  if constexpr (VEC) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    *reinterpret_cast<uint2*>(p) = uint2{__builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[0], x[1]}, b2)),
+                                         __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[2], x[3]}, b2))};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = f2bf(x[i]);
+  }
+}
+
+// HD / 8 lanes a head, eight values a lane: four pairs of the rotation, so nothing
+// but the norm's sum crosses lanes.  Pairs (i, i + P): values 4 j .. and P + 4 j ..
+// of lane j, the ones past the rotated part in order after them.  Neighbouring
+// pairs: eight values in a row.  VEC: both are runs of four values at aligned
+// addresses (P a multiple of 4).
+// Elements of value v (0 .. 7) of lane j: pair v / 2 in either layout.
+__device__ __forceinline__ int element(int j, int v, int P, bool cross) {
+  const int u = 4 * j + (v >> 1);
+  return cross && u < P ? u + (v & 1) * P : 2 * u + (v & 1);
+}
+
+// x[2 i], x[2 i + 1]: pair i of the lane.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_pairs(const T* p, int j, int P, bool cross, float* x) {
+  if constexpr (VEC) {
+    const bool turned = cross && 4 * j < P;
+    float a[8];
+    load4<true>(p + (turned ? 4 * j : 8 * j), a);
+    load4<true>(p + (turned ? P + 4 * j : 8 * j + 4), a + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = turned ? a[i] : a[2 * i];
+      x[2 * i + 1] = turned ? a[4 + i] : a[2 * i + 1];
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < 8; ++v) x[v] = ET<T>::to_f(p[element(j, v, P, cross)]);
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_pairs(T* p, int j, int P, bool cross, const float* x) {
+  if constexpr (VEC) {
+    const bool turned = cross && 4 * j < P;
+    float a[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = turned ? x[2 * i] : x[i];
+      a[4 + i] = turned ? x[2 * i + 1] : x[4 + i];
+    }
+    store4<true>(p + (turned ? 4 * j : 8 * j), a);
+    store4<true>(p + (turned ? P + 4 * j : 8 * j + 4), a + 4);
+  } else {
+#pragma unroll
+    for (int v = 0; v < 8; ++v) p[element(j, v, P, cross)] = ET<T>::from_f(x[v]);
+  }
+}
+
+template <int HD>
+__device__ __forceinline__ float head_sum(float v) {  // over the HD / 8 lanes of a head
+  if constexpr (HD == 128) return row16_sum(v);
+  v = v + dpp_mov<DPP_XOR1>(v);
+  v = v + dpp_mov<DPP_XOR2>(v);
+  return v + dpp_mov<DPP_MIRROR8>(v);
+}
+
+// y = x (mean(x^2) + eps)^-1/2 gain.  Squares that pass 2^128 are summed again at
+// 2^-128 of their size, where eps counts for nothing; an infinity makes its own
+// value NaN and the others 0, as the formula does.
+template <int HD>
+__device__ __forceinline__ void head_norm(float (&x)[8], const float (&gain)[8], float eps) {
+  float ss = 0.f;
+#pragma unroll
+  for (int v = 0; v < 8; ++v) ss = fmaf(x[v], x[v], ss);
+  ss = head_sum<HD>(ss);
+  if (__ballot(ss == CH_INF) != 0) {
+    if (ss == CH_INF) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) x[v] = x[v] * 0x1p-64f;
+      eps = 0.f;
+    }
+    float s2 = 0.f;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) s2 = fmaf(x[v], x[v], s2);
+    ss = head_sum<HD>(s2);
+  }
+  const float r = 1.0f / sqrtf(ss * (1.0f / HD) + eps);
+#pragma unroll
+  for (int v = 0; v < 8; ++v) x[v] = x[v] * r * gain[v];
+}
+
+// Grid (blocks of a row's heads, rows).  A lane does the same eight places of
+// every head it takes, so the table and the gains are read once.
+template <typename TI, typename TC, int HD, bool VEC>
+__global__ __launch_bounds__(256) void paged_append_kernel(const PagedView c, const AppendArgs a) {
+  constexpr int L = HD / 8, PER = 256 / L;
+  const int j = threadIdx.x % L, slot = blockIdx.x * PER + threadIdx.x / L;
+  const int P = a.pairs;
+  const bool cross = a.cross != 0;
+  const int heads = a.Hq + 2 * c.H;
+  for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    const int b = a.seq[row], p = a.pos[row];
+    if (b < 0 || b >= c.B || (P > 0 && p >= a.positions)) continue;
+    const uint32_t base = paged_row(c, c.page_table + (int64_t)b * c.max_pages, p);
+    if (base == PAGED_NONE) continue;
+    float cs[4], sn[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      cs[i] = 1.f, sn[i] = 0.f;
+      if (4 * j + i < P) {
+        const float2 t = a.table[(int64_t)p * P + 4 * j + i];
+        cs[i] = t.x, sn[i] = t.y;
+      }
+    }
+    for (int h = slot; h < heads; h += PER * gridDim.x) {  // the lanes of a head stay together
+      const bool is_q = h < a.Hq, is_v = h >= a.Hq + c.H;
+      const int kvh = h - a.Hq - (is_v ? c.H : 0);
+      const TI* src = is_q ? (const TI*)a.q + row * a.ld + h * HD
+                           : (const TI*)(is_v ? a.v : a.k) + row * a.ld + kvh * HD;
+      float x[8];
+      load_pairs<TI, VEC>(src, j, P, cross, x);
+      if (!is_v) {
+        const float* gain = is_q ? a.q_gain : a.k_gain;
+        if (gain != nullptr) {
+          float g[8];
+          load_pairs<float, VEC>(gain, j, P, cross, g);
+          head_norm<HD>(x, g, a.eps);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * j + i < P) {
+            const float u = x[2 * i], w = x[2 * i + 1];
+            x[2 * i] = u * cs[i] - w * sn[i];
+            x[2 * i + 1] = u * sn[i] + w * cs[i];
+          }
+      }
+      TC* dst = is_q ? (TC*)a.q_out + row * a.ldo + h * HD
+                     : (TC*)c.pool + ((uint64_t)base + (uint64_t)((is_v ? c.H : 0) + kvh) * c.ps.d) * HD;
+      store_pairs<TC, VEC>(dst, j, P, cross, x);
+    }
+  }
+}
+
+template <typename TI, typename TC, int HD>
+void append_go(const PagedView& c, const AppendArgs& a, bool vec, hipStream_t st) {
+  constexpr int PER = 256 / (HD / 8);
+  const int heads = a.Hq + 2 * c.H;
+  const dim3 grid((heads + PER - 1) / PER, a.rows < 65535 ? a.rows : 65535);
+  if (vec)
+    hipLaunchKernelGGL((paged_append_kernel<TI, TC, HD, true>), grid, dim3(256), 0, st, c, a);
+  else
+    hipLaunchKernelGGL((paged_append_kernel<TI, TC, HD, false>), grid, dim3(256), 0, st, c, a);
+}
+template <typename TI, typename TC>
+void append_t(const PagedView& c, const AppendArgs& a, bool vec, hipStream_t st) {
+  if (c.hd == 128)
+    append_go<TI, TC, 128>(c, a, vec, st);
+  else
+    append_go<TI, TC, 64>(c, a, vec, st);
+}
+
+}  // namespace
+
+void launch_rope_table(const RopeArgs& r, void* table, int positions, hipStream_t st) {
+  const int64_t n = (int64_t)positions * r.pairs;
+  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, r, (float2*)table, n);
+}
+
+void launch_paged_append(int dtype, int held, const PagedView& c, const AppendArgs& a, hipStream_t st) {
+  const int ei = dtype == DT_BF16 ? 2 : 4, ec = held == DT_BF16 ? 2 : 4;
+  auto runs = [](const void* p, int64_t ld, int es) { return ((uintptr_t)p % (4 * es)) == 0 && ld % 4 == 0; };
+  auto gain = [](const float* p) { return ((uintptr_t)p & 15) == 0; };
+  const bool vec = (a.cross == 0 || a.pairs % 4 == 0) && runs(a.q, a.ld, ei) && runs(a.k, a.ld, ei) &&
+                   runs(a.v, a.ld, ei) && (a.Hq == 0 || runs(a.q_out, a.ldo, ec)) && gain(a.q_gain) && gain(a.k_gain);
+  if (dtype == DT_BF16)
+    held == DT_BF16 ? append_t<bf16_t, bf16_t>(c, a, vec, st) : append_t<bf16_t, float>(c, a, vec, st);
+  else
+    held == DT_BF16 ? append_t<float, bf16_t>(c, a, vec, st) : append_t<float, float>(c, a, vec, st);
+}

@@ -8,32 +8,12 @@
 #include "abi.h"
 #include "chimera.h"
 #include "kernels.h"
+#include "ops.h"
 
 namespace {
 
 constexpr int FP4_MAX_ROWS = 4096;  // rows of a product: two prefill chunks
 
-int64_t round256(int64_t b) { return (b + 255) / 256 * 256; }
-
-void check_dtype(int32_t dtype) {
-  REQUIRE(dtype == CHIMERA_F32 || dtype == CHIMERA_BF16, CHIMERA_EINVAL, "dtype");
-}
-void check_aligned(const void* p, const char* what) {
-  REQUIRE(((uintptr_t)p & 15) == 0, CHIMERA_EINVAL, std::string(what) + " must be 16-byte aligned");
-}
-// The caller's stream must belong to the current device: the kernels are
-// launched there.
-hipStream_t check_stream(void* stream) {
-  hipStream_t st = (hipStream_t)stream;
-  if (st != nullptr) {
-    hipDevice_t on = 0;
-    int dev = 0;
-    HIPCK(hipStreamGetDevice(st, &on));
-    HIPCK(hipGetDevice(&dev));
-    REQUIRE((int)on == dev, CHIMERA_EINVAL, "the stream belongs to another device than the current one");
-  }
-  return st;
-}
 void check_matrix(int32_t N, int32_t K) {
   REQUIRE(N > 0 && N % 16 == 0 && K > 0 && K % 32 == 0, CHIMERA_EINVAL, "N must be a multiple of 16, K of 32");
   REQUIRE(N <= 1 << 20 && K <= 1 << 20, CHIMERA_EINVAL, "N and K are at most 2^20");
