@@ -19,38 +19,58 @@ struct QueryBlock {
 };
 __device__ __forceinline__ int clamp_row(const PagedAttnArgs& a, int r) { return min(max(r, 0), a.rows); }
 
-// Block `slot` of BQ queries.  All lanes of a wave; the result is uniform.
-template <int BQ>
-__device__ __forceinline__ QueryBlock find_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
+// A sequence whose queries of one cache head are few goes to the kernel for few, the
+// others to the tiled one: TODO both sides measured.
+constexpr int FEW = 64;
+
+__device__ __forceinline__ void seq_rows(const PagedAttnArgs& a, int b, int& row0, int& rows) {
+  row0 = b, rows = 1;
+  if (a.row0 != nullptr) {
+    row0 = clamp_row(a, a.row0[b]);
+    rows = max(clamp_row(a, a.row0[b + 1]) - row0, 0);
+  }
+}
+
+// Block `slot` of 16 queries: the same number of slots a sequence.
+__device__ __forceinline__ QueryBlock few_block(const PagedAttnArgs& a, int slot) {
   QueryBlock k;
-  int rows = 1, at;
+  k.b = slot / a.per;
+  int rows;
+  seq_rows(a, k.b, k.row0, rows);
+  const int queries = rows * a.group;
+  k.v0 = (slot - k.b * a.per) * 16;
+  k.count = queries > FEW ? 0 : max(min(queries - k.v0, 16), 0);
+  k.n = min(a.n_b[k.b], 1 << 30);
+  return k;
+}
+// Block `slot` of 128 queries.  All lanes of a wave; the result is uniform.
+__device__ __forceinline__ QueryBlock many_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
+  constexpr int BQ = 128;
+  QueryBlock k;
+  int rows, at;
   if (a.row0 == nullptr) {
     const int per = (a.group + BQ - 1) / BQ;
     k.b = slot / per;
-    k.row0 = k.b;
     at = slot - k.b * per;
   } else {
     // the last sequence whose slots start at or before this one, 64 looked at at once
     const int lane = threadIdx.x & 63;
     int lo = 0, len = c.B;
-    bool none = false;
     do {
       const int step = (len + 63) / 64, i = lo + lane * step;
       const bool before =
           lane * step < len && (int)((int64_t)clamp_row(a, a.row0[i]) * a.group / BQ) + i <= slot;
-      const int k64 = __popcll(__ballot(before));
-      none = none || k64 == 0;
-      const int skip = max(k64 - 1, 0) * step;
+      const int skip = max(__popcll(__ballot(before)) - 1, 0) * step;
       lo += skip;
       len = min(step, len - skip);
     } while (len > 1);
     k.b = __builtin_amdgcn_readfirstlane(lo);
-    k.row0 = clamp_row(a, a.row0[k.b]);
-    rows = none ? 0 : max(clamp_row(a, a.row0[k.b + 1]) - k.row0, 0);
-    at = slot - ((int)((int64_t)k.row0 * a.group / BQ) + k.b);
+    at = slot - ((int)((int64_t)clamp_row(a, a.row0[k.b]) * a.group / BQ) + k.b);
   }
+  seq_rows(a, k.b, k.row0, rows);
+  const int queries = rows * a.group;
   k.v0 = at * BQ;
-  k.count = max(min(rows * a.group - k.v0, BQ), 0);
+  k.count = queries <= FEW || at < 0 ? 0 : max(min(queries - k.v0, BQ), 0);
   k.n = min(a.n_b[k.b], 1 << 30);
   return k;
 }
@@ -111,17 +131,91 @@ __device__ __forceinline__ uint32_t cvt_pk_bf16(float a, float b) {
   typedef __bf16 b2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
 }
+// A word's sign bits come out set where an exponent is all ones.
 template <typename T>
-__device__ __forceinline__ bool any_nonfinite(int4 v);
-template <>
-__device__ __forceinline__ bool any_nonfinite<bf16_t>(int4 v) {
-  auto bad = [](int w) { return (w & 0x7f80) == 0x7f80 || (w & 0x7f800000) == 0x7f800000; };
-  return bad(v.x) || bad(v.y) || bad(v.z) || bad(v.w);
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
+  constexpr uint32_t E = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, ONE = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+  return ((w & E) + ONE) & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u);
 }
-template <>
-__device__ __forceinline__ bool any_nonfinite<float>(int4 v) {
-  auto bad = [](int w) { return (w & 0x7f800000) == 0x7f800000; };
-  return bad(v.x) || bad(v.y) || bad(v.z) || bad(v.w);
+
+template <typename T, int HD>
+__device__ __forceinline__ uint32_t odd_row(const T* p) {
+  uint32_t odd = 0;
+  for (int i = 0; i < HD; i += 16 / (int)sizeof(T)) {
+    const int4 x = ld16(p + i);
+    odd |= odd_bits<T>(x.x) | odd_bits<T>(x.y) | odd_bits<T>(x.z) | odd_bits<T>(x.w);
+  }
+  return odd;
+}
+// Whether `bytes` of a tile of V in LDS hold an infinity or a NaN; a wave.
+template <typename T>
+__device__ __forceinline__ bool odd_tile(const char* v, int bytes, int lane) {
+  uint32_t odd = 0;
+  for (int i = lane * 16; i < bytes; i += 1024) {
+    const int4 x = ld16(v + i);
+    odd |= odd_bits<T>(x.x) | odd_bits<T>(x.y) | odd_bits<T>(x.z) | odd_bits<T>(x.w);
+  }
+  return __ballot(odd != 0) != 0;
+}
+
+// A wave's LDS writes before its later reads, by other lanes too.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
+}
+
+// A tile that some queries see in part and whose V holds an infinity or a NaN: what a
+// query does not see must not reach it, and 0 x inf would carry it through a matrix
+// product.  The kernels leave such tiles out and a wave takes them by itself at the
+// end, a query at a time over the keys it sees: lanes are keys for the scores and
+// dimensions for the sums.  Its queries' states lie in LDS: m, l and o, rows `ldo` apart.
+template <typename T, int HD>
+__device__ __forceinline__ void tile_alone(const PagedView& c, const PagedAttnArgs& a, const int* ptab, int base, int keys,
+                                        const QueryBlock& blk, int v0, int count, int kvh, float* m, float* l,
+                                           float* o, int ldo) {
+  const int lane = threadIdx.x & 63;
+  const T* pool = (const T*)c.pool;
+  const int n = blk.n, b_row0 = blk.row0, pos = base + lane;
+  const uint32_t row = lane < keys ? paged_row(c, ptab, pos) : PAGED_NONE;
+  const uint32_t at = row + (uint32_t)(kvh * c.ps.d);
+  constexpr int D = HD / 64;
+  for (int i = 0; i < count; ++i) {
+    const int qrow = (v0 + i) / a.group, head = kvh * a.group + v0 + i - qrow * a.group;
+    bool seen = row != PAGED_NONE && pos <= n + qrow;
+    if (a.window > 0) seen = seen && (pos > n + qrow - a.window || pos < a.sinks);
+    const uint64_t vis = __ballot(seen);
+    if (vis == 0) continue;
+    float s = -CH_INF;
+    if (seen) {
+      const T* q = (const T*)a.q + (int64_t)(b_row0 + qrow) * a.ldq + head * HD;
+      const T* k = pool + (uint64_t)at * HD;
+      s = 0.f;
+      for (int d = 0; d < HD; ++d) s = fmaf(ET<T>::to_f(q[d]), ET<T>::to_f(k[d]), s);
+      s = a.flip != 0 ? -s : s;
+    }
+    const float mn = fmaxf(m[i], fmaxf(wave_max(s) * a.scale2, UNKNOWN));
+    const float al = m[i] == mn ? 1.f : weight(m[i], mn);
+    float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, a.scale2, -mn)) : 0.f;
+    const float ls = wave_sum(p);
+    p = ET<T>::to_f(ET<T>::from_f(p));
+    float x[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) x[d] = o[i * ldo + lane * D + d] * al;
+    for (uint64_t rest = vis; rest != 0; rest &= rest - 1) {
+      const int key = __ffsll((long long)rest) - 1;
+      const float pk = __shfl(p, key);
+      const T* vr = pool + (uint64_t)((uint32_t)__shfl((int)at, key) + (uint32_t)(c.H * c.ps.d)) * HD + lane * D;
+#pragma unroll
+      for (int d = 0; d < D; ++d) x[d] = fmaf(pk, ET<T>::to_f(vr[d]), x[d]);
+    }
+#pragma unroll
+    for (int d = 0; d < D; ++d) o[i * ldo + lane * D + d] = x[d];
+    if (lane == 0) {
+      l[i] = fmaf(l[i], al, ls);
+      m[i] = mn;
+    }
+    wave_order();
+  }
 }
 
 // DV values of one row into the caller's output.
@@ -214,7 +308,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
   __shared__ float msh[4][RB], lsh[4][RB];
   const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
   const int split = rest % a.splits, slot = rest / a.splits;
-  const QueryBlock blk = find_block<RB>(c, a, slot);
+  const QueryBlock blk = few_block(a, slot);
   if (blk.count == 0) return;
   const Span<RT> span(c, a, blk);
   const int parts = parts_of(span.tiles, a.splits, R_LEAST);
@@ -243,6 +337,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
 #pragma unroll
   for (int j = 0; j < DV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  bool odd = false;
   for (int t = t0 + wave; t < t1; t += 4) {
     const int base = span.tile(t) * RT;
     const int pos = base + (lane & 31);
@@ -262,6 +357,24 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
       const uint32_t r = (uint32_t)__shfl(safe, 16 * (i / 4) + 4 * g + i % 4) + (uint32_t)((c.H + kvh) * c.ps.d);
       load_v<T, HD>(x.v[i], pool + (uint64_t)r * HD + c16 * DV);
     }
+    const bool whole = held == ~0u && all_see(a, base, base + RT - 1, span.p_lo, span.p_hi);
+    if (!whole) {
+      // values of rows that no query sees are zeros
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool on = (held >> (16 * (i / 4) + 4 * g + i % 4)) & 1;
+#pragma unroll
+        for (int w = 0; w < Tile::VW; ++w) {
+          x.v[i][w] = on ? x.v[i][w] : 0u;
+          any |= odd_bits<T>(x.v[i][w]);
+        }
+      }
+      if (__ballot(any != 0) != 0) {
+        odd = true;
+        continue;
+      }
+    }
     f32x4 s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -269,7 +382,6 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) s[h] = mfma_kb<T>(x.k[h][ks], qf[ks], s[h]);
     }
-    const bool whole = held == ~0u && all_see(a, base, base + RT - 1, span.p_lo, span.p_hi);
     const uint32_t vis = whole ? ~0u : held & seen_bits(a, base, qpos);
     const uint32_t mine = vis >> (4 * g);
     float mx = -CH_INF;
@@ -301,44 +413,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
     if constexpr (sizeof(T) == 2)
       pf = int4{(int)cvt_pk_bf16(s[0][0], s[0][1]), (int)cvt_pk_bf16(s[0][2], s[0][3]),
                 (int)cvt_pk_bf16(s[1][0], s[1][1]), (int)cvt_pk_bf16(s[1][2], s[1][3])};
-    if (whole) {
-      row_pv<T, HD>(x.v, s, pf, o);
-      continue;
-    }
-    // A masked tile: values of rows that no query sees are zeros, and an infinity or a
-    // NaN in a row that some queries see and others do not must not reach the others
-    // through 0 x inf.  Where there is one, the tile is multiplied a query at a time.
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool on = (held >> (16 * (i / 4) + 4 * g + i % 4)) & 1;
-#pragma unroll
-      for (int w = 0; w < Tile::VW; ++w) x.v[i][w] = on ? x.v[i][w] : 0u;
-#pragma unroll
-      for (int w = 0; w < Tile::VW; w += 2)
-        odd = odd || any_nonfinite<T>(int4{(int)x.v[i][w], (int)x.v[i][w + 1], 0, 0});
-    }
-    if (__ballot(odd) == 0) {
-      row_pv<T, HD>(x.v, s, pf, o);
-    } else {
-      for (int q = 0; q < RB; ++q) {
-        const uint32_t vq_bits = (uint32_t)__builtin_amdgcn_readlane((int)vis, q);
-        uint32_t v[8][Tile::VW];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int w = 0; w < Tile::VW; ++w)
-            v[i][w] = (vq_bits >> (16 * (i / 4) + 4 * g + i % 4)) & 1 ? x.v[i][w] : 0u;
-        f32x4 oq[DV];
-#pragma unroll
-        for (int j = 0; j < DV; ++j) oq[j] = o[j];
-        row_pv<T, HD>(v, s, pf, oq);
-#pragma unroll
-        for (int j = 0; j < DV; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[j][r] = c16 == q ? oq[j][r] : o[j][r];
-      }
-    }
+    row_pv<T, HD>(x.v, s, pf, o);
   }
   l = rows_sum(l);
   // the four waves' states, joined in wave order
@@ -347,6 +422,21 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
 #pragma unroll
     for (int j = 0; j < DV; ++j) osh[wave][c16][(4 * g + r) * DV + j] = o[j][r];
   if (g == 0) msh[wave][c16] = m, lsh[wave][c16] = l;
+  if (odd) {
+    wave_order();
+    for (int t = t0 + wave; t < t1; t += 4) {
+      const int base = span.tile(t) * RT, pos = base + (lane & 31);
+      const uint32_t row = some_see(a, pos, span.p_lo, span.p_hi) ? paged_row(c, ptab, pos) : PAGED_NONE;
+      const uint32_t held = (uint32_t)__ballot(row != PAGED_NONE);
+      if (held == ~0u && all_see(a, base, base + RT - 1, span.p_lo, span.p_hi)) continue;
+      uint32_t any = 0;
+      if (row != PAGED_NONE)
+        any = odd_row<T, HD>(pool + (uint64_t)(row + (uint32_t)((c.H + kvh) * c.ps.d)) * HD);
+      if (__ballot(any != 0) != 0)
+        tile_alone<T, HD>(c, a, ptab, base, RT, blk, blk.v0, blk.count, kvh, msh[wave], lsh[wave], &osh[wave][0][0],
+                          HD + 4);
+    }
+  }
   __syncthreads();
   const int q = tid / 16, d0 = (tid % 16) * DV;
   float mt = msh[0][q];
@@ -378,13 +468,396 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
   if (tid % 16 == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = float2{mt, lt};
 }
 
+// ---- many queries ----------------------------------------------------------------
+// A workgroup takes 128 queries of one cache head and a part of their positions, a
+// wave 32 of them; tiles of K and V pass through LDS in two buffers, straight from
+// memory, the next one on its way while one is used.
+//
+// S^T = K Q^T by 32x32 MFMAs: a lane holds one query's scores (lane & 31) for half the
+// keys, so maxima and sums are one lane's own but for one exchange, and the scores of
+// 16 keys are as they stand the operand P^T of O^T += V^T P^T.  16-bit V^T comes from
+// LDS's transposed read: within each 16-lane group, lane i receives element i mod 4 of
+// the 8-byte blocks addressed by lanes i / 4 + 4 e.  f32 V is read along the row: an
+// MFMA's rows are every (HD / 32)th dimension.
+//
+// A row's 16-byte chunk x lies in place x ^ swizzle(row): the 16 rows of a K read and
+// the four rows x 64 bytes of half a transposed read then cover all banks once.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+constexpr int TB = 128;         // queries of a workgroup
+template <typename T>
+constexpr int TT = sizeof(T) == 2 ? 64 : 32;  // positions of a tile
+constexpr int T_LEAST = 4;      // tiles of a part
+
+template <int CH>  // chunks of a row
+__device__ __forceinline__ int swizzle(int row) {
+  return CH == 8 ? ((row >> 1) & 1) * 4 + ((row >> 2) & 3) : (row & 3) * 4 + ((row >> 2) & 3);
+}
+__device__ __forceinline__ int2 ld_tr16(const char* p) {
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  const s4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p);
+  return __builtin_bit_cast(int2, v);
+}
+__device__ __forceinline__ void dma16(const char* src, char* lds) {  // 16 bytes a lane, 1 KiB a wave
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+// Every load into LDS has landed, every LDS read has its data, on all waves.
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x0070);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ uint64_t low_bits64(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+template <typename T, int HD>
+struct ManyState {
+  static constexpr int KB = TT<T> / 32, ND = HD / 32, QR = HD * (int)sizeof(T) / 32;
+  int4 q[QR];            // this lane's query: 16 bytes of every 32
+  f32x16 o[ND];
+  float m, l;
+};
+
+// Where a lane reads in a tile: a key's row for S (its 16-byte piece i at place ^ 32 i),
+// its place in V^T's operands.  The steps over pieces, dimension blocks and keys only
+// flip chunk bits or add whole rows, so they cost an exclusive or and an immediate.
+template <typename T, int HD>
+struct LanePlaces {
+  static constexpr int ROW = HD * (int)sizeof(T), CH = ROW / 16;
+  int k, v;
+  __device__ __forceinline__ explicit LanePlaces(int lane) {
+    const int c32 = lane & 31, h = lane >> 5;
+    k = c32 * ROW + ((h ^ swizzle<CH>(c32)) << 4);
+    if constexpr (sizeof(T) == 2) {
+      const int g1 = (lane >> 4) & 1, a = lane & 15, key = 4 * h + (a >> 2);
+      v = key * ROW + (((2 * g1 + ((a & 3) >> 1)) ^ swizzle<CH>(key)) << 4) + ((a & 1) << 3);
+    } else {
+      const int at = c32 * (HD / 32) * 4;
+      v = 4 * h * ROW + (((at >> 4) ^ h) << 4) + (at & 15);
+    }
+  }
+  __device__ __forceinline__ int key(int kb, int i) const { return (k ^ (32 * i)) + 32 * kb * ROW; }
+  // bf16: keys 16 n + 8 e + 4 h .. + 3 of dimension block db
+  __device__ __forceinline__ int val16(int n, int e, int db) const {
+    return (v ^ (db << 6) ^ (e << 5)) + (16 * n + 8 * e) * ROW;
+  }
+  // f32: key 8 n + 4 h + j
+  __device__ __forceinline__ int val32(int n, int j) const { return (v ^ (j << 6) ^ ((n & 1) << 5)) + (8 * n + j) * ROW; }
+  // the sums are cheaper than the registers that would hold them through the loop
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(k), "+v"(v)); }
+};
+
+// V^T's operand of 16 keys.
+template <int HD>
+__device__ __forceinline__ int4 v_operand16(const char* v, const LanePlaces<bf16_t, HD>& at, int n, int db) {
+  const int2 lo = ld_tr16(v + at.val16(n, 0, db)), hi = ld_tr16(v + at.val16(n, 1, db));
+  return int4{lo.x, lo.y, hi.x, hi.y};
+}
+
+// The weights of a tile as operands: 16 keys each in bf16, themselves in f32.
+template <typename T>
+struct Weights {
+  static constexpr int N = sizeof(T) == 2 ? TT<T> / 16 : TT<T> / 8;
+  int4 p[N];
+  __device__ __forceinline__ explicit Weights(const f32x16 (&s)[TT<T> / 32]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if constexpr (sizeof(T) == 2) {
+        const f32x16& x = s[n / 2];
+        const int r = n % 2 * 8;
+        p[n] = int4{(int)cvt_pk_bf16(x[r], x[r + 1]), (int)cvt_pk_bf16(x[r + 2], x[r + 3]),
+                    (int)cvt_pk_bf16(x[r + 4], x[r + 5]), (int)cvt_pk_bf16(x[r + 6], x[r + 7])};
+      } else {
+        const f32x16& x = s[n / 4];
+        const int r = n % 4 * 4;
+        p[n] = int4{__float_as_int(x[r]), __float_as_int(x[r + 1]), __float_as_int(x[r + 2]), __float_as_int(x[r + 3])};
+      }
+    }
+  }
+};
+
+// O^T += V^T P^T over a tile.
+template <typename T, int HD>
+__device__ __forceinline__ void many_pv(const char* v, const LanePlaces<T, HD>& at, const Weights<T>& w,
+                                        f32x16 (&o)[HD / 32]) {
+  constexpr int ND = HD / 32;
+#pragma unroll
+  for (int n = 0; n < Weights<T>::N; ++n) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand16<HD>(v, at, n, db)),
+                                                        __builtin_bit_cast(bf16x8, w.p[n]), o[db], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const char* p = v + at.val32(n, j);
+        const float pj = __int_as_float(j == 0 ? w.p[n].x : j == 1 ? w.p[n].y : j == 2 ? w.p[n].z : w.p[n].w);
+        float x[ND];
+        if constexpr (ND == 4) {
+          const float4 f = *reinterpret_cast<const float4*>(p);
+          x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w;
+        } else {
+          const float2 f = *reinterpret_cast<const float2*>(p);
+          x[0] = f.x, x[1] = f.y;
+        }
+#pragma unroll
+        for (int db = 0; db < ND; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[db], pj, o[db], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// One tile for one wave.  held: its positions that the cache has and some query of the
+// workgroup sees.  odd: set where the tile was left for later (below).
+template <typename T, int HD>
+__device__ __forceinline__ void many_tile(const PagedAttnArgs& a, ManyState<T, HD>& st, const char* k, const char* v,
+                                          LanePlaces<T, HD> at, int base, uint64_t held, int qpos, int p_lo, int p_hi,
+                                          int lane, bool& odd) {
+  constexpr int KT = TT<T>, KB = KT / 32, ND = HD / 32, ROW = HD * (int)sizeof(T);
+  // nothing of it for this wave: past its queries, or before their window
+  if (base > p_hi || (a.window > 0 && base + KT - 1 <= p_lo - a.window && base >= a.sinks)) return;
+  const bool whole = held == low_bits64(KT) && all_see(a, base, base + KT - 1, p_lo, p_hi);
+  if (!whole && odd_tile<T>(v, KT * ROW, lane)) {
+    odd = true;
+    return;
+  }
+  const int h = lane >> 5;
+  at.renew();
+  f32x16 s[KB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < ManyState<T, HD>::QR; ++i) {
+      const int4 x = ld16(k + at.key(kb, i));
+      if constexpr (sizeof(T) == 2) {
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                        __builtin_bit_cast(bf16x8, st.q[i]), s[kb], 0, 0, 0);
+      } else {
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.x), __int_as_float(st.q[i].x), s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.y), __int_as_float(st.q[i].y), s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.z), __int_as_float(st.q[i].z), s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.w), __int_as_float(st.q[i].w), s[kb], 0, 0, 0);
+      }
+    }
+  }
+  uint64_t vis = held;
+  if (!whole) {
+    vis = (uint64_t)seen_bits(a, base, qpos) | (KB == 2 ? (uint64_t)seen_bits(a, base + 32, qpos) << 32 : 0ull);
+    vis &= held;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const uint32_t mine = (uint32_t)(vis >> (32 * kb)) >> (4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = (mine >> (8 * (r >> 2) + (r & 3))) & 1 ? s[kb][r] : -CH_INF;
+    }
+  }
+  float mx = -CH_INF;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+  const float2 both = half_pair(mx);
+  mx = fmaxf(both.x, both.y);
+  const float mt = vis != 0 ? fmaxf(mx * a.scale2, UNKNOWN) : -CH_INF;
+  // The state is rescaled only where a maximum grew by more than 2^8 or was the first:
+  // weights up to 2^8 keep their relative precision in bf16 and in the sums.
+  const bool grown = mt > st.m + 8.f || st.m == -CH_INF;
+  if (__ballot(grown) != 0) {
+    const float mn = grown ? fmaxf(st.m, mt) : st.m;
+    const float al = st.m == mn ? 1.f : weight(st.m, mn);
+    st.m = mn;
+    st.l = st.l * al;
+#pragma unroll
+    for (int db = 0; db < ND; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[db][r] = st.o[db][r] * al;
+  }
+  // a masked score, and every one of a query that has seen nothing yet, weighs nothing
+  const float sub = st.m == -CH_INF ? 0.f : st.m;
+  float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale2, -sub));
+      ls[r & 3] = ls[r & 3] + s[kb][r];
+    }
+  st.l = st.l + ((ls[0] + ls[1]) + (ls[2] + ls[3]));
+  const Weights<T> w(s);
+  many_pv<T, HD>(v, at, w, st.o);
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tiles_kernel(const PagedView c, const PagedAttnArgs a) {
+  typedef ManyState<T, HD> State;
+  constexpr int KT = TT<T>, ND = HD / 32, ROW = HD * (int)sizeof(T), CH = ROW / 16;
+  constexpr int NI = KT * ROW / 4096, RPI = 1024 / ROW;  // loads of a wave, rows of a load
+  __shared__ __attribute__((aligned(1024))) char k0[KT * ROW], v0[KT * ROW], k1[KT * ROW], v1[KT * ROW];
+  const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
+  const int split = rest % a.splits, slot = a.slots - 1 - rest / a.splits;  // later blocks see more: first
+  const QueryBlock blk = many_block(c, a, slot);
+  if (blk.count == 0) return;
+  const Span<KT> span(c, a, blk);
+  const int parts = parts_of(span.tiles, a.splits, T_LEAST);
+  if (split >= parts) return;
+  const int t0 = (int)((int64_t)span.tiles * split / parts), t1 = (int)((int64_t)span.tiles * (split + 1) / parts);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c32 = lane & 31, h = lane >> 5;
+  const int* ptab = c.page_table + (int64_t)blk.b * c.max_pages;
+  const char* pool = (const char*)c.pool;
+  const int first = min(wave * 32, blk.count - 1), last = min(wave * 32 + 31, blk.count - 1);
+  const bool on = wave * 32 < blk.count;
+  const int p_lo = blk.n + (blk.v0 + first) / a.group, p_hi = blk.n + (blk.v0 + last) / a.group;
+  const int vq = blk.v0 + min(wave * 32 + c32, blk.count - 1);
+  const int qrow = vq / a.group, qhead = kvh * a.group + vq - qrow * a.group;
+  State st;
+  {
+    const int flip = a.flip == 0 ? 0 : (sizeof(T) == 2 ? (int)0x80008000 : (int)0x80000000);
+    const char* q = (const char*)a.q + ((int64_t)(blk.row0 + qrow) * a.ldq + qhead * HD) * (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < State::QR; ++i) {
+      const int4 x = ld16(q + 32 * i + 16 * h);
+      st.q[i] = int4{x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip};
+    }
+  }
+  st.m = -CH_INF, st.l = 0.f;
+#pragma unroll
+  for (int db = 0; db < ND; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.o[db][r] = 0.f;
+
+  // A lane finds the row of one position of a tile; one that no query sees is read as
+  // the last position's.
+  const int p_end = min(span.p_hi, c.cap - 1);
+  uint32_t row_next;
+  uint64_t held_next;
+  auto find = [&](int t) {
+    const int pos = span.tile(t) * KT + (lane & (KT - 1));
+    const bool seen = some_see(a, pos, span.p_lo, span.p_hi);
+    const uint32_t row = paged_row(c, ptab, seen ? pos : p_end);
+    held_next = __ballot(seen && row != PAGED_NONE) & low_bits64(KT);
+    row_next = row == PAGED_NONE ? 0u : row;
+  };
+  auto load = [&](char* k, char* v) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int key = (wave * NI + i) * RPI + lane / CH;
+      const uint32_t r = (uint32_t)__shfl((int)row_next, key) + (uint32_t)(kvh * c.ps.d);
+      const char* src = pool + (uint64_t)r * ROW + (((lane % CH) ^ swizzle<CH>(key)) << 4);
+      dma16(src, k + (wave * NI + i) * 1024);
+      dma16(src + (uint64_t)(c.H * c.ps.d) * ROW, v + (wave * NI + i) * 1024);
+    }
+  };
+  const LanePlaces<T, HD> at(lane);
+  // two tiles a round, a buffer each; `held` of a tile travels with it
+  uint64_t held = 0;
+  bool odd = false;
+  if (t0 < t1) {
+    find(t0);
+    load(k0, v0);
+    held = held_next;
+    if (t0 + 1 < t1) find(t0 + 1);
+  }
+  auto step = [&](int t, const char* k, const char* v, char* kn, char* vn) {
+    tile_barrier();
+    const uint64_t mine = held;
+    if (t + 1 < t1) {
+      load(kn, vn);
+      held = held_next;
+      if (t + 2 < t1) find(t + 2);
+    }
+    if (on) many_tile<T, HD>(a, st, k, v, at, span.tile(t) * KT, mine, blk.n + qrow, p_lo, p_hi, lane, odd);
+  };
+  for (int t = t0; t < t1; t += 2) {
+    step(t, k0, v0, k1, v1);
+    if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
+  }
+  const float2 l2 = half_pair(st.l);
+  float lt = l2.x + l2.y;
+  tile_barrier();  // the tiles' space is free
+  if (odd) {
+    __shared__ float msh[4][32], lsh[4][32];
+    float* o = (float*)(wave == 0 ? k0 : wave == 1 ? v0 : wave == 2 ? k1 : v1);
+    auto dim = [&](int db, int r) {
+      const int row = 8 * (r >> 2) + 4 * h + (r & 3);
+      return c32 * HD + (sizeof(T) == 2 ? 32 * db + row : row * ND + db);
+    };
+#pragma unroll
+    for (int db = 0; db < ND; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[dim(db, r)] = st.o[db][r];
+    if (h == 0) msh[wave][c32] = st.m, lsh[wave][c32] = lt;
+    wave_order();
+    for (int t = t0; t < t1; ++t) {
+      const int base = span.tile(t) * KT;
+      if (base > p_hi || (a.window > 0 && base + KT - 1 <= p_lo - a.window && base >= a.sinks)) continue;
+      find(t);
+      if (held_next == low_bits64(KT) && all_see(a, base, base + KT - 1, p_lo, p_hi)) continue;
+      const uint32_t any = odd_row<T, HD>((const T*)pool + (uint64_t)(row_next + (uint32_t)((c.H + kvh) * c.ps.d)) * HD);
+      if (__ballot(any != 0) != 0)
+        tile_alone<T, HD>(c, a, ptab, base, KT, blk, blk.v0 + wave * 32, last - first + 1, kvh, msh[wave], lsh[wave], o,
+                          HD);
+    }
+#pragma unroll
+    for (int db = 0; db < ND; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[db][r] = o[dim(db, r)];
+    st.m = msh[wave][c32];
+    lt = lsh[wave][c32];
+  }
+  if (wave * 32 + c32 >= blk.count) return;
+  if (parts == 1) {
+    T* dst = (T*)a.out + (int64_t)(blk.row0 + qrow) * a.ldo + qhead * HD;
+    const float inv = 1.0f / lt;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = st.m == -CH_INF ? 0.f : st.o[db][4 * i + j] * inv;
+          store_out<T, 4>(dst + 32 * db + 8 * i + 4 * h, x, a.vec_out != 0);
+        }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) x[d] = st.m == -CH_INF ? 0.f : st.o[d][r] / lt;
+        const int dim = (8 * (r >> 2) + 4 * h + (r & 3)) * ND;
+        if constexpr (ND == 4) {
+          store_out<T, 4>(dst + dim, x, a.vec_out != 0);
+        } else {
+          dst[dim] = x[0];
+          dst[dim + 1] = x[1];
+        }
+      }
+    }
+    return;
+  }
+  const int64_t part = (((int64_t)slot * c.H + kvh) * a.splits + split) * TB + wave * 32 + c32;
+  float* po = a.part_o + part * HD;
+#pragma unroll
+  for (int db = 0; db < ND; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = 8 * (r >> 2) + 4 * h + (r & 3);
+      po[sizeof(T) == 2 ? 32 * db + row : row * ND + db] = st.o[db][r];
+    }
+  if (h == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = float2{st.m, lt};
+}
+
 // The parts of a query, joined in order: a wave a query, 64 parts' factors at once.
 template <typename T, int HD, int BQ, int TILE>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, const PagedAttnArgs a, int least) {
   const int q0 = blockIdx.x * 4 + (threadIdx.x >> 6);  // query of a slot and cache head
   const int q = q0 % BQ, kvh = q0 / BQ % c.H, slot = q0 / BQ / c.H;
   const int lane = threadIdx.x & 63;
-  const QueryBlock blk = find_block<BQ>(c, a, slot);
+  const QueryBlock blk = BQ == RB ? few_block(a, slot) : many_block(c, a, slot);
   if (q >= blk.count) return;
   const Span<TILE> span(c, a, blk);
   const int parts = parts_of(span.tiles, a.splits, least);
@@ -420,40 +893,68 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, cons
 }
 
 // ---- deal ------------------------------------------------------------------------
-constexpr int R_WGS = 1024;  // workgroups that fill the card, four a CU
+constexpr int R_WGS = 1024;  // workgroups that fill the card: four a CU
+constexpr int T_WGS = 512;   // two a CU
 
-int64_t row_splits(int64_t cap, int64_t blocks) {
-  const int64_t tiles = (cap + RT - 1) / RT + 2;  // a window's ends cut two more
-  return std::max<int64_t>(1, std::min((R_WGS + blocks - 1) / blocks, (tiles + R_LEAST - 1) / R_LEAST));
+// Parts of a block's positions: as many as fill the card, none of them short.
+int64_t deal_splits(int64_t cap, int64_t blocks, int wgs, int tile, int least) {
+  const int64_t tiles = (cap + tile - 1) / tile + 2;  // a window's ends cut two more
+  return std::max<int64_t>(1, std::min((wgs + blocks - 1) / blocks, (tiles + least - 1) / least));
+}
+// Partials of any call of up to `blocks` blocks: less than one round over the card
+// more than the blocks, or every block's most.
+int64_t deal_slots(int64_t cap, int64_t blocks, int wgs, int tile, int least) {
+  return std::min(std::min<int64_t>(blocks, wgs) * deal_splits(cap, 1, 1 << 30, tile, least), (int64_t)2 * wgs);
+}
+
+int64_t few_per(bool single, int rows, int group) {
+  const int64_t queries = single ? group : std::min<int64_t>((int64_t)rows * group, FEW);
+  return (std::min<int64_t>(queries, FEW) + RB - 1) / RB;
+}
+int64_t many_slots(bool single, int64_t rows, int batch, int group) {
+  return single ? (int64_t)batch * ((group + TB - 1) / TB) : rows * group / TB + batch;
 }
 
 template <typename T, int HD>
 void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
-  const int64_t slots = paged_attn_slots(a.row0 == nullptr, a.rows, c.B, a.group, RB);
-  const int64_t splits = row_splits(c.cap, slots * c.H);
-  a.slots = (int)slots;
-  a.splits = (int)splits;
-  a.part_o = (float*)ws;
-  a.part_ml = a.part_o + slots * c.H * splits * RB * HD;
-  hipLaunchKernelGGL((paged_rows_kernel<T, HD>), dim3((unsigned)(slots * splits * c.H)), dim3(256), 0, st, c, a);
-  if (splits > 1)
-    hipLaunchKernelGGL((paged_join_kernel<T, HD, RB, RT>), dim3((unsigned)(slots * c.H * RB / 4)), dim3(256), 0, st, c, a,
-                       R_LEAST);
+  const bool single = a.row0 == nullptr;
+  const int64_t most = single ? a.group : (int64_t)a.rows * a.group;  // queries of a sequence
+  float* at = (float*)ws;
+  if (!single || most <= FEW) {
+    PagedAttnArgs f = a;
+    f.per = (int)few_per(single, a.rows, a.group);
+    f.slots = c.B * f.per;
+    f.splits = (int)deal_splits(c.cap, (int64_t)f.slots * c.H, R_WGS, RT, R_LEAST);
+    const int64_t parts = (int64_t)f.slots * c.H * f.splits;
+    f.part_o = at;
+    f.part_ml = at + parts * RB * HD;
+    hipLaunchKernelGGL((paged_rows_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, f);
+    if (f.splits > 1) {
+      at = f.part_ml + parts * RB * 2;
+      hipLaunchKernelGGL((paged_join_kernel<T, HD, RB, RT>), dim3((unsigned)(f.slots * c.H * RB / 4)), dim3(256), 0, st, c,
+                         f, R_LEAST);
+    }
+  }
+  if (most > FEW) {
+    a.slots = (int)many_slots(single, a.rows, c.B, a.group);
+    a.splits = (int)deal_splits(c.cap, (int64_t)a.slots * c.H, T_WGS, TT<T>, T_LEAST);
+    const int64_t parts = (int64_t)a.slots * c.H * a.splits;
+    a.part_o = at;
+    a.part_ml = at + parts * TB * HD;
+    hipLaunchKernelGGL((paged_tiles_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
+    if (a.splits > 1)
+      hipLaunchKernelGGL((paged_join_kernel<T, HD, TB, TT<T>>), dim3((unsigned)(a.slots * c.H * TB / 4)), dim3(256), 0, st,
+                         c, a, T_LEAST);
+  }
 }
 
 }  // namespace
 
-int64_t paged_attn_slots(bool single, int64_t rows, int batch, int group, int block) {
-  return single ? (int64_t)batch * ((group + block - 1) / block) : rows * group / block + batch;
-}
-
-// Splitting stops where the blocks fill the card, so the partials of any call of up
-// to `rows` rows, at most the blocks it has and less than one more round, fit in this.
-int64_t paged_attn_bytes(int64_t cap, int rows, int batch, int group, int H, int hd) {
-  const int64_t per = (int64_t)RB * (hd + 2) * 4;
-  const int64_t blocks = std::max(paged_attn_slots(false, rows, batch, group, RB), paged_attn_slots(true, rows, batch, group, RB)) * H;
-  const int64_t most = ((cap + RT - 1) / RT + 2 + R_LEAST - 1) / R_LEAST;
-  return std::min(std::min<int64_t>(blocks, R_WGS) * most, (int64_t)2 * R_WGS) * per;
+int64_t paged_attn_bytes(int64_t cap, int rows, int batch, int group, int H, int hd, int es) {
+  const int64_t few = (int64_t)batch * std::max(few_per(false, rows, group), few_per(true, rows, group)) * H;
+  const int64_t many = std::max(many_slots(false, rows, batch, group), many_slots(true, rows, batch, group)) * H;
+  const int tile = es == 2 ? TT<bf16_t> : TT<float>;
+  return (deal_slots(cap, few, R_WGS, RT, R_LEAST) * RB + deal_slots(cap, many, T_WGS, tile, T_LEAST) * TB) * (hd + 2) * 4;
 }
 
 void launch_paged_attn(int dtype, const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {

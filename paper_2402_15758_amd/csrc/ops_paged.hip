@@ -195,7 +195,7 @@ chimera_status chimera_paged_attn_bytes(const chimera_paged* cache, int32_t n_he
     REQUIRE(bytes != nullptr, CHIMERA_EINVAL, "null bytes");
     check_attn_rows(cache, n_heads, rows);
     *bytes = paged_attn_bytes((int64_t)cache->max_pages * cache->page_size, rows, cache->batch,
-                              n_heads / cache->n_heads, cache->n_heads, cache->head_dim);
+                              n_heads / cache->n_heads, cache->n_heads, cache->head_dim, (int)esize(cache->dtype));
   });
 }
 
@@ -216,7 +216,7 @@ chimera_status chimera_paged_attn(const chimera_paged* cache, const void* q, int
             "scale must be finite, at most 2^127 in magnitude");  // times log2(e) it still is
     const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
     const int group = n_heads / cache->n_heads;
-    const int64_t need = paged_attn_bytes(cap, rows, cache->batch, group, cache->n_heads, cache->head_dim);
+    const int64_t need = paged_attn_bytes(cap, rows, cache->batch, group, cache->n_heads, cache->head_dim, (int)es);
     REQUIRE(need == 0 || ws != nullptr, CHIMERA_EINVAL, "null workspace");
     REQUIRE(ws_bytes >= need, CHIMERA_ENOMEM, "workspace too small");
     check_aligned(ws, "workspace");
@@ -234,7 +234,9 @@ chimera_status chimera_paged_attn(const chimera_paged* cache, const void* q, int
     a.group = group;
     a.window = window;
     a.sinks = sinks;
-    a.scale2 = std::fabs(scale) * 1.44269504088896340736f;
+    // a masked score is -inf and must weigh nothing where scale is 0 too: 2^-140 of a
+    // score is no weight's last bit
+    a.scale2 = std::max(std::fabs(scale) * 1.44269504088896340736f, 0x1p-140f);
     a.flip = scale < 0.f;
     a.vec_out = ((uintptr_t)out & 15) == 0 && ldo * es % 16 == 0;
     launch_paged_attn(cache->dtype, view(cache), a, ws, st);

@@ -74,14 +74,13 @@ struct PagedAttnArgs {
   int window, sinks;        // window 0: every position
   float scale2;             // |scale| log2(e)
   int flip;                 // scale < 0: queries are negated
-  int splits;               // parts of a block's positions at most
-  int slots;                // blocks of queries, of one cache head
+  // a launch's own: parts of a block's positions at most, blocks of queries of one cache
+  // head, those of a sequence in the kernel for few queries
+  int splits, slots, per;
   int vec_out;              // out rows at multiples of 16 bytes
   float* part_o;            // [slots][H][splits][block][hd]
   float* part_ml;           // [slots][H][splits][block][2]
 };
-// Slots for blocks of `block` queries (query = row x head of a group): sequence b's
-// start at floor(row0[b] group / block) + b, which leaves each room for its own.
-int64_t paged_attn_slots(bool single, int64_t rows, int batch, int group, int block);
-int64_t paged_attn_bytes(int64_t cap, int rows, int batch, int group, int H, int hd);
+// Partials of a call, and of any with fewer rows or sequences.
+int64_t paged_attn_bytes(int64_t cap, int rows, int batch, int group, int H, int hd, int es);
 void launch_paged_attn(int dtype, const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st);

@@ -305,7 +305,6 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, bad):
     for lens, rows, at, window in (([40], [60], 70, 0), ([200], [9], 204, 0), ([100], [50], 100, 20), ([7], [3], 8, 2),
                                    ([300], [140], 310, 64)):
         q, pool, table = attn_inputs(dtype, lens, rows, 2, 1, 64, 16, 8)
-        clean = attend(q, pool, table, lens, rows, dtype, 0.125, window)
         for kv in (0, 1):
             spoilt = pool.clone()
             spoilt[table[0, at // 16], kv, :, at % 16, 3] = bad
@@ -313,10 +312,14 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, bad):
             ref, mag, big = R.attention(q, spoilt, table, lens, rows, 0.125, window)
             p = lens[0] + torch.arange(rows[0])
             free = (p < at) | ((p >= at + window) if window else torch.zeros_like(p, dtype=torch.bool))
-            assert torch.equal(got[free], clean[free])
             assert bool(free.any()) and not bool(free.all())
+            # The tile that holds it is summed in another way than it would be without it,
+            # so its rows keep their values to the bound of any way of summing (the
+            # reference sums what a row sees) and not to the bit.
+            near = (got - ref).abs() <= R.attention_bound(dtype, ref, mag, big, 500, 64)
+            assert bool(near[free].all())
             if kv == 1:  # a value: only its dimension, as the sum has it
-                assert torch.equal(got[~free][..., :3], clean[~free][..., :3])
+                assert bool(near[~free][..., :3].all()) and bool(near[~free][..., 4:].all())
                 assert bool((got[~free][..., 3].isnan() if math.isnan(bad) else got[~free][..., 3] == bad).all())
             elif math.isnan(bad):
                 assert bool(got[~free].isnan().all())
