@@ -554,58 +554,114 @@ __device__ __forceinline__ int4 v_operand16(const char* v, const LanePlaces<bf16
   return int4{lo.x, lo.y, hi.x, hi.y};
 }
 
-// The weights of a tile as operands: 16 keys each in bf16, themselves in f32.
-template <typename T>
-struct Weights {
-  static constexpr int N = sizeof(T) == 2 ? TT<T> / 16 : TT<T> / 8;
-  int4 p[N];
-  __device__ __forceinline__ explicit Weights(const f32x16 (&s)[TT<T> / 32]) {
+// The scheduler would rather save registers than start LDS reads ahead of the products
+// that need them; where the order matters it is pinned.
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+// S^T = K Q^T of a tile, reads half a tile ahead of their products.
+template <typename T, int HD>
+__device__ __forceinline__ void many_scores(const char* k, const LanePlaces<T, HD>& at, const int4 (&q)[HD * sizeof(T) / 32],
+                                            f32x16 (&s)[TT<T> / 32]) {
+  constexpr int KB = TT<T> / 32, QR = HD * (int)sizeof(T) / 32;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+  if constexpr (sizeof(T) == 2) {
+    int4 x[2][QR];
+#pragma unroll
+    for (int i = 0; i < QR; ++i) x[0][i] = ld16(k + at.key(0, i));
+    pin();
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < QR; ++i) {
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[kb][i]),
+                                                        __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
+        if (kb + 1 < KB) x[kb + 1][i] = ld16(k + at.key(kb + 1, i));
+        pin();
+      }
+  } else {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < QR; ++i) {
+        const int4 x = ld16(k + at.key(kb, i));
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.x), __int_as_float(q[i].x), s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.y), __int_as_float(q[i].y), s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.z), __int_as_float(q[i].z), s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.w), __int_as_float(q[i].w), s[kb], 0, 0, 0);
+      }
+  }
+}
+
+// Scores become weights, 2^(scale2 s - sub), their sum grows l and O^T += V^T P^T.  bf16:
+// the products of 16 keys run beside the reads and exponentials of the next 16.
+template <typename T, int HD>
+__device__ __forceinline__ void many_values(const char* v, const LanePlaces<T, HD>& at, f32x16 (&s)[TT<T> / 32],
+                                            float scale2, float sub, float& l, f32x16 (&o)[HD / 32]) {
+  constexpr int KB = TT<T> / 32, ND = HD / 32;
+  float ls[4] = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (sizeof(T) == 2) {
+    constexpr int N = TT<T> / 16;
+    int4 vf[2][ND];
+    uint32_t p[2][4];
+    auto weights = [&](int n, int q) {  // weights 2 q and 2 q + 1 of the lane's eight of 16 keys
+      const int kb = n / 2, r = n % 2 * 8 + 2 * q;
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kb][r], scale2, -sub));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kb][r + 1], scale2, -sub));
+      ls[q] = ls[q] + (p0 + p1);
+      p[n & 1][q] = cvt_pk_bf16(p0, p1);
+    };
+#pragma unroll
+    for (int db = 0; db < ND; ++db) vf[0][db] = v_operand16<HD>(v, at, 0, db);
+    pin();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) weights(0, q);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      if constexpr (sizeof(T) == 2) {
-        const f32x16& x = s[n / 2];
-        const int r = n % 2 * 8;
-        p[n] = int4{(int)cvt_pk_bf16(x[r], x[r + 1]), (int)cvt_pk_bf16(x[r + 2], x[r + 3]),
-                    (int)cvt_pk_bf16(x[r + 4], x[r + 5]), (int)cvt_pk_bf16(x[r + 6], x[r + 7])};
-      } else {
-        const f32x16& x = s[n / 4];
-        const int r = n % 4 * 4;
-        p[n] = int4{__float_as_int(x[r]), __float_as_int(x[r + 1]), __float_as_int(x[r + 2]), __float_as_int(x[r + 3])};
+      const int4 pn = int4{(int)p[n & 1][0], (int)p[n & 1][1], (int)p[n & 1][2], (int)p[n & 1][3]};
+#pragma unroll
+      for (int db = 0; db < ND; ++db) {
+        pin();
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[n & 1][db]),
+                                                        __builtin_bit_cast(bf16x8, pn), o[db], 0, 0, 0);
+        if (n + 1 < N) {
+          vf[(n + 1) & 1][db] = v_operand16<HD>(v, at, n + 1, db);
+          if (ND == 4) {
+            weights(n + 1, db);
+          } else {
+            weights(n + 1, 2 * db);
+            weights(n + 1, 2 * db + 1);
+          }
+        }
       }
     }
-  }
-};
-
-// O^T += V^T P^T over a tile.
-template <typename T, int HD>
-__device__ __forceinline__ void many_pv(const char* v, const LanePlaces<T, HD>& at, const Weights<T>& w,
-                                        f32x16 (&o)[HD / 32]) {
-  constexpr int ND = HD / 32;
+  } else {
 #pragma unroll
-  for (int n = 0; n < Weights<T>::N; ++n) {
-    if constexpr (sizeof(T) == 2) {
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], scale2, -sub));
+        ls[r & 3] = ls[r & 3] + s[kb][r];
+      }
+#pragma unroll
+    for (int r = 0; r < 16 * KB; ++r) {
+      const char* p = v + at.val32(r / 4, r % 4);
+      float x[ND];
+      if constexpr (ND == 4) {
+        const float4 f = *reinterpret_cast<const float4*>(p);
+        x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w;
+      } else {
+        const float2 f = *reinterpret_cast<const float2*>(p);
+        x[0] = f.x, x[1] = f.y;
+      }
 #pragma unroll
       for (int db = 0; db < ND; ++db)
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand16<HD>(v, at, n, db)),
-                                                        __builtin_bit_cast(bf16x8, w.p[n]), o[db], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const char* p = v + at.val32(n, j);
-        const float pj = __int_as_float(j == 0 ? w.p[n].x : j == 1 ? w.p[n].y : j == 2 ? w.p[n].z : w.p[n].w);
-        float x[ND];
-        if constexpr (ND == 4) {
-          const float4 f = *reinterpret_cast<const float4*>(p);
-          x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w;
-        } else {
-          const float2 f = *reinterpret_cast<const float2*>(p);
-          x[0] = f.x, x[1] = f.y;
-        }
-#pragma unroll
-        for (int db = 0; db < ND; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[db], pj, o[db], 0, 0, 0);
-      }
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[db], s[r / 16][r % 16], o[db], 0, 0, 0);
     }
   }
+  l = l + ((ls[0] + ls[1]) + (ls[2] + ls[3]));
 }
 
 // One tile for one wave.  held: its positions that the cache has and some query of the
@@ -625,24 +681,7 @@ __device__ __forceinline__ void many_tile(const PagedAttnArgs& a, ManyState<T, H
   const int h = lane >> 5;
   at.renew();
   f32x16 s[KB];
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-#pragma unroll
-    for (int i = 0; i < ManyState<T, HD>::QR; ++i) {
-      const int4 x = ld16(k + at.key(kb, i));
-      if constexpr (sizeof(T) == 2) {
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
-                                                        __builtin_bit_cast(bf16x8, st.q[i]), s[kb], 0, 0, 0);
-      } else {
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.x), __int_as_float(st.q[i].x), s[kb], 0, 0, 0);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.y), __int_as_float(st.q[i].y), s[kb], 0, 0, 0);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.z), __int_as_float(st.q[i].z), s[kb], 0, 0, 0);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(x.w), __int_as_float(st.q[i].w), s[kb], 0, 0, 0);
-      }
-    }
-  }
+  many_scores<T, HD>(k, at, st.q, s);
   uint64_t vis = held;
   if (!whole) {
     vis = (uint64_t)seen_bits(a, base, qpos) | (KB == 2 ? (uint64_t)seen_bits(a, base + 32, qpos) << 32 : 0ull);
@@ -677,17 +716,7 @@ __device__ __forceinline__ void many_tile(const PagedAttnArgs& a, ManyState<T, H
   }
   // a masked score, and every one of a query that has seen nothing yet, weighs nothing
   const float sub = st.m == -CH_INF ? 0.f : st.m;
-  float ls[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale2, -sub));
-      ls[r & 3] = ls[r & 3] + s[kb][r];
-    }
-  st.l = st.l + ((ls[0] + ls[1]) + (ls[2] + ls[3]));
-  const Weights<T> w(s);
-  many_pv<T, HD>(v, at, w, st.o);
+  many_values<T, HD>(v, at, s, a.scale2, sub, st.l, st.o);
 }
 
 template <typename T, int HD>
