@@ -726,7 +726,10 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
   constexpr int NI = KT * ROW / 4096, RPI = 1024 / ROW;  // loads of a wave, rows of a load
   __shared__ __attribute__((aligned(1024))) char k0[KT * ROW], v0[KT * ROW], k1[KT * ROW], v1[KT * ROW];
   const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
-  const int split = rest % a.splits, slot = a.slots - 1 - rest / a.splits;  // later blocks see more: first
+  // later blocks see more: those first, and then the others from the other end, so that
+  // a CU's second workgroup is short where its first is long
+  const int split = rest % a.splits, nth = rest / a.splits, lead = a.slots - a.slots / 2;
+  const int slot = nth < lead ? a.slots - 1 - nth : nth - lead;
   const QueryBlock blk = many_block(c, a, slot);
   if (blk.count == 0) return;
   const Span<KT> span(c, a, blk);
