@@ -762,16 +762,28 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
     for (int r = 0; r < 16; ++r) st.o[db][r] = 0.f;
 
   // A lane finds the row of one position of a tile; one that no query sees is read as
-  // the last position's.
+  // the last position's.  Its page is asked for before the loads of the tile before it
+  // are: loads are waited for in order.
   const int p_end = min(span.p_hi, c.cap - 1);
   uint32_t row_next;
   uint64_t held_next;
-  auto find = [&](int t) {
+  int page = 0, slot_in = 0;
+  bool seen = false;
+  auto ask = [&](int t) {
     const int pos = span.tile(t) * KT + (lane & (KT - 1));
-    const bool seen = some_see(a, pos, span.p_lo, span.p_hi);
-    const uint32_t row = paged_row(c, ptab, seen ? pos : p_end);
-    held_next = __ballot(seen && row != PAGED_NONE) & low_bits64(KT);
-    row_next = row == PAGED_NONE ? 0u : row;
+    seen = some_see(a, pos, span.p_lo, span.p_hi) && pos < c.cap;
+    const int p = seen ? pos : p_end, pi = c.ps.quot(p);
+    slot_in = p - pi * c.ps.d;
+    page = ptab[pi];
+  };
+  auto settle = [&]() {
+    const bool there = page >= 0 && page < c.n_pages;
+    held_next = __ballot(seen && there) & low_bits64(KT);
+    row_next = there ? (uint32_t)page * c.page_rows + (uint32_t)slot_in : 0u;
+  };
+  auto find = [&](int t) {
+    ask(t);
+    settle();
   };
   auto load = [&](char* k, char* v) {
 #pragma unroll
@@ -797,11 +809,12 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
     tile_barrier();
     const uint64_t mine = held;
     if (t + 1 < t1) {
+      if (t + 2 < t1) ask(t + 2);
       load(kn, vn);
       held = held_next;
-      if (t + 2 < t1) find(t + 2);
     }
     if (on) many_tile<T, HD>(a, st, k, v, at, span.tile(t) * KT, mine, blk.n + qrow, p_lo, p_hi, lane, odd);
+    if (t + 2 < t1) settle();
   };
   for (int t = t0; t < t1; t += 2) {
     step(t, k0, v0, k1, v1);
