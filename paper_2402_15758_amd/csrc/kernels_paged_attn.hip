@@ -19,10 +19,6 @@ struct QueryBlock {
 };
 __device__ __forceinline__ int clamp_row(const PagedAttnArgs& a, int r) { return min(max(r, 0), a.rows); }
 
-// A sequence whose queries of one cache head are few goes to the kernel for few, the
-// others to the tiled one: TODO both sides measured.
-constexpr int FEW = 64;
-
 __device__ __forceinline__ void seq_rows(const PagedAttnArgs& a, int b, int& row0, int& rows) {
   row0 = b, rows = 1;
   if (a.row0 != nullptr) {
@@ -39,39 +35,49 @@ __device__ __forceinline__ QueryBlock few_block(const PagedAttnArgs& a, int slot
   seq_rows(a, k.b, k.row0, rows);
   const int queries = rows * a.group;
   k.v0 = (slot - k.b * a.per) * 16;
-  k.count = queries > FEW ? 0 : max(min(queries - k.v0, 16), 0);
+  k.count = queries > a.few ? 0 : max(min(queries - k.v0, 16), 0);
   k.n = min(a.n_b[k.b], 1 << 30);
   return k;
 }
-// Block `slot` of 128 queries.  All lanes of a wave; the result is uniform.
+// Block `slot` of 128 queries: sequence b's slots start at floor(row0[b] group / 128) + b,
+// which leaves each room for its own.  All lanes of a wave; the result is uniform.
 __device__ __forceinline__ QueryBlock many_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
   constexpr int BQ = 128;
   QueryBlock k;
-  int rows, at;
+  int rows = 1, at;
   if (a.row0 == nullptr) {
     const int per = (a.group + BQ - 1) / BQ;
     k.b = slot / per;
     at = slot - k.b * per;
+    k.row0 = k.b;
+    k.n = a.n_b[k.b];
   } else {
-    // the last sequence whose slots start at or before this one, 64 looked at at once
+    // the last sequence whose slots start at or before this one, 64 looked at at once;
+    // the last look brings all that is needed of it
     const int lane = threadIdx.x & 63;
     int lo = 0, len = c.B;
-    do {
-      const int step = (len + 63) / 64, i = lo + lane * step;
-      const bool before =
-          lane * step < len && (int)((int64_t)clamp_row(a, a.row0[i]) * a.group / BQ) + i <= slot;
-      const int skip = max(__popcll(__ballot(before)) - 1, 0) * step;
-      lo += skip;
-      len = min(step, len - skip);
-    } while (len > 1);
-    k.b = __builtin_amdgcn_readfirstlane(lo);
-    at = slot - ((int)((int64_t)clamp_row(a, a.row0[k.b]) * a.group / BQ) + k.b);
+    for (;;) {
+      const int step = (len + 63) / 64, i = lo + min(lane * step, len - 1);
+      const int r = clamp_row(a, a.row0[i]);
+      const int start = (int)((int64_t)r * a.group / BQ) + i;
+      const int last = max(__popcll(__ballot(lane * step < len && start <= slot)) - 1, 0);
+      if (step == 1) {
+        const int end = clamp_row(a, a.row0[i + 1]), n = a.n_b[i];
+        k.b = lo + last;
+        k.row0 = __builtin_amdgcn_readlane(r, last);
+        k.n = __builtin_amdgcn_readlane(n, last);
+        rows = max(__builtin_amdgcn_readlane(end, last) - k.row0, 0);
+        at = slot - __builtin_amdgcn_readlane(start, last);
+        break;
+      }
+      lo += last * step;
+      len = min(step, len - last * step);
+    }
   }
-  seq_rows(a, k.b, k.row0, rows);
   const int queries = rows * a.group;
+  k.n = min(k.n, 1 << 30);
   k.v0 = at * BQ;
-  k.count = queries <= FEW || at < 0 ? 0 : max(min(queries - k.v0, BQ), 0);
-  k.n = min(a.n_b[k.b], 1 << 30);
+  k.count = queries <= a.few || at < 0 ? 0 : max(min(queries - k.v0, BQ), 0);
   return k;
 }
 
@@ -147,12 +153,13 @@ __device__ __forceinline__ uint32_t odd_row(const T* p) {
   }
   return odd;
 }
-// Whether `bytes` of a tile of V in LDS hold an infinity or a NaN; a wave.
-template <typename T>
-__device__ __forceinline__ bool odd_tile(const char* v, int bytes, int lane) {
+// Whether a tile of V in LDS holds an infinity or a NaN; a wave.
+template <typename T, int BYTES>
+__device__ __forceinline__ bool odd_tile(const char* v, int lane) {
   uint32_t odd = 0;
-  for (int i = lane * 16; i < bytes; i += 1024) {
-    const int4 x = ld16(v + i);
+#pragma unroll
+  for (int i = 0; i < BYTES; i += 1024) {
+    const int4 x = ld16(v + i + lane * 16);
     odd |= odd_bits<T>(x.x) | odd_bits<T>(x.y) | odd_bits<T>(x.z) | odd_bits<T>(x.w);
   }
   return __ballot(odd != 0) != 0;
@@ -486,7 +493,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int TB = 128;         // queries of a workgroup
 template <typename T>
 constexpr int TT = sizeof(T) == 2 ? 64 : 32;  // positions of a tile
-constexpr int T_LEAST = 4;      // tiles of a part
+constexpr int T_LEAST = 8;      // tiles of a part
 
 template <int CH>  // chunks of a row
 __device__ __forceinline__ int swizzle(int row) {
@@ -674,7 +681,7 @@ __device__ __forceinline__ void many_tile(const PagedAttnArgs& a, ManyState<T, H
   // nothing of it for this wave: past its queries, or before their window
   if (base > p_hi || (a.window > 0 && base + KT - 1 <= p_lo - a.window && base >= a.sinks)) return;
   const bool whole = held == low_bits64(KT) && all_see(a, base, base + KT - 1, p_lo, p_hi);
-  if (!whole && odd_tile<T>(v, KT * ROW, lane)) {
+  if (!whole && odd_tile<T, KT * ROW>(v, lane)) {
     odd = true;
     return;
   }
@@ -896,65 +903,158 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
   if (h == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = float2{st.m, lt};
 }
 
-// The parts of a query, joined in order: a wave a query, 64 parts' factors at once.
+// The parts of a query, joined in a fixed order.  Up to JOIN_FEW of them: 16 queries a
+// workgroup, 16 threads a query, all parts on their way at once.  More: a workgroup a
+// query, each wave every fourth part, eight on their way at once.
+constexpr int JOIN_FEW = 8;
+
 template <typename T, int HD, int BQ, int TILE>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, const PagedAttnArgs a, int least) {
-  const int q0 = blockIdx.x * 4 + (threadIdx.x >> 6);  // query of a slot and cache head
-  const int q = q0 % BQ, kvh = q0 / BQ % c.H, slot = q0 / BQ / c.H;
-  const int lane = threadIdx.x & 63;
+  constexpr int D = HD / 16;
+  const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
+  const int q = rest % (BQ / 16) * 16 + threadIdx.x / 16, slot = rest / (BQ / 16);
   const QueryBlock blk = BQ == RB ? few_block(a, slot) : many_block(c, a, slot);
-  if (q >= blk.count) return;
   const Span<TILE> span(c, a, blk);
   const int parts = parts_of(span.tiles, a.splits, least);
-  if (parts == 1) return;  // written whole
+  if (q >= blk.count || parts == 1) return;  // no query, or written whole
+  const int64_t first = ((int64_t)slot * c.H + kvh) * a.splits * BQ + q;
+  const float* po = a.part_o + first * HD + threadIdx.x % 16 * D;
+  float2 ml[JOIN_FEW];
+  float4 o[JOIN_FEW][D / 4];
+#pragma unroll
+  for (int i = 0; i < JOIN_FEW; ++i) {
+    const int k = min(i, parts - 1);
+    ml[i] = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)k * BQ) * 2);
+#pragma unroll
+    for (int j = 0; j < D / 4; ++j) o[i][j] = *reinterpret_cast<const float4*>(po + (int64_t)k * BQ * HD + 4 * j);
+  }
+  float mt = ml[0].x;
+#pragma unroll
+  for (int i = 1; i < JOIN_FEW; ++i) mt = fmaxf(mt, ml[i].x);
+  float lt = 0.f, x[D];
+#pragma unroll
+  for (int j = 0; j < D; ++j) x[j] = 0.f;
+#pragma unroll
+  for (int i = 0; i < JOIN_FEW; ++i) {
+    if (i >= parts || ml[i].x == -CH_INF) continue;  // not there, or nothing seen
+    const float f = __builtin_amdgcn_exp2f(ml[i].x - mt);
+    lt = fmaf(ml[i].y, f, lt);
+#pragma unroll
+    for (int j = 0; j < D / 4; ++j) {
+      x[4 * j] = fmaf(o[i][j].x, f, x[4 * j]);
+      x[4 * j + 1] = fmaf(o[i][j].y, f, x[4 * j + 1]);
+      x[4 * j + 2] = fmaf(o[i][j].z, f, x[4 * j + 2]);
+      x[4 * j + 3] = fmaf(o[i][j].w, f, x[4 * j + 3]);
+    }
+  }
+  const int r = (blk.v0 + q) / a.group, h = blk.v0 + q - r * a.group;
+#pragma unroll
+  for (int j = 0; j < D; ++j) x[j] = mt == -CH_INF ? 0.f : x[j] / lt;
+  store_out<T, D>((T*)a.out + (int64_t)(blk.row0 + r) * a.ldo + (kvh * a.group + h) * HD + threadIdx.x % 16 * D, x,
+                  a.vec_out != 0);
+}
+
+template <typename T, int HD, int BQ, int TILE>
+__global__ __launch_bounds__(256) void paged_join_many_kernel(const PagedView c, const PagedAttnArgs a, int least) {
+  constexpr int D = HD / 64, U = 8, W = 4;
+  const int nth = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int q = blockIdx.x % BQ, kvh = blockIdx.x / BQ % c.H, slot = blockIdx.x / BQ / c.H;
+  const QueryBlock blk = BQ == RB ? few_block(a, slot) : many_block(c, a, slot);
+  const Span<TILE> span(c, a, blk);
+  const int parts = parts_of(span.tiles, a.splits, least);
+  if (q >= blk.count || parts == 1) return;  // for the whole workgroup alike
   const int64_t first = ((int64_t)slot * c.H + kvh) * a.splits * BQ + q;
   float mt = -CH_INF;
   for (int i = lane; i < parts; i += 64) mt = fmaxf(mt, a.part_ml[(first + (int64_t)i * BQ) * 2]);
   mt = wave_max(mt);
-  constexpr int D = HD / 64;
   float lt = 0.f, x[D];
 #pragma unroll
   for (int j = 0; j < D; ++j) x[j] = 0.f;
-  for (int i0 = 0; i0 < parts; i0 += 64) {
+  const float* po = a.part_o + first * HD + lane * D;
+  for (int i0 = nth; i0 < parts; i0 += 64 * W) {  // 64 of this wave's parts
+    const int n = min(64, (parts - i0 + W - 1) / W);
     float f = 0.f, fl = 0.f;
-    if (i0 + lane < parts) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)(i0 + lane) * BQ) * 2);
+    if (lane < n) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)(i0 + lane * W) * BQ) * 2);
       f = weight(ml.x, mt);
-      fl = f == 0.f && ml.x == -CH_INF ? 0.f : ml.y * f;
+      fl = ml.x == -CH_INF ? 0.f : ml.y * f;
     }
     lt = lt + wave_sum(fl);
-    const int n = min(64, parts - i0);
-    for (int i = 0; i < n; ++i) {
-      const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i));
-      const float* p = a.part_o + (first + (int64_t)(i0 + i) * BQ) * HD + lane * D;
+    for (int i = 0; i < n; i += U) {
+      float v[U][D];
 #pragma unroll
-      for (int j = 0; j < D; ++j) x[j] = fmaf(p[j], fi, x[j]);
+      for (int k = 0; k < U; ++k) {
+        const float* p = po + (int64_t)(i0 + min(i + k, n - 1) * W) * BQ * HD;
+#pragma unroll
+        for (int j = 0; j < D; ++j) v[k][j] = p[j];
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        // past n: the last part read again, and nothing of it (0 of an infinity is a NaN)
+        const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), min(i + k, 63)));
+#pragma unroll
+        for (int j = 0; j < D; ++j) x[j] = fmaf(i + k < n ? v[k][j] : 0.f, fi, x[j]);
+      }
     }
   }
+  __shared__ float xsh[W][HD], lsh[W];
+#pragma unroll
+  for (int j = 0; j < D; ++j) xsh[nth][lane * D + j] = x[j];
+  if (lane == 0) lsh[nth] = lt;
+  __syncthreads();
+  if (nth != 0) return;
+#pragma unroll
+  for (int j = 0; j < D; ++j)
+    x[j] = (xsh[0][lane * D + j] + xsh[1][lane * D + j]) + (xsh[2][lane * D + j] + xsh[3][lane * D + j]);
+  lt = (lsh[0] + lsh[1]) + (lsh[2] + lsh[3]);
   const int r = (blk.v0 + q) / a.group, h = blk.v0 + q - r * a.group;
   T* dst = (T*)a.out + (int64_t)(blk.row0 + r) * a.ldo + (kvh * a.group + h) * HD + lane * D;
 #pragma unroll
   for (int j = 0; j < D; ++j) dst[j] = ET<T>::from_f(mt == -CH_INF ? 0.f : x[j] / lt);
 }
 
+template <typename T, int HD, int BQ, int TILE>
+void join_go(const PagedView& c, const PagedAttnArgs& a, int least, hipStream_t st) {
+  const unsigned blocks = (unsigned)(a.slots * c.H);
+  if (a.splits > JOIN_FEW)
+    hipLaunchKernelGGL((paged_join_many_kernel<T, HD, BQ, TILE>), dim3(blocks * BQ), dim3(256), 0, st, c, a, least);
+  else
+    hipLaunchKernelGGL((paged_join_kernel<T, HD, BQ, TILE>), dim3(blocks * (BQ / 16)), dim3(256), 0, st, c, a, least);
+}
+
 // ---- deal ------------------------------------------------------------------------
 constexpr int R_WGS = 1024;  // workgroups that fill the card: four a CU
 constexpr int T_WGS = 512;   // two a CU
+constexpr double FEW_FLOPS = 2.5e9;
 
 // Parts of a block's positions: as many as fill the card, none of them short.
 int64_t deal_splits(int64_t cap, int64_t blocks, int wgs, int tile, int least) {
   const int64_t tiles = (cap + tile - 1) / tile + 2;  // a window's ends cut two more
-  return std::max<int64_t>(1, std::min((wgs + blocks - 1) / blocks, (tiles + least - 1) / least));
+  return std::max<int64_t>(1, std::min((wgs + blocks / 2) / blocks, (tiles + least - 1) / least));
 }
-// Partials of any call of up to `blocks` blocks: less than one round over the card
-// more than the blocks, or every block's most.
+// Partials of any call of up to `blocks` blocks: half a round over the card more than
+// one at most, or every block's most.
 int64_t deal_slots(int64_t cap, int64_t blocks, int wgs, int tile, int least) {
-  return std::min(std::min<int64_t>(blocks, wgs) * deal_splits(cap, 1, 1 << 30, tile, least), (int64_t)2 * wgs);
+  return std::min<int64_t>(std::min<int64_t>(blocks, wgs) * deal_splits(cap, 1, 1 << 30, tile, least), wgs + wgs / 2);
 }
 
-int64_t few_per(bool single, int rows, int group) {
-  const int64_t queries = single ? group : std::min<int64_t>((int64_t)rows * group, FEW);
-  return (std::min<int64_t>(queries, FEW) + RB - 1) / RB;
+// Sequences of up to this many queries of a cache head go to the kernel for few.
+int few_queries(const PagedView& c, const PagedAttnArgs& a) {
+#ifdef FORCE_FEW
+  return FORCE_FEW;
+#else
+  const bool single = a.row0 == nullptr;
+  const int64_t most = single ? a.group : (int64_t)a.rows * a.group;
+  if (most <= RB) return RB;
+  const int64_t seen = a.window > 0 ? std::min<int64_t>(c.cap, (int64_t)a.window + a.sinks) : c.cap;
+  const double flops = 4.0 * a.rows * a.Hq * c.hd * (double)seen;
+  if (flops <= FEW_FLOPS) return (int)std::min<int64_t>(most, INT32_MAX);
+  return c.B == 1 && !single ? 0 : RB;
+#endif
+}
+int64_t few_slots(bool single, int rows, int batch, int group, int64_t few) {
+  const int64_t queries = single ? group : std::min<int64_t>((int64_t)rows * group, few);
+  return (std::min<int64_t>(queries, few) + RB - 1) / RB * batch;
 }
 int64_t many_slots(bool single, int64_t rows, int batch, int group) {
   return single ? (int64_t)batch * ((group + TB - 1) / TB) : rows * group / TB + batch;
@@ -965,10 +1065,11 @@ void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
   const bool single = a.row0 == nullptr;
   const int64_t most = single ? a.group : (int64_t)a.rows * a.group;  // queries of a sequence
   float* at = (float*)ws;
-  if (!single || most <= FEW) {
+  a.few = few_queries(c, a);
+  if (a.few > 0 && (!single || most <= a.few)) {
     PagedAttnArgs f = a;
-    f.per = (int)few_per(single, a.rows, a.group);
-    f.slots = c.B * f.per;
+    f.slots = (int)few_slots(single, a.rows, c.B, a.group, a.few);
+    f.per = f.slots / c.B;
     f.splits = (int)deal_splits(c.cap, (int64_t)f.slots * c.H, R_WGS, RT, R_LEAST);
     const int64_t parts = (int64_t)f.slots * c.H * f.splits;
     f.part_o = at;
@@ -976,28 +1077,24 @@ void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
     hipLaunchKernelGGL((paged_rows_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, f);
     if (f.splits > 1) {
       at = f.part_ml + parts * RB * 2;
-      hipLaunchKernelGGL((paged_join_kernel<T, HD, RB, RT>), dim3((unsigned)(f.slots * c.H * RB / 4)), dim3(256), 0, st, c,
-                         f, R_LEAST);
+      join_go<T, HD, RB, RT>(c, f, R_LEAST, st);
     }
   }
-  if (most > FEW) {
+  if (most > a.few) {
     a.slots = (int)many_slots(single, a.rows, c.B, a.group);
     a.splits = (int)deal_splits(c.cap, (int64_t)a.slots * c.H, T_WGS, TT<T>, T_LEAST);
     const int64_t parts = (int64_t)a.slots * c.H * a.splits;
     a.part_o = at;
     a.part_ml = at + parts * TB * HD;
     hipLaunchKernelGGL((paged_tiles_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
-    if (a.splits > 1)
-      hipLaunchKernelGGL((paged_join_kernel<T, HD, TB, TT<T>>), dim3((unsigned)(a.slots * c.H * TB / 4)), dim3(256), 0, st,
-                         c, a, T_LEAST);
+    if (a.splits > 1) join_go<T, HD, TB, TT<T>>(c, a, T_LEAST, st);
   }
 }
 
 }  // namespace
 
 int64_t paged_attn_bytes(int64_t cap, int rows, int batch, int group, int H, int hd, int es) {
-  const int64_t few = (int64_t)batch * std::max(few_per(false, rows, group), few_per(true, rows, group)) * H;
-  const int64_t many = std::max(many_slots(false, rows, batch, group), many_slots(true, rows, batch, group)) * H;
+  const int64_t few = R_WGS, many = std::max(many_slots(false, rows, batch, group), many_slots(true, rows, batch, group)) * H;
   const int tile = es == 2 ? TT<bf16_t> : TT<float>;
   return (deal_slots(cap, few, R_WGS, RT, R_LEAST) * RB + deal_slots(cap, many, T_WGS, tile, T_LEAST) * TB) * (hd + 2) * 4;
 }

@@ -77,6 +77,7 @@ struct PagedAttnArgs {
   // a launch's own: parts of a block's positions at most, blocks of queries of one cache
   // head, those of a sequence in the kernel for few queries
   int splits, slots, per;
+  int few;                  // queries of a sequence that the kernel for few takes
   int vec_out;              // out rows at multiples of 16 bytes
   float* part_o;            // [slots][H][splits][block][hd]
   float* part_ml;           // [slots][H][splits][block][2]
