@@ -18,19 +18,19 @@ struct AcceptArgs {
   const int* tokens;        // [B][N]
   const double* u;          // [B][N]
   int B, N, V, K;           // K: the tree's depth
-  double inv_T;
+  double scale;             // 32 / (temperature ln 2)
   int* new_tokens;          // [B][K + 1]
   int* n_new;               // [B]
   int* path;                // [B][K + 1], nullptr: not wanted
   int parts;                // of a row
-  // scratch: each part's maximum and sum of exp((z - maximum) inv_T), target rows
+  // scratch: each part's maximum and sum of exp((z - maximum) / temperature), target rows
   // then draft rows; the residual's parts
   float* part_m;            // [2][B N][parts]
   double* part_s;
   double* resid;            // [B][parts]
   AcceptTree tree;
 };
-constexpr int ACCEPT_PART = 4096;  // entries of a part
+constexpr int ACCEPT_PART = 1024;  // entries of a part: 16 a lane
 int64_t accept_bytes(int B, int N, int V, bool drawn);
 void accept_carve(AcceptArgs& a, void* ws);
 void launch_accept(int dtype, const AcceptArgs& a, hipStream_t st);

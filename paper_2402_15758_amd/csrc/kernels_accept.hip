@@ -13,29 +13,38 @@
 
 namespace {
 
-// e^x for x <= 0 (or NaN), relative error below 2^-50: x = n ln 2 + r, |r| <= ln 2 / 2,
-// with ln 2 in two parts, and Taylor's series of e^r up to r^12 / 12! (the next term is
-// below 2^-52 / 8).  0 from -745.2 on.
-__device__ __forceinline__ double exp_neg(double x) {
-  const double y = fmax(x, -800.0);
-  const double n = rint(y * 1.4426950408889634074);
-  double r = fma(n, -0x1.62e42fee00000p-1, y);
-  r = fma(n, -0x1.a39ef35793c76p-33, r);
-  double p = 1.0 / 479001600.0;
-  p = fma(p, r, 1.0 / 39916800.0);
-  p = fma(p, r, 1.0 / 3628800.0);
-  p = fma(p, r, 1.0 / 362880.0);
-  p = fma(p, r, 1.0 / 40320.0);
-  p = fma(p, r, 1.0 / 5040.0);
-  p = fma(p, r, 1.0 / 720.0);
-  p = fma(p, r, 1.0 / 120.0);
-  p = fma(p, r, 1.0 / 24.0);
-  p = fma(p, r, 1.0 / 6.0);
-  p = fma(p, r, 0.5);
-  p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  return ldexp(p, (int)n);
+// 2^(y / 32) for y <= 0: y = n + f, |f| <= 1/2, 2^(n / 32) = 2^(n >> 5) times a table's
+// entry, and Taylor's series of e^(f ln 2 / 32) up to the fifth power (the next is below
+// 2^-48).  A weight is exp((z - m) / T) = 2^(y / 32) with y = (z - m) 32 / (T ln 2): the
+// sum of a row's errors stays below 2^-47 of its weights.  0 from 2^-1100 on.
+__device__ const double POW32[32] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+constexpr double LN2_32[5] = {0x1.62e42fefa39efp-6, 0x1.ebfbdff82c58fp-13, 0x1.c6b08d704a0c0p-20, 0x1.3b2ab6fba4e77p-27, 0x1.5d87fe78a6731p-35};  // (ln 2 / 32)^k / k!
+
+__device__ __forceinline__ void fill_table(double* table) {  // LDS, [32]
+  if (threadIdx.x < 32) table[threadIdx.x] = POW32[threadIdx.x];
 }
+__device__ __forceinline__ double pow32(double y, const double* table) {
+  y = fmax(y, -35200.0);
+  const double n = rint(y), f = y - n;
+  const int i = (int)n;
+  double p = LN2_32[4];
+  p = fma(p, f, LN2_32[3]);
+  p = fma(p, f, LN2_32[2]);
+  p = fma(p, f, LN2_32[1]);
+  p = fma(p, f, LN2_32[0]);
+  const double t = table[i & 31];
+  return ldexp(fma(p * f, t, t), i >> 5);
+}
+// (z - m) 32 / (T ln 2); scale: 32 / (T ln 2), at most 2^156
+__device__ __forceinline__ double exponent(float z, double m, double scale) { return ((double)z - m) * scale; }
 
 __device__ __forceinline__ double shfl_f64(double v, int lane) {
   const uint64_t u = (uint64_t)__double_as_longlong(v);
@@ -63,59 +72,82 @@ template <typename T>
 __device__ __forceinline__ float logit(const void* row, int64_t i) {
   return ET<T>::to_f(((const T*)row)[i]);
 }
+// Sixteen of a part's entries a lane, -inf past n; VEC: 16 bytes at once.  Lane l holds
+// entries l * E + 64 E i + e of run i, E = 16 / sizeof(T) (1 without VEC).
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_part(const T* z, int n, int lane, float (&x)[16]) {
+  constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
+#pragma unroll
+  for (int i = 0; i < 16 / E; ++i) {
+    const int v = lane * E + 64 * E * i;
+    if (VEC && v + E <= n) {
+      const int4 w = ld16(z + v);
+      if constexpr (sizeof(T) == 4) {
+        x[4 * i] = __int_as_float(w.x), x[4 * i + 1] = __int_as_float(w.y);
+        x[4 * i + 2] = __int_as_float(w.z), x[4 * i + 3] = __int_as_float(w.w);
+      } else {
+        const uint32_t u[4] = {(uint32_t)w.x, (uint32_t)w.y, (uint32_t)w.z, (uint32_t)w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[E * i + 2 * k] = __uint_as_float(u[k] << 16);
+          x[E * i + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[E * i + e] = v + e < n ? ET<T>::to_f(z[v + e]) : -CH_INF;
+    }
+  }
+}
 
 // ---- parts of rows -----------------------------------------------------------------
-// Grid (rows, parts, target | draft).  A thread holds its entries, so a row is read
-// once.  A NaN or +inf makes the part's sum NaN: such a row has no distribution.
-template <typename T>
+// Grid (rows, groups of four parts, target | draft), a wave a part.  A NaN or +inf makes
+// the part's sum NaN: such a row has no distribution.
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
-  constexpr int E = ACCEPT_PART / 256;
-  const int part = blockIdx.y, row = blockIdx.x, tid = threadIdx.x;
+  __shared__ double table[32];
+  fill_table(table);
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const int part = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool of_draft = blockIdx.z != 0;
   const int b = row / a.N;
-  if (a.tokens[(int64_t)b * a.N] < 0) return;  // an empty place
-  const void* z = of_draft ? (const void*)((const T*)a.draft + (int64_t)row * a.ldd)
-                           : (const void*)((const T*)a.logits + (int64_t)row * a.ld);
-  const int v0 = part * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
-  float x[E];
+  const int v0 = part * ACCEPT_PART;
+  const bool on = v0 < a.V && a.tokens[(int64_t)b * a.N] >= 0;
+  const T* z = (of_draft ? (const T*)a.draft + (int64_t)row * a.ldd : (const T*)a.logits + (int64_t)row * a.ld) + v0;
+  float x[16];
+  if (on) load_part<T, VEC>(z, min(ACCEPT_PART, a.V - v0), lane, x);
+  __syncthreads();
+  if (!on) return;
   bool bad = false;
   float m = -CH_INF;
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int v = tid + 256 * i;
-    x[i] = v < n ? logit<T>(z, v0 + v) : -CH_INF;
+  for (int i = 0; i < 16; ++i) {
     bad = bad || !(x[i] < CH_INF);
     m = fmaxf(m, x[i]);
   }
-  __shared__ float msh[4];
-  __shared__ double ssh[4];
   m = wave_max(m);
-  if ((tid & 63) == 0) msh[tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(msh[0], msh[1]), fmaxf(msh[2], msh[3]));
   double s = 0.0;
+  if (m != -CH_INF) {
 #pragma unroll
-  for (int i = 0; i < E; ++i)
-    s = s + (x[i] == -CH_INF ? 0.0 : exp_neg(((double)x[i] - (double)m) * a.inv_T));
+    for (int i = 0; i < 16; ++i) s = s + pow32(exponent(x[i], (double)m, a.scale), table);
+  }
   if (bad) s = __builtin_nan("");
   s = wave_sum_f64(s);
-  if ((tid & 63) == 0) ssh[tid >> 6] = s;
-  __syncthreads();
-  if (tid == 0) {
+  if (lane == 0) {
     const int64_t at = ((int64_t)blockIdx.z * a.B * a.N + row) * a.parts + part;
     a.part_m[at] = m;
-    a.part_s[at] = (ssh[0] + ssh[1]) + (ssh[2] + ssh[3]);
+    a.part_s[at] = s;
   }
 }
 
 // A row's maximum and sum out of its parts, by one wave.  ok: it has a distribution.
 struct RowSum {
   double m, s;
-  bool ok;
+  __device__ __forceinline__ bool ok() const { return s > 0.0 && s < HUGE_VAL && m < (double)CH_INF; }
 };
-__device__ __forceinline__ RowSum row_sum(const AcceptArgs& a, int64_t row, bool of_draft) {
+__device__ __forceinline__ RowSum row_sum(const AcceptArgs& a, int64_t row, const double* table) {
   const int lane = threadIdx.x & 63;
-  const int64_t at = ((of_draft ? (int64_t)a.B * a.N : 0) + row) * a.parts;
+  const int64_t at = row * a.parts;
   float m = -CH_INF;
   for (int i = lane; i < a.parts; i += 64) m = fmaxf(m, a.part_m[at + i]);
   m = wave_max(m);
@@ -123,134 +155,157 @@ __device__ __forceinline__ RowSum row_sum(const AcceptArgs& a, int64_t row, bool
   for (int i = lane; i < a.parts; i += 64) {
     const float pm = a.part_m[at + i];
     const double ps = a.part_s[at + i];
-    s = s + (pm == -CH_INF ? ps : ps * exp_neg(((double)pm - (double)m) * a.inv_T));
+    s = s + (pm == -CH_INF ? ps : ps * pow32(exponent(pm, (double)m, a.scale), table));
   }
-  s = wave_sum_f64(s);
-  return {(double)m, s, s > 0.0 && s < HUGE_VAL && m < CH_INF};
+  return {(double)m, wave_sum_f64(s)};
 }
 
 // ---- the walk ----------------------------------------------------------------------
 // Lane u holds node u.  From the root down: a node's children are tested in the order
 // of their ids; the walk goes on at the first accepted one and ends where there is
-// none.  One wave; the result is uniform.
+// none.  All rows' sums and all nodes' probabilities come first, so the walk itself
+// touches no memory.
 struct Walk {
   int node, depth;          // node -1: an empty place
   bool ok;                  // the last row has a distribution
   uint64_t path, rejected;  // nodes on the path; rejected children of the last one
   RowSum p, q;              // of the last row
 };
-template <typename T>
-__device__ Walk accept_walk(const AcceptArgs& a, int b) {
-  const int lane = threadIdx.x & 63;
-  uint32_t pw = a.tree.parent[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) pw = lane / 4 == i ? a.tree.parent[i] : pw;
-  const int parent = lane == 0 ? -1 : (int)(pw >> (8 * (lane & 3))) & 255;
+struct WalkSpace {
+  double table[32];
+  RowSum rows[2][64];
+  Walk walk;
+};
+// By WAVES waves; ends with a barrier.
+template <typename T, int WAVES>
+__device__ void accept_walk(const AcceptArgs& a, int b, WalkSpace& sh) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row0 = (int64_t)b * a.N;
+  const bool drawn = a.draft != nullptr;
   const int tok = lane < a.N ? a.tokens[row0 + lane] : -1;
   const double u = lane < a.N ? a.u[row0 + lane] : 0.0;
-  Walk w{};
-  if (__builtin_amdgcn_readfirstlane(tok) < 0) {
-    w.node = -1;
-    return w;
-  }
-  const bool named = lane > 0 && lane < a.N && tok >= 0 && tok < a.V;
-  w.path = 1;
-  for (;;) {
-    w.rejected = 0;
-    w.p = row_sum(a, row0 + w.node, false);
-    w.ok = w.p.ok;
-    if (!w.ok) return w;
-    uint64_t kids = __ballot(named && parent == w.node);
-    if (kids == 0) return w;
-    if (a.draft != nullptr) {
-      w.q = row_sum(a, row0 + w.node, true);
-      w.ok = w.q.ok;
-      if (!w.ok) return w;
+  const bool empty = __builtin_amdgcn_readfirstlane(tok) < 0;
+  fill_table(sh.table);
+  __syncthreads();
+  if (!empty)
+    for (int i = wave; i < (drawn ? 2 : 1) * a.N; i += WAVES) {
+      const int z = i >= a.N ? 1 : 0, r = i - z * a.N;
+      const RowSum s = row_sum(a, z * (int64_t)a.B * a.N + row0 + r, sh.table);
+      if (lane == 0) sh.rows[z][r] = s;
     }
-    double p = 0.0, q = 1.0;
-    if ((kids >> lane) & 1) {
-      const double z = (double)logit<T>((const T*)a.logits + (row0 + w.node) * a.ld, tok);
-      p = exp_neg((z - w.p.m) * a.inv_T) / w.p.s;
-      if (a.draft != nullptr) {
-        const double zq = (double)logit<T>((const T*)a.draft + (row0 + w.node) * a.ldd, tok);
-        q = exp_neg((zq - w.q.m) * a.inv_T) / w.q.s;
+  __syncthreads();
+  if (wave == 0) {
+    uint32_t pw = a.tree.parent[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) pw = lane / 4 == i ? a.tree.parent[i] : pw;
+    const int parent = lane == 0 ? -1 : (int)(pw >> (8 * (lane & 3))) & 255;
+    Walk w{};
+    w.node = empty ? -1 : 0;
+    if (!empty) {
+      const bool named = lane > 0 && lane < a.N && tok >= 0 && tok < a.V;
+      double p = 0.0, q = 1.0;
+      if (named) {
+        const RowSum rp = sh.rows[0][parent];
+        p = pow32(exponent(logit<T>((const T*)a.logits + (row0 + parent) * a.ld, tok), rp.m, a.scale), sh.table) / rp.s;
+        if (drawn) {
+          const RowSum rq = sh.rows[1][parent];
+          q = pow32(exponent(logit<T>((const T*)a.draft + (row0 + parent) * a.ldd, tok), rq.m, a.scale), sh.table) / rq.s;
+        }
+      }
+      w.path = 1;
+      for (;;) {
+        w.rejected = 0;
+        w.p = sh.rows[0][w.node];
+        w.ok = w.p.ok();
+        if (!w.ok) break;
+        const uint64_t kids = __ballot(named && parent == w.node);
+        if (kids == 0) break;
+        if (drawn) {
+          w.q = sh.rows[1][w.node];
+          w.ok = w.q.ok();
+          if (!w.ok) break;
+        }
+        double left = 1.0;  // the mass of what is not rejected
+        int next = -1;
+        for (uint64_t rest = kids; rest != 0; rest &= rest - 1) {
+          const int c = __ffsll((long long)rest) - 1;
+          const double pc = shfl_f64(p, c), uc = shfl_f64(u, c);
+          if (uc * (drawn ? shfl_f64(q, c) : left) < pc) {
+            next = c;
+            break;
+          }
+          w.rejected |= 1ull << c;
+          left = left - pc;
+          if (tok == __shfl(tok, c)) p = 0.0;  // a sibling of the same token
+        }
+        if (next < 0) break;
+        w.node = next;
+        w.depth += 1;
+        w.path |= 1ull << next;
       }
     }
-    double left = 1.0;  // the mass of what is not rejected
-    int next = -1;
-    for (uint64_t rest = kids; rest != 0; rest &= rest - 1) {
-      const int c = __ffsll((long long)rest) - 1;
-      const double pc = shfl_f64(p, c), uc = shfl_f64(u, c);
-      if (uc * (a.draft != nullptr ? shfl_f64(q, c) : left) < pc) {
-        next = c;
-        break;
-      }
-      w.rejected |= 1ull << c;
-      left = left - pc;
-      if (tok == __shfl(tok, c)) p = 0.0;  // a sibling of the same token
-    }
-    if (next < 0) return w;
-    w.node = next;
-    w.depth += 1;
-    w.path |= 1ull << next;
+    if (lane == 0) sh.walk = w;
   }
+  __syncthreads();
 }
 
 // ---- the next token ------------------------------------------------------------------
-// Weight of entry v where a walk ended: the target's probability (times the row's sum)
+// Weight of an entry where a walk ended: the target's probability (times the row's sum)
 // where it is not a rejected token, or what the draft leaves of it.
 template <typename T>
 struct Weights {
   const T *z, *zq;          // zq: nullptr without a residual
-  double m, mq, inv_T, scale, scale_q;
+  double m, mq, scale, one, one_q;
+  const double* table;
+  __device__ __forceinline__ double of(float x, float xq) const {
+    const double p = pow32(exponent(x, m, scale), table) * one;
+    return zq == nullptr ? p : fmax(p - pow32(exponent(xq, mq, scale), table) * one_q, 0.0);
+  }
   __device__ __forceinline__ double operator()(int v) const {
-    const double p = exp_neg(((double)ET<T>::to_f(z[v]) - m) * inv_T) * scale;
-    if (zq == nullptr) return p;
-    return fmax(p - exp_neg(((double)ET<T>::to_f(zq[v]) - mq) * inv_T) * scale_q, 0.0);
+    return of(ET<T>::to_f(z[v]), zq == nullptr ? 0.f : ET<T>::to_f(zq[v]));
   }
 };
 
-// Drawn tokens: every part of the residual, grid (parts, sequences).  Each workgroup
-// walks by itself, which is cheaper than a launch between.
-template <typename T>
+// Drawn tokens: every part of the residual, grid (groups of four parts, sequences), a
+// wave a part.  Each workgroup walks by itself, which is cheaper than a launch between.
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void accept_resid_kernel(const AcceptArgs a) {
-  const int part = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-  __shared__ Walk wsh;
-  if (tid < 64) {
-    const Walk w = accept_walk<T>(a, b);
-    if (tid == 0) wsh = w;
-  }
-  __syncthreads();
-  const Walk w = wsh;
-  if (w.node < 0 || !w.ok || w.rejected == 0) return;
+  __shared__ WalkSpace sh;
+  const int b = blockIdx.y, lane = threadIdx.x & 63;
+  const int part = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  accept_walk<T, 4>(a, b, sh);
+  const Walk& w = sh.walk;
+  const int v0 = part * ACCEPT_PART;
+  if (w.node < 0 || !w.ok || w.rejected == 0 || v0 >= a.V) return;
   const int64_t row = (int64_t)b * a.N + w.node;
-  const Weights<T> f{(const T*)a.logits + row * a.ld, (const T*)a.draft + row * a.ldd, w.p.m, w.q.m, a.inv_T,
-                     1.0 / w.p.s, 1.0 / w.q.s};
-  const int v0 = part * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
+  const Weights<T> f{(const T*)a.logits + row * a.ld, (const T*)a.draft + row * a.ldd, w.p.m, w.q.m, a.scale,
+                     1.0 / w.p.s, 1.0 / w.q.s, sh.table};
+  float x[16], xq[16];
+  const int n = min(ACCEPT_PART, a.V - v0);
+  load_part<T, VEC>(f.z + v0, n, lane, x);
+  load_part<T, VEC>(f.zq + v0, n, lane, xq);
   double s = 0.0;
-  for (int v = tid; v < n; v += 256) s = s + f(v0 + v);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s = s + f.of(x[i], xq[i]);
   s = wave_sum_f64(s);
-  __shared__ double ssh[4];
-  if ((tid & 63) == 0) ssh[tid >> 6] = s;
-  __syncthreads();
-  if (tid == 0) a.resid[(int64_t)b * a.parts + part] = (ssh[0] + ssh[1]) + (ssh[2] + ssh[3]);
+  if (lane == 0) a.resid[(int64_t)b * a.parts + part] = s;
 }
 
 // A workgroup of 1024 a sequence: the walk, its results, and the first entry whose
 // running sum passes u[0] of the whole, by parts and then within one.
-template <typename T>
+template <typename T, bool VEC>
 __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row0 = (int64_t)b * a.N;
   const int K1 = a.K + 1;
-  __shared__ Walk wsh;
+  __shared__ WalkSpace sh;
   __shared__ int gone[64], n_gone;       // rejected tokens
   __shared__ double wave_s[16], redo[64];
-  __shared__ int part_sh;
+  __shared__ int part_sh, first_sh[16], last_sh[16];
   __shared__ double before_sh, target_sh;
+  accept_walk<T, 16>(a, b, sh);
+  const Walk w = sh.walk;
   if (tid < 64) {
-    const Walk w = accept_walk<T>(a, b);
     const int tok = lane < a.N ? a.tokens[row0 + lane] : -1;
     const int len = w.node < 0 ? 0 : w.depth + 1;
     if (lane < a.N && w.node >= 0 && ((w.path >> lane) & 1)) {
@@ -264,14 +319,11 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
     }
     if (lane == 0) {
       a.n_new[b] = len;
-      wsh = w;
-      part_sh = -1;
       n_gone = a.draft == nullptr ? __popcll(w.rejected) : 0;
     }
     if (a.draft == nullptr && ((w.rejected >> lane) & 1)) gone[__popcll(w.rejected & ((1ull << lane) - 1))] = tok;
   }
   __syncthreads();
-  const Walk w = wsh;
   if (w.node < 0) return;
   if (!w.ok) {
     if (tid == 0) a.new_tokens[(int64_t)b * K1 + w.depth] = -1;
@@ -279,20 +331,27 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   }
   const int64_t row = row0 + w.node;
   const bool resid = a.draft != nullptr && w.rejected != 0;
-  Weights<T> f{(const T*)a.logits + row * a.ld, resid ? (const T*)a.draft + row * a.ldd : nullptr, w.p.m, w.q.m, a.inv_T,
-               resid ? 1.0 / w.p.s : 1.0, resid ? 1.0 / w.q.s : 1.0};
+  Weights<T> f{(const T*)a.logits + row * a.ld, resid ? (const T*)a.draft + row * a.ldd : nullptr, w.p.m, w.q.m, a.scale,
+               resid ? 1.0 / w.p.s : 1.0, resid ? 1.0 / w.q.s : 1.0, sh.table};
   int ng = n_gone;
-  auto weight_of = [&](int v) {
-    for (int i = 0; i < ng; ++i)
-      if (gone[i] == v) return 0.0;
-    return f(v);
+  auto is_gone = [&](int v) {
+    bool g = false;
+    for (int i = 0; i < ng; ++i) g = g || gone[i] == v;
+    return g;
   };
-  // parts that hold a rejected token are summed without it, a wave each: taking it off
-  // the sum would leave rounding where it was most of it
+  // Parts that hold a rejected token are summed without it, a wave each: taking it off
+  // the sum would leave rounding where it was most of it.
   for (int i = wave; i < ng; i += 16) {
     const int v0 = gone[i] / ACCEPT_PART * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
+    constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
+    float x[16];
+    load_part<T, VEC>(f.z + v0, n, lane, x);
     double s = 0.0;
-    for (int v = lane; v < n; v += 64) s = s + weight_of(v0 + v);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const double one = pow32(exponent(x[k], w.p.m, a.scale), sh.table);
+      s = s + (is_gone(v0 + lane * E + 64 * E * (k / E) + k % E) ? 0.0 : one);
+    }
     s = wave_sum_f64(s);
     if (lane == 0) redo[i] = s;
   }
@@ -308,7 +367,7 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
         for (int j = 0; j < ng; ++j)
           if (gone[j] / ACCEPT_PART == i) return redo[j];
         const float pm = a.part_m[row * a.parts + i];
-        return pm == -CH_INF ? 0.0 : a.part_s[row * a.parts + i] * exp_neg(((double)pm - w.p.m) * a.inv_T);
+        return pm == -CH_INF ? 0.0 : a.part_s[row * a.parts + i] * pow32(exponent(pm, w.p.m, a.scale), sh.table) * f.one;
       };
       double total = 0.0;
       for (int i0 = 0; i0 < a.parts; i0 += 64) total = total + wave_sum_f64(part_weight(i0 + lane));
@@ -339,38 +398,24 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
     __syncthreads();
     ng = 0;
     f.zq = nullptr;
-    f.scale = 1.0;
+    f.one = 1.0;
   }
   if (part_sh < 0) {  // u was no number
     if (tid == 0) a.new_tokens[(int64_t)b * K1 + w.depth] = -1;
     return;
   }
-  // within the part: four entries a thread, in order
-  const int v0 = part_sh * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
-  double x[4], s = 0.0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = 4 * tid + i < n ? weight_of(v0 + 4 * tid + i) : 0.0;
-    s = s + x[i];
-  }
-  const double scan = wave_scan_f64(s);
+  // within the part, an entry a thread
+  static_assert(ACCEPT_PART == 1024, "an entry a thread");
+  const int v = part_sh * ACCEPT_PART + tid;
+  const double x = v < a.V && !is_gone(v) ? f(v) : 0.0;
+  const double scan = wave_scan_f64(x);
   if (lane == 63) wave_s[wave] = scan;
   __syncthreads();
   double run = before_sh;
   for (int i = 0; i < wave; ++i) run = run + wave_s[i];
-  run = run + (scan - s);
-  int mine = 0x7fffffff, pos = -1;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    run = run + x[i];
-    if (x[i] > 0.0) {
-      if (run > target_sh && mine == 0x7fffffff) mine = v0 + 4 * tid + i;
-      pos = v0 + 4 * tid + i;
-    }
-  }
+  run = run + scan;
   // the first that passes; where rounding leaves none, the last with any weight
-  __shared__ int first_sh[16], last_sh[16];
-  const int wf = wave_min_i(mine), wl = -wave_min_i(-pos);
+  const int wf = wave_min_i(x > 0.0 && run > target_sh ? v : 0x7fffffff), wl = -wave_min_i(x > 0.0 ? -v : 1);
   if (lane == 0) first_sh[wave] = wf, last_sh[wave] = wl;
   __syncthreads();
   if (tid == 0) {
@@ -383,13 +428,21 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   }
 }
 
+template <typename T, bool VEC>
+void accept_go(const AcceptArgs& a, hipStream_t st) {
+  const int groups = (a.parts + 3) / 4;
+  hipLaunchKernelGGL((accept_parts_kernel<T, VEC>), dim3(a.B * a.N, groups, a.draft != nullptr ? 2 : 1), dim3(256), 0, st, a);
+  if (a.draft != nullptr && a.N > 1)
+    hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3(groups, a.B), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((accept_pick_kernel<T, VEC>), dim3(a.B), dim3(1024), 0, st, a);
+}
 template <typename T>
 void accept_t(const AcceptArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((accept_parts_kernel<T>), dim3(a.B * a.N, a.parts, a.draft != nullptr ? 2 : 1), dim3(256), 0, st,
-                     a);
-  if (a.draft != nullptr && a.N > 1)
-    hipLaunchKernelGGL((accept_resid_kernel<T>), dim3(a.parts, a.B), dim3(256), 0, st, a);
-  hipLaunchKernelGGL((accept_pick_kernel<T>), dim3(a.B), dim3(1024), 0, st, a);
+  auto whole = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
+  if (whole(a.logits, a.ld) && whole(a.draft, a.draft != nullptr ? a.ldd : 0))
+    accept_go<T, true>(a, st);
+  else
+    accept_go<T, false>(a, st);
 }
 
 int64_t up(int64_t b) { return (b + 255) / 256 * 256; }

@@ -285,7 +285,7 @@ chimera_status chimera_accept(int32_t dtype, const void* logits, int64_t ld, con
     a.B = batch;
     a.N = n_nodes;
     a.V = vocab;
-    a.inv_T = 1.0 / (double)temperature;
+    a.scale = 32.0 / ((double)temperature * 0.69314718055994530942);
     a.new_tokens = new_tokens;
     a.n_new = n_new;
     a.path = path_nodes;
