@@ -10,6 +10,18 @@ struct AcceptTree {
   void set(int u, int p) { parent[u / 4] |= (uint32_t)(u == 0 ? 0 : p) << (8 * (u % 4)); }
 };
 
+// A row's largest logit and its sum of exp((z - largest) / temperature).
+struct RowSum {
+  double m, s;
+};
+// Where a sequence's walk ended.
+struct Walk {
+  int node, depth;          // node -1: an empty place
+  bool ok;                  // the last row has a distribution
+  uint64_t path, rejected;  // nodes on the path; rejected children of the last one
+  RowSum p, q;              // of the last row
+};
+
 struct AcceptArgs {
   const void* logits;       // [B N][ld]
   int64_t ld;
@@ -24,10 +36,12 @@ struct AcceptArgs {
   int* path;                // [B][K + 1], nullptr: not wanted
   int parts;                // of a row
   // scratch: each part's maximum and sum of exp((z - maximum) / temperature), target rows
-  // then draft rows; the residual's parts
+  // then draft rows; the residual's parts; the walks
   float* part_m;            // [2][B N][parts]
   double* part_s;
   double* resid;            // [B][parts]
+  Walk* walks;              // [B]
+  uint64_t inner;           // nodes with children
   AcceptTree tree;
 };
 constexpr int ACCEPT_PART = 1024;  // entries of a part: 16 a lane

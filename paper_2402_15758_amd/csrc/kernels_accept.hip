@@ -51,6 +51,13 @@ __device__ __forceinline__ double shfl_f64(double v, int lane) {
   return __longlong_as_double((long long)((uint64_t)(uint32_t)__shfl((int)(uint32_t)u, lane) |
                                           ((uint64_t)(uint32_t)__shfl((int)(uint32_t)(u >> 32), lane) << 32)));
 }
+// A uniform lane's value, without a trip through LDS.
+__device__ __forceinline__ double lane_f64(double v, int lane) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
 // Over the 64 lanes, in the same order on each.
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
@@ -101,76 +108,85 @@ __device__ __forceinline__ void load_part(const T* z, int n, int lane, float (&x
 }
 
 // ---- parts of rows -----------------------------------------------------------------
-// Grid (rows, groups of four parts, target | draft), a wave a part.  A NaN or +inf makes
-// the part's sum NaN: such a row has no distribution.
-template <typename T, bool VEC>
+// Grid (rows, groups of parts, target | draft), a wave PER parts one after another, the
+// next one's entries on their way while one is summed.  A NaN or +inf makes a part's sum
+// NaN: such a row has no distribution.
+template <typename T, bool VEC, int PER>
 __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
   __shared__ double table[32];
-  fill_table(table);
   const int row = blockIdx.x, lane = threadIdx.x & 63;
-  const int part = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b = row / a.N, node = row - b * a.N;
   const bool of_draft = blockIdx.z != 0;
-  const int b = row / a.N;
-  const int v0 = part * ACCEPT_PART;
-  const bool on = v0 < a.V && a.tokens[(int64_t)b * a.N] >= 0;
-  const T* z = (of_draft ? (const T*)a.draft + (int64_t)row * a.ldd : (const T*)a.logits + (int64_t)row * a.ld) + v0;
-  float x[16];
-  if (on) load_part<T, VEC>(z, min(ACCEPT_PART, a.V - v0), lane, x);
+  // nothing is drawn after a node without children
+  if (of_draft && !((a.inner >> node) & 1)) return;
+  const int first = blockIdx.y * 4 * PER + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const T* z = of_draft ? (const T*)a.draft + (int64_t)row * a.ldd : (const T*)a.logits + (int64_t)row * a.ld;
+  const int root = a.tokens[(int64_t)b * a.N];
+  auto load = [&](int i, float (&x)[16]) {
+    const int v0 = (first + 4 * i) * ACCEPT_PART;
+    if (v0 < a.V) load_part<T, VEC>(z + v0, min(ACCEPT_PART, a.V - v0), lane, x);
+  };
+  float x[2][16];
+  load(0, x[0]);
+  fill_table(table);
   __syncthreads();
-  if (!on) return;
-  bool bad = false;
-  float m = -CH_INF;
+  if (root < 0) return;  // an empty place
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    bad = bad || !(x[i] < CH_INF);
-    m = fmaxf(m, x[i]);
-  }
-  m = wave_max(m);
-  double s = 0.0;
-  if (m != -CH_INF) {
+  for (int i = 0; i < PER; ++i) {
+    const int part = first + 4 * i;
+    if (part >= a.parts) return;
+    if (i + 1 < PER) load(i + 1, x[(i + 1) & 1]);
+    float (&y)[16] = x[i & 1];
+    bool bad = false;
+    float m = -CH_INF;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s = s + pow32(exponent(x[i], (double)m, a.scale), table);
-  }
-  if (bad) s = __builtin_nan("");
-  s = wave_sum_f64(s);
-  if (lane == 0) {
-    const int64_t at = ((int64_t)blockIdx.z * a.B * a.N + row) * a.parts + part;
-    a.part_m[at] = m;
-    a.part_s[at] = s;
+    for (int k = 0; k < 16; ++k) {
+      bad = bad || !(y[k] < CH_INF);
+      m = fmaxf(m, y[k]);
+    }
+    m = wave_max(m);
+    double s = 0.0;
+    if (m != -CH_INF) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) s = s + pow32(exponent(y[k], (double)m, a.scale), table);
+    }
+    if (bad) s = __builtin_nan("");
+    s = wave_sum_f64(s);
+    if (lane == 0) {
+      const int64_t at = ((int64_t)blockIdx.z * a.B * a.N + row) * a.parts + part;
+      a.part_m[at] = m;
+      a.part_s[at] = s;
+    }
   }
 }
 
-// A row's maximum and sum out of its parts, by one wave.  ok: it has a distribution.
-struct RowSum {
-  double m, s;
-  __device__ __forceinline__ bool ok() const { return s > 0.0 && s < HUGE_VAL && m < (double)CH_INF; }
-};
+// A row's maximum and sum out of its parts, by one wave.
+__device__ __forceinline__ bool distributes(const RowSum& r) {
+  return r.s > 0.0 && r.s < HUGE_VAL && r.m < (double)CH_INF;
+}
 __device__ __forceinline__ RowSum row_sum(const AcceptArgs& a, int64_t row, const double* table) {
   const int lane = threadIdx.x & 63;
   const int64_t at = row * a.parts;
   float m = -CH_INF;
-  for (int i = lane; i < a.parts; i += 64) m = fmaxf(m, a.part_m[at + i]);
-  m = wave_max(m);
   double s = 0.0;
-  for (int i = lane; i < a.parts; i += 64) {
+  for (int i = lane; i < a.parts; i += 64) {  // 64 parts at a time, a lane's own scaled to its largest
     const float pm = a.part_m[at + i];
     const double ps = a.part_s[at + i];
-    s = s + (pm == -CH_INF ? ps : ps * pow32(exponent(pm, (double)m, a.scale), table));
+    const float mn = fmaxf(m, pm);
+    s = m == -CH_INF ? s : s * pow32(exponent(m, (double)mn, a.scale), table);
+    s = s + (pm == -CH_INF ? ps : ps * pow32(exponent(pm, (double)mn, a.scale), table));
+    m = mn;
   }
-  return {(double)m, wave_sum_f64(s)};
+  const float mt = wave_max(m);
+  s = m == -CH_INF ? s : s * pow32(exponent(m, (double)mt, a.scale), table);
+  return {(double)mt, wave_sum_f64(s)};
 }
 
 // ---- the walk ----------------------------------------------------------------------
 // Lane u holds node u.  From the root down: a node's children are tested in the order
 // of their ids; the walk goes on at the first accepted one and ends where there is
-// none.  All rows' sums and all nodes' probabilities come first, so the walk itself
-// touches no memory.
-struct Walk {
-  int node, depth;          // node -1: an empty place
-  bool ok;                  // the last row has a distribution
-  uint64_t path, rejected;  // nodes on the path; rejected children of the last one
-  RowSum p, q;              // of the last row
-};
+// none.  The sums of all rows with children and all nodes' probabilities come first, so
+// the walk itself touches no memory but for the row of a node without children.
 struct WalkSpace {
   double table[32];
   RowSum rows[2][64];
@@ -182,61 +198,72 @@ __device__ void accept_walk(const AcceptArgs& a, int b, WalkSpace& sh) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row0 = (int64_t)b * a.N;
   const bool drawn = a.draft != nullptr;
+  uint32_t pw = a.tree.parent[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) pw = lane / 4 == i ? a.tree.parent[i] : pw;
+  const int parent = lane == 0 ? -1 : (int)(pw >> (8 * (lane & 3))) & 255;
   const int tok = lane < a.N ? a.tokens[row0 + lane] : -1;
-  const double u = lane < a.N ? a.u[row0 + lane] : 0.0;
+  const bool named = lane > 0 && lane < a.N && tok >= 0 && tok < a.V;
+  double u = 0.0;
+  float zp = 0.f, zq = 0.f;
+  if (wave == 0 && named) {  // on their way beside the rows' sums
+    u = a.u[row0 + lane];
+    zp = logit<T>((const T*)a.logits + (row0 + parent) * a.ld, tok);
+    if (drawn) zq = logit<T>((const T*)a.draft + (row0 + parent) * a.ldd, tok);
+  }
   const bool empty = __builtin_amdgcn_readfirstlane(tok) < 0;
   fill_table(sh.table);
   __syncthreads();
-  if (!empty)
-    for (int i = wave; i < (drawn ? 2 : 1) * a.N; i += WAVES) {
-      const int z = i >= a.N ? 1 : 0, r = i - z * a.N;
+  if (!empty) {
+    const int n = __popcll(a.inner);
+    for (int i = wave; i < (drawn ? 2 : 1) * n; i += WAVES) {
+      const int z = i >= n ? 1 : 0;
+      uint64_t left = a.inner;
+      for (int k = i - z * n; k > 0; --k) left &= left - 1;
+      const int r = __ffsll((long long)left) - 1;
       const RowSum s = row_sum(a, z * (int64_t)a.B * a.N + row0 + r, sh.table);
       if (lane == 0) sh.rows[z][r] = s;
     }
+  }
   __syncthreads();
   if (wave == 0) {
-    uint32_t pw = a.tree.parent[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) pw = lane / 4 == i ? a.tree.parent[i] : pw;
-    const int parent = lane == 0 ? -1 : (int)(pw >> (8 * (lane & 3))) & 255;
     Walk w{};
     w.node = empty ? -1 : 0;
     if (!empty) {
-      const bool named = lane > 0 && lane < a.N && tok >= 0 && tok < a.V;
       double p = 0.0, q = 1.0;
       if (named) {
         const RowSum rp = sh.rows[0][parent];
-        p = pow32(exponent(logit<T>((const T*)a.logits + (row0 + parent) * a.ld, tok), rp.m, a.scale), sh.table) / rp.s;
+        p = pow32(exponent(zp, rp.m, a.scale), sh.table) / rp.s;
         if (drawn) {
           const RowSum rq = sh.rows[1][parent];
-          q = pow32(exponent(logit<T>((const T*)a.draft + (row0 + parent) * a.ldd, tok), rq.m, a.scale), sh.table) / rq.s;
+          q = pow32(exponent(zq, rq.m, a.scale), sh.table) / rq.s;
         }
       }
       w.path = 1;
       for (;;) {
         w.rejected = 0;
-        w.p = sh.rows[0][w.node];
-        w.ok = w.p.ok();
+        w.p = (a.inner >> w.node) & 1 ? sh.rows[0][w.node] : row_sum(a, row0 + w.node, sh.table);
+        w.ok = distributes(w.p);
         if (!w.ok) break;
         const uint64_t kids = __ballot(named && parent == w.node);
         if (kids == 0) break;
         if (drawn) {
           w.q = sh.rows[1][w.node];
-          w.ok = w.q.ok();
+          w.ok = distributes(w.q);
           if (!w.ok) break;
         }
         double left = 1.0;  // the mass of what is not rejected
         int next = -1;
         for (uint64_t rest = kids; rest != 0; rest &= rest - 1) {
-          const int c = __ffsll((long long)rest) - 1;
-          const double pc = shfl_f64(p, c), uc = shfl_f64(u, c);
-          if (uc * (drawn ? shfl_f64(q, c) : left) < pc) {
+          const int c = __builtin_amdgcn_readfirstlane(__ffsll((long long)rest) - 1);
+          const double pc = lane_f64(p, c);
+          if (lane_f64(u, c) * (drawn ? lane_f64(q, c) : left) < pc) {
             next = c;
             break;
           }
           w.rejected |= 1ull << c;
           left = left - pc;
-          if (tok == __shfl(tok, c)) p = 0.0;  // a sibling of the same token
+          if (tok == __builtin_amdgcn_readlane(tok, c)) p = 0.0;  // a sibling of the same token
         }
         if (next < 0) break;
         w.node = next;
@@ -266,20 +293,29 @@ struct Weights {
   }
 };
 
-// Drawn tokens: every part of the residual, grid (groups of four parts, sequences), a
-// wave a part.  Each workgroup walks by itself, which is cheaper than a launch between.
+// Drawn tokens: the walks, a workgroup a sequence, and then every part of the residual,
+// grid (groups of four parts, sequences), a wave a part.
+template <typename T>
+__global__ __launch_bounds__(1024) void accept_walk_kernel(const AcceptArgs a) {
+  __shared__ WalkSpace sh;
+  accept_walk<T, 16>(a, blockIdx.x, sh);
+  if (threadIdx.x == 0) a.walks[blockIdx.x] = sh.walk;
+}
+
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void accept_resid_kernel(const AcceptArgs a) {
-  __shared__ WalkSpace sh;
+  __shared__ double table[32];
   const int b = blockIdx.y, lane = threadIdx.x & 63;
   const int part = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  accept_walk<T, 4>(a, b, sh);
-  const Walk& w = sh.walk;
+  const Walk w = a.walks[b];
+  if (w.node < 0 || !w.ok || w.rejected == 0) return;
+  fill_table(table);
+  __syncthreads();
   const int v0 = part * ACCEPT_PART;
-  if (w.node < 0 || !w.ok || w.rejected == 0 || v0 >= a.V) return;
+  if (v0 >= a.V) return;
   const int64_t row = (int64_t)b * a.N + w.node;
   const Weights<T> f{(const T*)a.logits + row * a.ld, (const T*)a.draft + row * a.ldd, w.p.m, w.q.m, a.scale,
-                     1.0 / w.p.s, 1.0 / w.q.s, sh.table};
+                     1.0 / w.p.s, 1.0 / w.q.s, table};
   float x[16], xq[16];
   const int n = min(ACCEPT_PART, a.V - v0);
   load_part<T, VEC>(f.z + v0, n, lane, x);
@@ -303,7 +339,13 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   __shared__ double wave_s[16], redo[64];
   __shared__ int part_sh, first_sh[16], last_sh[16];
   __shared__ double before_sh, target_sh;
-  accept_walk<T, 16>(a, b, sh);
+  if (a.draft != nullptr && a.N > 1) {
+    fill_table(sh.table);
+    if (tid == 0) sh.walk = a.walks[b];
+    __syncthreads();
+  } else {
+    accept_walk<T, 16>(a, b, sh);
+  }
   const Walk w = sh.walk;
   if (tid < 64) {
     const int tok = lane < a.N ? a.tokens[row0 + lane] : -1;
@@ -341,7 +383,15 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   };
   // Parts that hold a rejected token are summed without it, a wave each: taking it off
   // the sum would leave rounding where it was most of it.
-  for (int i = wave; i < ng; i += 16) {
+  const int64_t parts0 = row * a.parts;
+  float pm0 = -CH_INF;
+  double ps0 = 0.0;
+  if (wave == 0 && lane < a.parts) {  // the first parts, on their way beside this
+    pm0 = a.part_m[parts0 + lane];
+    ps0 = f.zq != nullptr ? a.resid[(int64_t)b * a.parts + lane] : a.part_s[parts0 + lane];
+  }
+  for (int i = wave - 1; i < ng; i += 15) {
+    if (wave == 0) break;
     const int v0 = gone[i] / ACCEPT_PART * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
     constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
     float x[16];
@@ -363,11 +413,13 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
     if (wave == 0) {
       auto part_weight = [&](int i) {
         if (i >= a.parts) return 0.0;
-        if (f.zq != nullptr) return a.resid[(int64_t)b * a.parts + i];
+        const bool kept = i < 64 && attempt == 0;
+        if (f.zq != nullptr) return kept ? ps0 : a.resid[(int64_t)b * a.parts + i];
         for (int j = 0; j < ng; ++j)
           if (gone[j] / ACCEPT_PART == i) return redo[j];
-        const float pm = a.part_m[row * a.parts + i];
-        return pm == -CH_INF ? 0.0 : a.part_s[row * a.parts + i] * pow32(exponent(pm, w.p.m, a.scale), sh.table) * f.one;
+        const float pm = kept ? pm0 : a.part_m[parts0 + i];
+        const double ps = kept ? ps0 : a.part_s[parts0 + i];
+        return pm == -CH_INF ? 0.0 : ps * pow32(exponent(pm, w.p.m, a.scale), sh.table) * f.one;
       };
       double total = 0.0;
       for (int i0 = 0; i0 < a.parts; i0 += 64) total = total + wave_sum_f64(part_weight(i0 + lane));
@@ -428,12 +480,20 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   }
 }
 
+constexpr int64_t ACCEPT_MANY = 32768;  // parts
+
 template <typename T, bool VEC>
 void accept_go(const AcceptArgs& a, hipStream_t st) {
-  const int groups = (a.parts + 3) / 4;
-  hipLaunchKernelGGL((accept_parts_kernel<T, VEC>), dim3(a.B * a.N, groups, a.draft != nullptr ? 2 : 1), dim3(256), 0, st, a);
-  if (a.draft != nullptr && a.N > 1)
-    hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3(groups, a.B), dim3(256), 0, st, a);
+  const int rows = a.B * a.N, kinds = a.draft != nullptr ? 2 : 1;
+  // a wave takes four parts where that still fills the card several times
+  if ((int64_t)rows * kinds * a.parts >= ACCEPT_MANY)
+    hipLaunchKernelGGL((accept_parts_kernel<T, VEC, 4>), dim3(rows, (a.parts + 15) / 16, kinds), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((accept_parts_kernel<T, VEC, 1>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
+  if (a.draft != nullptr && a.N > 1) {
+    hipLaunchKernelGGL((accept_walk_kernel<T>), dim3(a.B), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3((a.parts + 3) / 4, a.B), dim3(256), 0, st, a);
+  }
   hipLaunchKernelGGL((accept_pick_kernel<T, VEC>), dim3(a.B), dim3(1024), 0, st, a);
 }
 template <typename T>
@@ -451,7 +511,7 @@ int64_t up(int64_t b) { return (b + 255) / 256 * 256; }
 
 int64_t accept_bytes(int B, int N, int V, bool drawn) {
   const int64_t parts = (V + ACCEPT_PART - 1) / ACCEPT_PART, rows = (int64_t)B * N * (drawn ? 2 : 1);
-  return up(rows * parts * 8) + up(rows * parts * 4) + up(drawn ? B * parts * 8 : 0);
+  return up(rows * parts * 8) + up(rows * parts * 4) + up(drawn ? B * parts * 8 : 0) + up(drawn ? B * sizeof(Walk) : 0);
 }
 
 void accept_carve(AcceptArgs& a, void* ws) {
@@ -463,6 +523,8 @@ void accept_carve(AcceptArgs& a, void* ws) {
   a.part_m = (float*)p;
   p += up(rows * a.parts * 4);
   a.resid = (double*)p;
+  p += up(a.draft != nullptr ? a.B * (int64_t)a.parts * 8 : 0);
+  a.walks = (Walk*)p;
 }
 
 void launch_accept(int dtype, const AcceptArgs& a, hipStream_t st) {

@@ -272,6 +272,7 @@ chimera_status chimera_accept(int32_t dtype, const void* logits, int64_t ld, con
       depth[i] = i == 0 ? 0 : depth[p] + 1;
       a.K = std::max(a.K, depth[i]);
       a.tree.set(i, p);
+      if (i > 0) a.inner |= (uint64_t)1 << p;
     }
     check_aligned(ws, "workspace");
     REQUIRE(ws_bytes >= accept_bytes(batch, n_nodes, vocab, draft != nullptr), CHIMERA_ENOMEM, "workspace too small");
