@@ -250,8 +250,16 @@ chimera_status chimera_set_graph(chimera_ctx* ctx, int32_t enable);
  *    SplitMix64(SplitMix64(SplitMix64(SplitMix64(seed) ^ b) ^ position) ^ v),
  *    b the sequence, position the token's position, v the token id.
  * Not lossless: the stream is a sample, reproducible from the seed.
+ * CHIMERA_DECODE_SAMPLED samples from the target at the given temperature (eps
+ * and delta are not used), whatever the draft proposes: chimera_accept's rule
+ * for chosen candidates on the tree, after a prompt plain sampling.  u[b][i] of a
+ * step at committed length n is the top 53 bits of SplitMix64(SplitMix64(
+ * SplitMix64(SplitMix64(seed) ^ b) ^ n) ^ i) / 2^53, i the node, and 64 for the
+ * first token after a prompt of n tokens.  Every token is distributed as the
+ * target's own; the stream is reproducible from the seed.  A token is 0 where the
+ * target's logits hold no distribution.
  * Takes effect from the next prefill or step. */
-enum { CHIMERA_DECODE_GREEDY = 0, CHIMERA_DECODE_TYPICAL = 1 };
+enum { CHIMERA_DECODE_GREEDY = 0, CHIMERA_DECODE_TYPICAL = 1, CHIMERA_DECODE_SAMPLED = 2 };
 chimera_status chimera_set_decoding(chimera_ctx* ctx, int32_t mode, float temperature, float eps, float delta,
                                     uint64_t seed);
 

@@ -11,7 +11,7 @@ LIB_PATH = os.path.join(_HERE, "libchimera.so")
 
 CHIMERA_F32, CHIMERA_BF16 = 0, 1
 CHIMERA_WEIGHTS_FP4 = 0x100
-CHIMERA_DECODE_GREEDY, CHIMERA_DECODE_TYPICAL = 0, 1
+CHIMERA_DECODE_GREEDY, CHIMERA_DECODE_TYPICAL, CHIMERA_DECODE_SAMPLED = 0, 1, 2
 CHIMERA_DRAFT_CHAIN, CHIMERA_DRAFT_BRANCH = 0, 1
 DBG_VERIFY_LOGITS, DBG_DRAFT_LOGITS, DBG_TREE_TOKENS, DBG_DRAFT_LISTS, DBG_SEQ_LEN, DBG_TOKENS = range(6)
 CHIMERA_ROPE_HALF, CHIMERA_ROPE_PAIRS = 0, 1

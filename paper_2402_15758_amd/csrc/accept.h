@@ -42,9 +42,18 @@ struct AcceptArgs {
   double* resid;            // [B][parts]
   Walk* walks;              // [B]
   uint64_t inner;           // nodes with children
+  int none;                 // what stands for a token where a row has no distribution
   AcceptTree tree;
 };
 constexpr int ACCEPT_PART = 1024;  // entries of a part: 16 a lane
+inline double accept_scale(float temperature) { return 32.0 / ((double)temperature * 0.69314718055994530942); }
 int64_t accept_bytes(int B, int N, int V, bool drawn);
 void accept_carve(AcceptArgs& a, void* ws);
 void launch_accept(int dtype, const AcceptArgs& a, hipStream_t st);
+// Random numbers of a step: u[b][i] of sequence b and node i at its committed length
+// n_b[b], the top 53 bits of SplitMix64(SplitMix64(SplitMix64(SplitMix64(seed) ^ b) ^ n)
+// ^ i).
+void launch_accept_uniforms(const int* n_b, int B, int N, unsigned long long seed, double* u, hipStream_t st);
+// The same for prompts that end in a prefill chunk, i = 64; tokens[j] = 0.
+struct PrefillEnds;
+void launch_accept_first(const PrefillEnds& e, unsigned long long seed, double* u, int* tokens, hipStream_t st);

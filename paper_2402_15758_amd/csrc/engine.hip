@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "abi.h"
+#include "accept.h"
 #include "chimera.h"
 #include "kernels.h"
 
@@ -189,6 +190,11 @@ struct chimera_ctx {
   double* t_lse = nullptr;  // [Mv]
   double* t_H = nullptr;    // [Mv]
   int* t_sample = nullptr;  // [Mv]
+  // sampled decoding: the tree and the workspaces of accept.h
+  int sampled = 0;
+  AcceptArgs walk{};
+  double* acc_u = nullptr;  // [max(Mv, PREFILL_SEGS)]
+  void* acc_ws = nullptr;
   int* v_qrow = nullptr;
   // draft workspaces
   void* tri_in = nullptr;
@@ -514,6 +520,11 @@ StepState make_state(chimera_ctx* c) {
   s.t_lse = c->t_lse;
   s.t_H = c->t_H;
   s.t_sample = c->t_sample;
+  s.sampled = c->sampled;
+  s.acc_stride = c->D + 1;
+  s.acc_n = c->walk.n_new;
+  s.acc_path = c->walk.path;
+  s.acc_tok = c->walk.new_tokens;
   const TreeMeta& dm = c->branch ? c->tree : c->chain;
   s.d_nodes = c->d_nodes;
   s.d_parent = dm.parent;
@@ -710,7 +721,19 @@ void prefill_chunk(chimera_ctx* c, const StepState& s, const PrefillChunk& ch, c
   el.out_f = c->logits;
   el.ldo = V;
   g.run(c->hl, mtl, ends.n, m->lm_head, V, d, el);
-  if (c->typical)  // the first generated token is sampled at position n
+  if (c->sampled) {  // the first generated token is drawn from the target
+    AcceptArgs f = c->walk;
+    launch_accept_first(ends, c->t_seed, c->acc_u, f.path, st);
+    f.tokens = f.path;
+    f.path = nullptr;
+    f.new_tokens = c->amax;
+    f.B = ends.n;
+    f.N = 1;
+    f.K = 0;
+    f.inner = 0;
+    accept_carve(f, c->acc_ws);
+    launch_accept(DT_F32, f, st);
+  } else if (c->typical)  // the first generated token is sampled at position n
     for (int j = 0; j < ends.n; ++j)
       launch_typical_stats(c->logits + (size_t)j * V, 1, V, 1, ends.seq[j], nullptr, nullptr, ends.len[j],
                            1.f / c->temperature, c->t_seed, c->t_lse, c->t_H, c->amax + j, st);
@@ -863,6 +886,12 @@ void carve_ctx(chimera_ctx* c, Arena& a) {
   c->t_lse = a.arr<double>(Mv);
   c->t_H = a.arr<double>(Mv);
   c->t_sample = a.arr<int>(Mv);
+  const size_t acc_rows = std::max<size_t>(Mv, PREFILL_SEGS);
+  c->walk.new_tokens = a.arr<int>(acc_rows);
+  c->walk.n_new = a.arr<int>(acc_rows);
+  c->walk.path = a.arr<int>(acc_rows);
+  c->acc_u = a.arr<double>(acc_rows);
+  c->acc_ws = a.take((size_t)accept_bytes((int)acc_rows, 1, (int)V, false));
   c->tri.hit = a.arr<int>(Md);
   c->tri.miss = a.arr<int>(1);
   c->tri.stats = a.arr<unsigned long long>(2);
@@ -1298,6 +1327,18 @@ chimera_status chimera_ctx_create(chimera_model* m, chimera_kv* kv, const int32_
       carve_ctx(c, a);
       c->K = K_used;
       upload_meta(c->tree, c->parent, c->rank, c->depth, c->anc);
+      AcceptArgs& f = c->walk;  // with a step's batch and the temperature as they come
+      for (int u = 0; u < c->N; ++u) {
+        f.tree.set(u, c->parent[u]);
+        if (u > 0) f.inner |= 1ull << c->parent[u];
+      }
+      f.logits = c->logits;
+      f.ld = m->cfg.vocab;
+      f.tokens = c->tree_tok;
+      f.u = c->acc_u;
+      f.N = c->N;
+      f.V = m->cfg.vocab;
+      f.K = c->D;
       std::vector<int> cp(64), cr(64, 0), cd(64);
       std::vector<unsigned long long> ca(64);
       for (int u = 0; u < 64; ++u) {
@@ -1447,7 +1488,13 @@ void enqueue_step(chimera_ctx* ctx, hipStream_t st) {
     el.out_f = ctx->logits;
     el.ldo = V;
     gq.run(ctx->hl, ctx->mt_v, M, m->lm_head, V, d, el);
-    if (ctx->typical)
+    if (ctx->sampled) {
+      launch_accept_uniforms(ctx->n, ctx->batch, ctx->N, ctx->t_seed, ctx->acc_u, q);
+      AcceptArgs f = ctx->walk;
+      f.B = ctx->batch;
+      accept_carve(f, ctx->acc_ws);
+      launch_accept(DT_F32, f, q);
+    } else if (ctx->typical)
       launch_typical_stats(ctx->logits, M, V, ctx->N, 0, ctx->n, ctx->tree.depth, -1, 1.f / ctx->temperature,
                            ctx->t_seed, ctx->t_lse, ctx->t_H, ctx->t_sample, q);
     else
@@ -1897,13 +1944,19 @@ chimera_status chimera_set_decoding(chimera_ctx* ctx, int32_t mode, float temper
                                     uint64_t seed) {
   return guard([&] {
     check_ctx(ctx);
-    REQUIRE(mode == CHIMERA_DECODE_GREEDY || mode == CHIMERA_DECODE_TYPICAL, CHIMERA_EINVAL, "decoding mode");
+    REQUIRE(mode == CHIMERA_DECODE_GREEDY || mode == CHIMERA_DECODE_TYPICAL || mode == CHIMERA_DECODE_SAMPLED,
+            CHIMERA_EINVAL, "decoding mode");
     if (mode == CHIMERA_DECODE_TYPICAL)
       REQUIRE(temperature > 0.f && eps >= 0.f && delta >= 0.f, CHIMERA_EINVAL,
               "typical decoding needs temperature > 0, eps >= 0, delta >= 0");
+    if (mode == CHIMERA_DECODE_SAMPLED)
+      REQUIRE(std::isfinite(temperature) && temperature > 0.f, CHIMERA_EINVAL,
+              "sampled decoding needs a finite temperature > 0");
     drop_graph(ctx);
     ctx->typical = mode == CHIMERA_DECODE_TYPICAL;
-    ctx->temperature = mode == CHIMERA_DECODE_TYPICAL ? temperature : 1.f;
+    ctx->sampled = mode == CHIMERA_DECODE_SAMPLED;
+    ctx->temperature = mode == CHIMERA_DECODE_GREEDY ? 1.f : temperature;
+    ctx->walk.scale = accept_scale(ctx->temperature);
     ctx->t_eps = eps;
     ctx->t_delta = delta;
     ctx->t_seed = seed;

@@ -326,6 +326,12 @@ struct StepState {
   const double* t_lse;      // [B*N]
   const double* t_H;        // [B*N]
   const int* t_sample;      // [B*N]
+  // sampled decoding (sampled != 0): where each sequence's walk ended (accept.h), rows of
+  // acc_stride
+  int sampled, acc_stride;
+  const int* acc_n;         // [B]
+  const int* acc_path;      // [B][acc_stride]
+  const int* acc_tok;       // [B][acc_stride]
   // drafting plan.  The draft tree is the rank-0 chain (chain drafting: node
   // k at depth k) or the verify tree itself (branch-conditioned drafting).
   // Level k drafts the depth-k draft-tree nodes that have children.

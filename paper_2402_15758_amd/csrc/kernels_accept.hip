@@ -368,7 +368,7 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   __syncthreads();
   if (w.node < 0) return;
   if (!w.ok) {
-    if (tid == 0) a.new_tokens[(int64_t)b * K1 + w.depth] = -1;
+    if (tid == 0) a.new_tokens[(int64_t)b * K1 + w.depth] = a.none;
     return;
   }
   const int64_t row = row0 + w.node;
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
     f.one = 1.0;
   }
   if (part_sh < 0) {  // u was no number
-    if (tid == 0) a.new_tokens[(int64_t)b * K1 + w.depth] = -1;
+    if (tid == 0) a.new_tokens[(int64_t)b * K1 + w.depth] = a.none;
     return;
   }
   // within the part, an entry a thread
@@ -481,6 +481,26 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
 }
 
 constexpr int64_t ACCEPT_MANY = 32768;  // parts
+
+__device__ __forceinline__ uint64_t mix(uint64_t x) {  // SplitMix64
+  uint64_t z = x + 0x9e3779b97f4a7c15ull;
+  z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ull;
+  z = (z ^ (z >> 27)) * 0x94d049bb133111ebull;
+  return z ^ (z >> 31);
+}
+__device__ __forceinline__ double uniform(uint64_t seed, int b, int n, int i) {
+  return (double)(mix(mix(mix(mix(seed) ^ (uint64_t)b) ^ (uint64_t)n) ^ (uint64_t)i) >> 11) * 0x1p-53;
+}
+__global__ void accept_uniforms_kernel(const int* __restrict__ n_b, int N, unsigned long long seed, double* u) {
+  const int b = blockIdx.x, i = threadIdx.x;
+  if (i < N) u[(int64_t)b * N + i] = uniform(seed, b, n_b[b], i);
+}
+__global__ void accept_first_kernel(const PrefillEnds e, unsigned long long seed, double* u, int* tokens) {
+  const int j = threadIdx.x;
+  if (j >= e.n) return;
+  u[j] = uniform(seed, e.seq[j], e.len[j], 64);
+  tokens[j] = 0;
+}
 
 template <typename T, bool VEC>
 void accept_go(const AcceptArgs& a, hipStream_t st) {
@@ -532,4 +552,11 @@ void launch_accept(int dtype, const AcceptArgs& a, hipStream_t st) {
     accept_t<bf16_t>(a, st);
   else
     accept_t<float>(a, st);
+}
+
+void launch_accept_uniforms(const int* n_b, int B, int N, unsigned long long seed, double* u, hipStream_t st) {
+  hipLaunchKernelGGL(accept_uniforms_kernel, dim3(B), dim3(64), 0, st, n_b, N, seed, u);
+}
+void launch_accept_first(const PrefillEnds& e, unsigned long long seed, double* u, int* tokens, hipStream_t st) {
+  hipLaunchKernelGGL(accept_first_kernel, dim3(1), dim3(PREFILL_SEGS), 0, st, e, seed, u, tokens);
 }

@@ -446,7 +446,11 @@ __device__ __forceinline__ int accept_path(const StepState& s, int b, int u, boo
   const unsigned long long anc = valid ? s.t_anc[u] : 0ull;
   const int dep = s.t_depth[valid ? u : 0];
   int v, bonus;
-  if (!s.typical) {
+  if (s.sampled) {
+    const int last = b * s.acc_stride + s.acc_n[b] - 1;  // the root is accepted at least
+    v = s.acc_path[last];
+    bonus = s.acc_tok[last];
+  } else if (!s.typical) {
     // greedy: every non-root token equals the target argmax at its parent;
     // the deepest such node (unique: siblings are distinct)
     const int a_u = s.amax[row];

@@ -286,10 +286,11 @@ chimera_status chimera_accept(int32_t dtype, const void* logits, int64_t ld, con
     a.B = batch;
     a.N = n_nodes;
     a.V = vocab;
-    a.scale = 32.0 / ((double)temperature * 0.69314718055994530942);
+    a.scale = accept_scale(temperature);
     a.new_tokens = new_tokens;
     a.n_new = n_new;
     a.path = path_nodes;
+    a.none = -1;
     accept_carve(a, ws);
     launch_accept(dtype, a, st);
     HIPCK(hipGetLastError());

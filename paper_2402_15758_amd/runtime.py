@@ -187,6 +187,10 @@ class Session:
         B.chimera_set_decoding(self.ctx, B.CHIMERA_DECODE_TYPICAL if typical else B.CHIMERA_DECODE_GREEDY,
                                temperature, eps, delta, seed)
 
+    def set_sampling(self, temperature: float = 1.0, seed: int = 0):
+        """Sampling from the target: drafted tokens are verified by their probabilities."""
+        B.chimera_set_decoding(self.ctx, B.CHIMERA_DECODE_SAMPLED, temperature, 0.0, 0.0, seed)
+
     def trigram_cache(self, n_entries: int):
         """Attach an empty trigram lookup cache of n_entries outputs (0 detaches)."""
         import torch
