@@ -19,38 +19,25 @@ struct QueryBlock {
 };
 __device__ __forceinline__ int clamp_row(const PagedAttnArgs& a, int r) { return min(max(r, 0), a.rows); }
 
-__device__ __forceinline__ void seq_rows(const PagedAttnArgs& a, int b, int& row0, int& rows) {
-  row0 = b, rows = 1;
-  if (a.row0 != nullptr) {
-    row0 = clamp_row(a, a.row0[b]);
-    rows = max(clamp_row(a, a.row0[b + 1]) - row0, 0);
-  }
-}
-
-// Block `slot` of 16 queries: the same number of slots a sequence.
-__device__ __forceinline__ QueryBlock few_block(const PagedAttnArgs& a, int slot) {
-  QueryBlock k;
-  k.b = slot / a.per;
-  int rows;
-  seq_rows(a, k.b, k.row0, rows);
-  const int queries = rows * a.group;
-  k.v0 = (slot - k.b * a.per) * 16;
-  k.count = queries > a.few ? 0 : max(min(queries - k.v0, 16), 0);
-  k.n = min(a.n_b[k.b], 1 << 30);
-  return k;
-}
-// Block `slot` of 128 queries: sequence b's slots start at floor(row0[b] group / 128) + b,
-// which leaves each room for its own.  All lanes of a wave; the result is uniform.
-__device__ __forceinline__ QueryBlock many_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
-  constexpr int BQ = 128;
+// Block `slot` of BQ queries of the sequences with more than `least` queries and up to
+// `most`.  All lanes of a wave; the result is uniform.
+//  - a.per > 0: the same number of slots a sequence;
+//  - else sequence b's slots start at floor(row0[b] group / BQ) + b, which leaves each
+//    room for its own.
+template <int BQ>
+__device__ __forceinline__ QueryBlock find_block(const PagedView& c, const PagedAttnArgs& a, int slot, int least,
+                                                 int most) {
   QueryBlock k;
   int rows = 1, at;
-  if (a.row0 == nullptr) {
-    const int per = (a.group + BQ - 1) / BQ;
-    k.b = slot / per;
-    at = slot - k.b * per;
+  if (a.per > 0) {
+    k.b = slot / a.per;
+    at = slot - k.b * a.per;
     k.row0 = k.b;
     k.n = a.n_b[k.b];
+    if (a.row0 != nullptr) {
+      k.row0 = clamp_row(a, a.row0[k.b]);
+      rows = max(clamp_row(a, a.row0[k.b + 1]) - k.row0, 0);
+    }
   } else {
     // the last sequence whose slots start at or before this one, 64 looked at at once;
     // the last look brings all that is needed of it
@@ -77,8 +64,14 @@ __device__ __forceinline__ QueryBlock many_block(const PagedView& c, const Paged
   const int queries = rows * a.group;
   k.n = min(k.n, 1 << 30);
   k.v0 = at * BQ;
-  k.count = queries <= a.few || at < 0 ? 0 : max(min(queries - k.v0, BQ), 0);
+  k.count = queries <= least || queries > most || at < 0 ? 0 : max(min(queries - k.v0, BQ), 0);
   return k;
+}
+__device__ __forceinline__ QueryBlock few_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
+  return find_block<16>(c, a, slot, 0, a.few);
+}
+__device__ __forceinline__ QueryBlock many_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
+  return find_block<128>(c, a, slot, a.few, INT32_MAX);
 }
 
 // The tiles of TILE positions that some query of a block sees: `lead` ones from
@@ -315,7 +308,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
   __shared__ float msh[4][RB], lsh[4][RB];
   const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
   const int split = rest % a.splits, slot = rest / a.splits;
-  const QueryBlock blk = few_block(a, slot);
+  const QueryBlock blk = few_block(c, a, slot);
   if (blk.count == 0) return;
   const Span<RT> span(c, a, blk);
   const int parts = parts_of(span.tiles, a.splits, R_LEAST);
@@ -913,7 +906,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, cons
   constexpr int D = HD / 16;
   const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
   const int q = rest % (BQ / 16) * 16 + threadIdx.x / 16, slot = rest / (BQ / 16);
-  const QueryBlock blk = BQ == RB ? few_block(a, slot) : many_block(c, a, slot);
+  const QueryBlock blk = BQ == RB ? few_block(c, a, slot) : many_block(c, a, slot);
   const Span<TILE> span(c, a, blk);
   const int parts = parts_of(span.tiles, a.splits, least);
   if (q >= blk.count || parts == 1) return;  // no query, or written whole
@@ -959,7 +952,7 @@ __global__ __launch_bounds__(256) void paged_join_many_kernel(const PagedView c,
   constexpr int D = HD / 64, U = 8, W = 4;
   const int nth = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int q = blockIdx.x % BQ, kvh = blockIdx.x / BQ % c.H, slot = blockIdx.x / BQ / c.H;
-  const QueryBlock blk = BQ == RB ? few_block(a, slot) : many_block(c, a, slot);
+  const QueryBlock blk = BQ == RB ? few_block(c, a, slot) : many_block(c, a, slot);
   const Span<TILE> span(c, a, blk);
   const int parts = parts_of(span.tiles, a.splits, least);
   if (q >= blk.count || parts == 1) return;  // for the whole workgroup alike
@@ -1040,9 +1033,6 @@ int64_t deal_slots(int64_t cap, int64_t blocks, int wgs, int tile, int least) {
 
 // Sequences of up to this many queries of a cache head go to the kernel for few.
 int few_queries(const PagedView& c, const PagedAttnArgs& a) {
-#ifdef FORCE_FEW
-  return FORCE_FEW;
-#else
   const bool single = a.row0 == nullptr;
   const int64_t most = single ? a.group : (int64_t)a.rows * a.group;
   if (most <= RB) return RB;
@@ -1050,14 +1040,18 @@ int few_queries(const PagedView& c, const PagedAttnArgs& a) {
   const double flops = 4.0 * a.rows * a.Hq * c.hd * (double)seen;
   if (flops <= FEW_FLOPS) return (int)std::min<int64_t>(most, INT32_MAX);
   return c.B == 1 && !single ? 0 : RB;
-#endif
 }
-int64_t few_slots(bool single, int rows, int batch, int group, int64_t few) {
-  const int64_t queries = single ? group : std::min<int64_t>((int64_t)rows * group, few);
-  return (std::min<int64_t>(queries, few) + RB - 1) / RB * batch;
-}
-int64_t many_slots(bool single, int64_t rows, int batch, int group) {
-  return single ? (int64_t)batch * ((group + TB - 1) / TB) : rows * group / TB + batch;
+// Slots of a launch and, where every sequence has as many, those of one (else 0).
+struct Deal {
+  int64_t slots;
+  int per;
+};
+Deal deal(bool single, int64_t rows, int batch, int group, int64_t most, int block) {
+  if (single || most <= block) {
+    const int per = (int)((std::min<int64_t>(single ? group : most, most) + block - 1) / block);
+    return {(int64_t)batch * per, per};
+  }
+  return {rows * group / block + batch, 0};
 }
 
 template <typename T, int HD>
@@ -1068,10 +1062,11 @@ void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
   a.few = few_queries(c, a);
   if (a.few > 0 && (!single || most <= a.few)) {
     PagedAttnArgs f = a;
-    f.slots = (int)few_slots(single, a.rows, c.B, a.group, a.few);
-    f.per = f.slots / c.B;
-    f.splits = (int)deal_splits(c.cap, (int64_t)f.slots * c.H, R_WGS, RT, R_LEAST);
-    const int64_t parts = (int64_t)f.slots * c.H * f.splits;
+    const Deal d = deal(single, a.rows, c.B, a.group, a.few, RB);
+    f.slots = (int)d.slots;
+    f.per = d.per;
+    f.splits = (int)deal_splits(c.cap, d.slots * c.H, R_WGS, RT, R_LEAST);
+    const int64_t parts = d.slots * c.H * f.splits;
     f.part_o = at;
     f.part_ml = at + parts * RB * HD;
     hipLaunchKernelGGL((paged_rows_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, f);
@@ -1081,9 +1076,11 @@ void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
     }
   }
   if (most > a.few) {
-    a.slots = (int)many_slots(single, a.rows, c.B, a.group);
-    a.splits = (int)deal_splits(c.cap, (int64_t)a.slots * c.H, T_WGS, TT<T>, T_LEAST);
-    const int64_t parts = (int64_t)a.slots * c.H * a.splits;
+    const Deal d = deal(single, a.rows, c.B, a.group, most, TB);
+    a.slots = (int)d.slots;
+    a.per = d.per;
+    a.splits = (int)deal_splits(c.cap, d.slots * c.H, T_WGS, TT<T>, T_LEAST);
+    const int64_t parts = d.slots * c.H * a.splits;
     a.part_o = at;
     a.part_ml = at + parts * TB * HD;
     hipLaunchKernelGGL((paged_tiles_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
@@ -1094,9 +1091,10 @@ void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
 }  // namespace
 
 int64_t paged_attn_bytes(int64_t cap, int rows, int batch, int group, int H, int hd, int es) {
-  const int64_t few = R_WGS, many = std::max(many_slots(false, rows, batch, group), many_slots(true, rows, batch, group)) * H;
+  const int64_t most = std::max<int64_t>((int64_t)rows * group, group);
+  const int64_t many = std::max(deal(false, rows, batch, group, most, TB).slots, deal(true, rows, batch, group, most, TB).slots);
   const int tile = es == 2 ? TT<bf16_t> : TT<float>;
-  return (deal_slots(cap, few, R_WGS, RT, R_LEAST) * RB + deal_slots(cap, many, T_WGS, tile, T_LEAST) * TB) * (hd + 2) * 4;
+  return (deal_slots(cap, R_WGS, R_WGS, RT, R_LEAST) * RB + deal_slots(cap, many * H, T_WGS, tile, T_LEAST) * TB) * (hd + 2) * 4;
 }
 
 void launch_paged_attn(int dtype, const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {

@@ -75,8 +75,9 @@ void check_heads(const chimera_paged* c, int32_t n_heads) {
 void check_attn_rows(const chimera_paged* c, int32_t n_heads, int32_t rows) {
   check_paged(c);
   check_heads(c, n_heads);
-  REQUIRE(rows >= 0 && (int64_t)rows * n_heads + (int64_t)c->batch * n_heads <= (int64_t)1 << 26, CHIMERA_EINVAL,
-          "(rows + batch) * n_heads is at most 2^26");
+  // a launch's threads are counted in 32 bits
+  REQUIRE(rows >= 0 && (int64_t)rows * n_heads <= (int64_t)1 << 26, CHIMERA_EINVAL, "rows * n_heads in [0, 2^26]");
+  REQUIRE((int64_t)c->batch * n_heads <= (int64_t)1 << 23, CHIMERA_EINVAL, "batch * n_heads is at most 2^23");
 }
 
 void check_tree(int32_t batch, int32_t n_nodes, int32_t vocab) {

@@ -200,9 +200,16 @@ def test_append_in_place_and_many_rows():
 
 
 # ---- attention -----------------------------------------------------------------------
-def attend(q, pool, table, lens, rows, dtype, scale, window=0, sinks=0, row0="starts", ldo=None, behind=2, ws=None):
-    """The operator's rows, and those behind the last sequence."""
+def attend(q, pool, table, lens, rows, dtype, scale, window=0, sinks=0, row0="starts", ldo=None, behind=2, ws=None,
+           far=False):
+    """The operator's rows, and those behind the last sequence.  far: a table of so many
+    pages that the work is dealt as for a long cache, 128 queries at once."""
     total, Hq, hd = q.shape
+    if far:
+        cap = int(4e9 / (4 * total * Hq * hd)) + 1
+        wide = torch.full((table.shape[0], table.shape[1] + cap // pool.shape[3]), -1, dtype=torch.int32)
+        wide[:, :table.shape[1]] = table
+        table = wide
     dq = torch.zeros(total + behind, Hq * hd, dtype=R.TYPES[dtype], device="cuda")
     dq[:total] = q.reshape(total, -1).cuda()
     ldo = ldo or Hq * hd
@@ -280,6 +287,23 @@ def test_single_tokens_of_many_sequences(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch", [65, 300, 5000])
+def test_ragged_rows_of_many_sequences(dtype, batch):
+    """Most sequences without rows, some with one or a few, three with a chunk; where the
+    cache is long the work is dealt in another way."""
+    g = torch.Generator().manual_seed(batch)
+    for far in (False, True):
+        rows, lens = [0] * batch, torch.randint(0, 60, (batch,), generator=g).tolist()
+        for i in torch.randint(0, batch, (60,), generator=g).tolist():
+            rows[i] = 1 + i % 5
+        rows[0], rows[batch // 2], rows[-1] = 40, 33, 150
+        q, pool, table = attn_inputs(dtype, lens, rows, 4, 2, 64, 16, batch)
+        got = attend(q, pool, table, lens, rows, dtype, 0.125, far=far)
+        ref, mag, big = R.attention(q, pool, table, lens, rows, 0.125)
+        assert bool(((got - ref).abs() <= R.attention_bound(dtype, ref, mag, big, 210, 64)).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_scales(dtype, scale):
     check(dtype, [90, 3], [1, 70], 4, 2, 64, 16, 5, scale=scale)
@@ -331,6 +355,64 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, bad):
                 assert bool(((got[~free] - ref[~free]).abs() <= bound)[ok].all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_attention_far(dtype, hd, case):
+    lens, rows, Hq, H, page = SHAPES[case]
+    check(dtype, lens, rows, Hq, H, hd, page, 10 * case + hd, far=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks", [(1, 900), (64, 836), (500, 400), (1000, 0), (901, 128), (1 << 30, 3)])
+def test_window_far(dtype, window, sinks):
+    """Blocks of 128 queries whose first tiles and last ones lie apart, meet or overlap."""
+    check(dtype, [800, 0, 1300], [600, 3, 90], 8, 1, 128, 16, window + sinks, window, sinks, far=True)
+    check(dtype, [1200], [693], 8, 2, 128, 64, window + sinks, window, sinks, far=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_parts_of_blocks_of_128(dtype):
+    """Blocks whole, in two to eight parts and in more."""
+    check(dtype, [4100], [40], 2, 1, 128, 16, 6, far=True)
+    check(dtype, [3000, 900], [130, 1], 4, 2, 64, 64, 6, far=True)
+    check(dtype, [2500], [500], 16, 16, 64, 16, 7)
+    check(dtype, [2000, 0, 700], [20, 1, 300], 16, 16, 128, 16, 7, far=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", [17, 64])
+def test_single_tokens_of_many_query_heads(dtype, heads):
+    """More query heads a cache head than a block of 16 has rows."""
+    for far in (False, True):
+        check(dtype, [900, 0, 33], [1, 1, 1], heads, 1, 64, 16, heads, row0=None, behind=0, far=far)
+        check(dtype, [900, 33], [2, 1], heads, 1, 128, 16, heads, far=far)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
+def test_scales_and_unaligned_output_far(dtype, scale):
+    check(dtype, [90, 3], [1, 70], 4, 2, 64, 16, 5, scale=scale, far=True, ldo=4 * 64 + 3)
+    check(dtype, [90], [70], 4, 2, 128, 16, 5, scale=scale, far=True, ldo=4 * 128 + 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_what_a_row_does_not_see_does_not_reach_it_far(dtype, bad):
+    """A value that is no number, behind the mask of some rows of a tile of 128."""
+    for lens, rows, at in (([40], [160], 70), ([200], [9], 204), ([300], [140], 310), ([0], [200], 63)):
+        for hd in (64, 128):
+            q, pool, table = attn_inputs(dtype, lens, rows, 2, 1, hd, 16, 8)
+            pool[table[0, at // 16], 1, :, at % 16, 3] = bad
+            got = attend(q, pool, table, lens, rows, dtype, 0.125, far=True)
+            ref, mag, big = R.attention(q, pool, table, lens, rows, 0.125)
+            free = lens[0] + torch.arange(rows[0]) < at
+            assert bool(free.any()) and not bool(free.all())
+            near = (got - ref).abs() <= R.attention_bound(dtype, ref, mag, big, 500, hd)
+            assert bool(near[free].all()) and bool(near[~free][..., :3].all()) and bool(near[~free][..., 4:].all())
+            assert bool((got[~free][..., 3].isnan() if math.isnan(bad) else got[~free][..., 3] == bad).all())
+
+
 def test_scores_past_the_range():
     """All scores -inf: NaN; some: they weigh nothing."""
     for rows in (1, 70):
@@ -354,9 +436,10 @@ def test_positions_and_pages_that_are_not_there():
         q, pool, table = attn_inputs("f32", lens, rows, 4, 2, hd, 16, 11)
         pool = pool.nan_to_num(0.5)
         table[0, 1], table[0, 2], table[1, 0] = -1, 1 << 30, pool.shape[0]
-        got = attend(q, pool, table, lens, rows, "f32", 0.125)
         ref, mag, big = R.attention(q, pool, table, lens, rows, 0.125)
-        assert bool(((got - ref).abs() <= R.attention_bound("f32", ref, mag, big, 80, hd)).all())
+        for far in (False, True):
+            got = attend(q, pool, table, lens, rows, "f32", 0.125, far=far)
+            assert bool(((got - ref).abs() <= R.attention_bound("f32", ref, mag, big, 80, hd)).all())
         # a sequence with no page at all, and one past its table
         table[1] = -5
         got = attend(q, pool, table, [10000, 20], rows, "f32", 0.125, 5, 0)
@@ -388,8 +471,10 @@ def test_starts_that_leave_rows_out():
 def test_equal_calls_give_equal_bits():
     q, pool, table = attn_inputs("bf16", [3000, 900], [70, 1], 4, 2, 128, 16, 13)
     a = attend(q, pool, table, [3000, 900], [70, 1], "bf16", 0.09)
+    b = attend(q, pool, table, [3000, 900], [70, 1], "bf16", 0.09, far=True)
     for _ in range(3):
         assert torch.equal(a, attend(q, pool, table, [3000, 900], [70, 1], "bf16", 0.09))
+        assert torch.equal(b, attend(q, pool, table, [3000, 900], [70, 1], "bf16", 0.09, far=True))
 
 
 def test_offsets_past_32_bits():

@@ -110,7 +110,8 @@ def test_attention_refusals():
     refused(E, "multiple", lambda: attn(heads=6))
     refused(E, "multiple", lambda: attn(heads=0))
     refused(E, "2^26", lambda: attn(rows=-1))
-    refused(E, "2^26", lambda: attn(rows=1 << 26))
+    refused(E, "2^26", lambda: attn(rows=1 << 25))
+    refused(E, "2^23", lambda: attn(cache(batch=65535), heads=256, ldq=1 << 20, ldo=1 << 20))
     refused(E, "without row0", lambda: attn(row0=None))
     for n in ("q", "n", "out"):
         refused(E, "null", lambda: attn(**{n: None}))
