@@ -108,10 +108,9 @@ __device__ __forceinline__ void load_part(const T* z, int n, int lane, float (&x
 }
 
 // ---- parts of rows -----------------------------------------------------------------
-// Grid (rows, groups of parts, target | draft), a wave PER parts one after another, the
-// next one's entries on their way while one is summed.  A NaN or +inf makes a part's sum
-// NaN: such a row has no distribution.
-template <typename T, bool VEC, int PER>
+// Grid (rows, groups of four parts, target | draft), a wave a part.  A NaN or +inf makes a
+// part's sum NaN: such a row has no distribution.
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
   __shared__ double table[32];
   const int row = blockIdx.x, lane = threadIdx.x & 63;
@@ -119,44 +118,34 @@ __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
   const bool of_draft = blockIdx.z != 0;
   // nothing is drawn after a node without children
   if (of_draft && !((a.inner >> node) & 1)) return;
-  const int first = blockIdx.y * 4 * PER + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const T* z = of_draft ? (const T*)a.draft + (int64_t)row * a.ldd : (const T*)a.logits + (int64_t)row * a.ld;
   const int root = a.tokens[(int64_t)b * a.N];
-  auto load = [&](int i, float (&x)[16]) {
-    const int v0 = (first + 4 * i) * ACCEPT_PART;
-    if (v0 < a.V) load_part<T, VEC>(z + v0, min(ACCEPT_PART, a.V - v0), lane, x);
-  };
-  float x[2][16];
-  load(0, x[0]);
+  const int v0 = part * ACCEPT_PART;
+  float x[16];
+  if (part < a.parts) load_part<T, VEC>(z + v0, min(ACCEPT_PART, a.V - v0), lane, x);
   fill_table(table);
   __syncthreads();
-  if (root < 0) return;  // an empty place
+  if (root < 0 || part >= a.parts) return;  // an empty place
+  bool bad = false;
+  float m = -CH_INF;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int part = first + 4 * i;
-    if (part >= a.parts) return;
-    if (i + 1 < PER) load(i + 1, x[(i + 1) & 1]);
-    float (&y)[16] = x[i & 1];
-    bool bad = false;
-    float m = -CH_INF;
+  for (int k = 0; k < 16; ++k) {
+    bad = bad || !(x[k] < CH_INF);
+    m = fmaxf(m, x[k]);
+  }
+  m = wave_max(m);
+  double s = 0.0;
+  if (m != -CH_INF) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      bad = bad || !(y[k] < CH_INF);
-      m = fmaxf(m, y[k]);
-    }
-    m = wave_max(m);
-    double s = 0.0;
-    if (m != -CH_INF) {
-#pragma unroll
-      for (int k = 0; k < 16; ++k) s = s + pow32(exponent(y[k], (double)m, a.scale), table);
-    }
-    if (bad) s = __builtin_nan("");
-    s = wave_sum_f64(s);
-    if (lane == 0) {
-      const int64_t at = ((int64_t)blockIdx.z * a.B * a.N + row) * a.parts + part;
-      a.part_m[at] = m;
-      a.part_s[at] = s;
-    }
+    for (int k = 0; k < 16; ++k) s = s + pow32(exponent(x[k], (double)m, a.scale), table);
+  }
+  if (bad) s = __builtin_nan("");
+  s = wave_sum_f64(s);
+  if (lane == 0) {
+    const int64_t at = ((int64_t)blockIdx.z * a.B * a.N + row) * a.parts + part;
+    a.part_m[at] = m;
+    a.part_s[at] = s;
   }
 }
 
@@ -480,8 +469,6 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   }
 }
 
-constexpr int64_t ACCEPT_MANY = 32768;  // parts
-
 __device__ __forceinline__ uint64_t mix(uint64_t x) {  // SplitMix64
   uint64_t z = x + 0x9e3779b97f4a7c15ull;
   z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ull;
@@ -505,11 +492,7 @@ __global__ void accept_first_kernel(const PrefillEnds e, unsigned long long seed
 template <typename T, bool VEC>
 void accept_go(const AcceptArgs& a, hipStream_t st) {
   const int rows = a.B * a.N, kinds = a.draft != nullptr ? 2 : 1;
-  // a wave takes four parts where that still fills the card several times
-  if ((int64_t)rows * kinds * a.parts >= ACCEPT_MANY)
-    hipLaunchKernelGGL((accept_parts_kernel<T, VEC, 4>), dim3(rows, (a.parts + 15) / 16, kinds), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((accept_parts_kernel<T, VEC, 1>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((accept_parts_kernel<T, VEC>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
   if (a.draft != nullptr && a.N > 1) {
     hipLaunchKernelGGL((accept_walk_kernel<T>), dim3(a.B), dim3(1024), 0, st, a);
     hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3((a.parts + 3) / 4, a.B), dim3(256), 0, st, a);

@@ -19,14 +19,12 @@ struct QueryBlock {
 };
 __device__ __forceinline__ int clamp_row(const PagedAttnArgs& a, int r) { return min(max(r, 0), a.rows); }
 
-// Block `slot` of BQ queries of the sequences with more than `least` queries and up to
-// `most`.  All lanes of a wave; the result is uniform.
+// Block `slot` of BQ queries.  All lanes of a wave; the result is uniform.
 //  - a.per > 0: the same number of slots a sequence;
 //  - else sequence b's slots start at floor(row0[b] group / BQ) + b, which leaves each
 //    room for its own.
 template <int BQ>
-__device__ __forceinline__ QueryBlock find_block(const PagedView& c, const PagedAttnArgs& a, int slot, int least,
-                                                 int most) {
+__device__ __forceinline__ QueryBlock find_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
   QueryBlock k;
   int rows = 1, at;
   if (a.per > 0) {
@@ -61,17 +59,10 @@ __device__ __forceinline__ QueryBlock find_block(const PagedView& c, const Paged
       len = min(step, len - last * step);
     }
   }
-  const int queries = rows * a.group;
   k.n = min(k.n, 1 << 30);
   k.v0 = at * BQ;
-  k.count = queries <= least || queries > most || at < 0 ? 0 : max(min(queries - k.v0, BQ), 0);
+  k.count = at < 0 ? 0 : max(min(rows * a.group - k.v0, BQ), 0);
   return k;
-}
-__device__ __forceinline__ QueryBlock few_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
-  return find_block<16>(c, a, slot, 0, a.few);
-}
-__device__ __forceinline__ QueryBlock many_block(const PagedView& c, const PagedAttnArgs& a, int slot) {
-  return find_block<128>(c, a, slot, a.few, INT32_MAX);
 }
 
 // The tiles of TILE positions that some query of a block sees: `lead` ones from
@@ -298,7 +289,6 @@ __device__ __forceinline__ void row_pv(const uint32_t (&v)[8][RowTile<T, HD>::VW
 }
 
 constexpr int RB = 16, RT = 32;  // queries and positions of a wave's tile
-constexpr int R_LEAST = 8;       // tiles of a part: two a wave
 
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, const PagedAttnArgs a) {
@@ -308,10 +298,10 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
   __shared__ float msh[4][RB], lsh[4][RB];
   const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
   const int split = rest % a.splits, slot = rest / a.splits;
-  const QueryBlock blk = few_block(c, a, slot);
+  const QueryBlock blk = find_block<RB>(c, a, slot);
   if (blk.count == 0) return;
   const Span<RT> span(c, a, blk);
-  const int parts = parts_of(span.tiles, a.splits, R_LEAST);
+  const int parts = parts_of(span.tiles, a.splits, a.least);
   if (split >= parts) return;
   const int t0 = (int)((int64_t)span.tiles * split / parts), t1 = (int)((int64_t)span.tiles * (split + 1) / parts);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -486,7 +476,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int TB = 128;         // queries of a workgroup
 template <typename T>
 constexpr int TT = sizeof(T) == 2 ? 64 : 32;  // positions of a tile
-constexpr int T_LEAST = 8;      // tiles of a part
 
 template <int CH>  // chunks of a row
 __device__ __forceinline__ int swizzle(int row) {
@@ -730,10 +719,10 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
   // a CU's second workgroup is short where its first is long
   const int split = rest % a.splits, nth = rest / a.splits, lead = a.slots - a.slots / 2;
   const int slot = nth < lead ? a.slots - 1 - nth : nth - lead;
-  const QueryBlock blk = many_block(c, a, slot);
+  const QueryBlock blk = find_block<TB>(c, a, slot);
   if (blk.count == 0) return;
   const Span<KT> span(c, a, blk);
-  const int parts = parts_of(span.tiles, a.splits, T_LEAST);
+  const int parts = parts_of(span.tiles, a.splits, a.least);
   if (split >= parts) return;
   const int t0 = (int)((int64_t)span.tiles * split / parts), t1 = (int)((int64_t)span.tiles * (split + 1) / parts);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -896,19 +885,21 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
   if (h == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = float2{st.m, lt};
 }
 
-// The parts of a query, joined in a fixed order.  Up to JOIN_FEW of them: 16 queries a
-// workgroup, 16 threads a query, all parts on their way at once.  More: a workgroup a
-// query, each wave every fourth part, eight on their way at once.
+// The parts of a query, joined in a fixed order.  Bound by two dependent round trips.  Up
+// to JOIN_FEW of them: 16 queries a workgroup, 16 threads a query, all parts on their way
+// at once (eight single tokens 72 us, 80 with the other form; chunks under a window 54
+// and 92).  More, which blocks of the card's size hold in no registers: a workgroup a query,
+// each wave every fourth part, eight on their way at once (64 parts of 32 queries 5.7 us).
 constexpr int JOIN_FEW = 8;
 
 template <typename T, int HD, int BQ, int TILE>
-__global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, const PagedAttnArgs a, int least) {
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, const PagedAttnArgs a) {
   constexpr int D = HD / 16;
   const int kvh = blockIdx.x % c.H, rest = blockIdx.x / c.H;
   const int q = rest % (BQ / 16) * 16 + threadIdx.x / 16, slot = rest / (BQ / 16);
-  const QueryBlock blk = BQ == RB ? few_block(c, a, slot) : many_block(c, a, slot);
+  const QueryBlock blk = find_block<BQ>(c, a, slot);
   const Span<TILE> span(c, a, blk);
-  const int parts = parts_of(span.tiles, a.splits, least);
+  const int parts = parts_of(span.tiles, a.splits, a.least);
   if (q >= blk.count || parts == 1) return;  // no query, or written whole
   const int64_t first = ((int64_t)slot * c.H + kvh) * a.splits * BQ + q;
   const float* po = a.part_o + first * HD + threadIdx.x % 16 * D;
@@ -948,13 +939,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, cons
 }
 
 template <typename T, int HD, int BQ, int TILE>
-__global__ __launch_bounds__(256) void paged_join_many_kernel(const PagedView c, const PagedAttnArgs a, int least) {
+__global__ __launch_bounds__(256) void paged_join_many_kernel(const PagedView c, const PagedAttnArgs a) {
   constexpr int D = HD / 64, U = 8, W = 4;
   const int nth = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int q = blockIdx.x % BQ, kvh = blockIdx.x / BQ % c.H, slot = blockIdx.x / BQ / c.H;
-  const QueryBlock blk = BQ == RB ? few_block(c, a, slot) : many_block(c, a, slot);
+  const QueryBlock blk = find_block<BQ>(c, a, slot);
   const Span<TILE> span(c, a, blk);
-  const int parts = parts_of(span.tiles, a.splits, least);
+  const int parts = parts_of(span.tiles, a.splits, a.least);
   if (q >= blk.count || parts == 1) return;  // for the whole workgroup alike
   const int64_t first = ((int64_t)slot * c.H + kvh) * a.splits * BQ + q;
   float mt = -CH_INF;
@@ -1007,39 +998,53 @@ __global__ __launch_bounds__(256) void paged_join_many_kernel(const PagedView c,
 }
 
 template <typename T, int HD, int BQ, int TILE>
-void join_go(const PagedView& c, const PagedAttnArgs& a, int least, hipStream_t st) {
+void join_go(const PagedView& c, const PagedAttnArgs& a, hipStream_t st) {
   const unsigned blocks = (unsigned)(a.slots * c.H);
   if (a.splits > JOIN_FEW)
-    hipLaunchKernelGGL((paged_join_many_kernel<T, HD, BQ, TILE>), dim3(blocks * BQ), dim3(256), 0, st, c, a, least);
+    hipLaunchKernelGGL((paged_join_many_kernel<T, HD, BQ, TILE>), dim3(blocks * BQ), dim3(256), 0, st, c, a);
   else
-    hipLaunchKernelGGL((paged_join_kernel<T, HD, BQ, TILE>), dim3(blocks * (BQ / 16)), dim3(256), 0, st, c, a, least);
+    hipLaunchKernelGGL((paged_join_kernel<T, HD, BQ, TILE>), dim3(blocks * (BQ / 16)), dim3(256), 0, st, c, a);
 }
 
 // ---- deal ------------------------------------------------------------------------
-constexpr int R_WGS = 1024;  // workgroups that fill the card: four a CU
-constexpr int T_WGS = 512;   // two a CU
-constexpr double FEW_FLOPS = 2.5e9;
+// Parts: a call's blocks of queries are cut until it has about the workgroups below, a
+// part no shorter than LEAST tiles (twice that where the kernel for few queries has a
+// workgroup a CU without a cut: 300 32-bit queries of 16 heads 10.8 us, 14.4 with cuts).
+//  - R_WGS: one token of 32768, 8 cache heads 34.5 us; 36 at 768, 38 at 1024.
+//  - T_WGS: a chunk of 2048 of 32 heads 124 us; 160 at 1024.  Eight chunks under a window
+//    of 1024 38 us; 48 at 768.
+//  - T_UNEVEN, for more than one sequence without a window, whose blocks differ: eight
+//    chunks behind up to 16000 positions 181 us, seven tokens and a chunk 114; 235 and 139
+//    at 512.  At 1024 164 and 120, and 63 tokens and a chunk 160 instead of 150.
+constexpr int CUS = 256, R_WGS = 512, T_WGS = 512, T_UNEVEN = 768, LEAST = 8;
 
 // Parts of a block's positions: as many as fill the card, none of them short.
-int64_t deal_splits(int64_t cap, int64_t blocks, int wgs, int tile, int least) {
-  const int64_t tiles = (cap + tile - 1) / tile + 2;  // a window's ends cut two more
+int64_t deal_splits(int64_t seen, int64_t blocks, int wgs, int tile, int least) {
+  const int64_t tiles = (seen + tile - 1) / tile + 2;  // a window's ends cut two more
   return std::max<int64_t>(1, std::min((wgs + blocks / 2) / blocks, (tiles + least - 1) / least));
 }
 // Partials of any call of up to `blocks` blocks: half a round over the card more than
 // one at most, or every block's most.
-int64_t deal_slots(int64_t cap, int64_t blocks, int wgs, int tile, int least) {
-  return std::min<int64_t>(std::min<int64_t>(blocks, wgs) * deal_splits(cap, 1, 1 << 30, tile, least), wgs + wgs / 2);
+int64_t deal_slots(int64_t cap, int64_t blocks, int wgs, int tile) {
+  return std::min<int64_t>(std::min<int64_t>(blocks, wgs) * deal_splits(cap, 1, 1 << 30, tile, LEAST), wgs + wgs / 2);
 }
 
-// Sequences of up to this many queries of a cache head go to the kernel for few.
-int few_queries(const PagedView& c, const PagedAttnArgs& a) {
-  const bool single = a.row0 == nullptr;
-  const int64_t most = single ? a.group : (int64_t)a.rows * a.group;
-  if (most <= RB) return RB;
-  const int64_t seen = a.window > 0 ? std::min<int64_t>(c.cap, (int64_t)a.window + a.sinks) : c.cap;
-  const double flops = 4.0 * a.rows * a.Hq * c.hd * (double)seen;
-  if (flops <= FEW_FLOPS) return (int)std::min<int64_t>(most, INT32_MAX);
-  return c.B == 1 && !single ? 0 : RB;
+// Positions that a query sees at most.
+int64_t seen_most(const PagedView& c, const PagedAttnArgs& a) {
+  return a.window > 0 ? std::min<int64_t>(c.cap, (int64_t)a.window + a.sinks) : c.cap;
+}
+// Whether a call goes to the kernel for few queries: where one block of it holds a
+// sequence's, and else by the work there can be, which the tiles of 128 queries do at
+// three times the rate once there is enough of it (32-bit ones at 1.4 times).
+// Few / many, us, at 32 heads of 128: 64 rows behind 2048 positions (2.1 GFLOP) 23 / 21, 256
+// behind none (1.1) 9 / 14, 512 behind none (4.3) 20 / 23, 128 behind 2048 (4.5) 31 / 25, 1024
+// behind none (17) 53 / 35; 32-bit, 16 heads: 1024 rows of heads of 64 (4.3) 39 / 49, of 128
+// (8.6) 82 / 92, 2048 (34) 259 / 189.  The host knows the table's positions, not the lengths:
+// 64 single tokens of up to 500 positions under tables of 32768 take 18 / 37.
+template <typename T>
+bool few_queries(const PagedView& c, const PagedAttnArgs& a, int64_t most) {
+  constexpr double FLOPS = sizeof(T) == 2 ? 2.5e9 : 9e9;
+  return most <= RB || 4.0 * a.rows * a.Hq * c.hd * (double)seen_most(c, a) <= FLOPS;
 }
 // Slots of a launch and, where every sequence has as many, those of one (else 0).
 struct Deal {
@@ -1058,33 +1063,23 @@ template <typename T, int HD>
 void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
   const bool single = a.row0 == nullptr;
   const int64_t most = single ? a.group : (int64_t)a.rows * a.group;  // queries of a sequence
-  float* at = (float*)ws;
-  a.few = few_queries(c, a);
-  if (a.few > 0 && (!single || most <= a.few)) {
-    PagedAttnArgs f = a;
-    const Deal d = deal(single, a.rows, c.B, a.group, a.few, RB);
-    f.slots = (int)d.slots;
-    f.per = d.per;
-    f.splits = (int)deal_splits(c.cap, d.slots * c.H, R_WGS, RT, R_LEAST);
-    const int64_t parts = d.slots * c.H * f.splits;
-    f.part_o = at;
-    f.part_ml = at + parts * RB * HD;
-    hipLaunchKernelGGL((paged_rows_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, f);
-    if (f.splits > 1) {
-      at = f.part_ml + parts * RB * 2;
-      join_go<T, HD, RB, RT>(c, f, R_LEAST, st);
-    }
-  }
-  if (most > a.few) {
-    const Deal d = deal(single, a.rows, c.B, a.group, most, TB);
-    a.slots = (int)d.slots;
-    a.per = d.per;
-    a.splits = (int)deal_splits(c.cap, d.slots * c.H, T_WGS, TT<T>, T_LEAST);
-    const int64_t parts = d.slots * c.H * a.splits;
-    a.part_o = at;
-    a.part_ml = at + parts * TB * HD;
+  const bool few = few_queries<T>(c, a, most);
+  const int block = few ? RB : TB, tile = few ? RT : TT<T>;
+  const Deal d = deal(single, a.rows, c.B, a.group, most, block);
+  const int64_t blocks = d.slots * c.H, seen = std::min<int64_t>(c.cap, seen_most(c, a) + block);
+  a.slots = (int)d.slots;
+  a.per = d.per;
+  a.least = few && blocks >= CUS ? 2 * LEAST : LEAST;
+  a.splits = (int)deal_splits(seen, blocks, few ? R_WGS : c.B > 1 && a.window == 0 ? T_UNEVEN : T_WGS, tile, a.least);
+  const int64_t parts = blocks * a.splits;
+  a.part_o = (float*)ws;
+  a.part_ml = a.part_o + parts * block * HD;
+  if (few) {
+    hipLaunchKernelGGL((paged_rows_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
+    if (a.splits > 1) join_go<T, HD, RB, RT>(c, a, st);
+  } else {
     hipLaunchKernelGGL((paged_tiles_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
-    if (a.splits > 1) join_go<T, HD, TB, TT<T>>(c, a, T_LEAST, st);
+    if (a.splits > 1) join_go<T, HD, TB, TT<T>>(c, a, st);
   }
 }
 
@@ -1092,9 +1087,10 @@ void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
 
 int64_t paged_attn_bytes(int64_t cap, int rows, int batch, int group, int H, int hd, int es) {
   const int64_t most = std::max<int64_t>((int64_t)rows * group, group);
-  const int64_t many = std::max(deal(false, rows, batch, group, most, TB).slots, deal(true, rows, batch, group, most, TB).slots);
-  const int tile = es == 2 ? TT<bf16_t> : TT<float>;
-  return (deal_slots(cap, R_WGS, R_WGS, RT, R_LEAST) * RB + deal_slots(cap, many * H, T_WGS, tile, T_LEAST) * TB) * (hd + 2) * 4;
+  const int64_t many =
+      std::max(deal(false, rows, batch, group, most, TB).slots, deal(true, rows, batch, group, most, TB).slots) * H;
+  return std::max(deal_slots(cap, R_WGS, R_WGS, RT) * RB, deal_slots(cap, many, T_UNEVEN, es == 2 ? TT<bf16_t> : TT<float>) * TB) *
+         (hd + 2) * 4;
 }
 
 void launch_paged_attn(int dtype, const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {

@@ -74,10 +74,9 @@ struct PagedAttnArgs {
   int window, sinks;        // window 0: every position
   float scale2;             // |scale| log2(e)
   int flip;                 // scale < 0: queries are negated
-  // a launch's own: parts of a block's positions at most, blocks of queries of one cache
-  // head, those of a sequence in the kernel for few queries
-  int splits, slots, per;
-  int few;                  // queries of a sequence that the kernel for few takes
+  // a launch's own: parts of a block's positions at most and tiles of one at least, blocks
+  // of queries of one cache head, those of each sequence (0: as its rows take)
+  int splits, least, slots, per;
   int vec_out;              // out rows at multiples of 16 bytes
   float* part_o;            // [slots][H][splits][block][hd]
   float* part_ml;           // [slots][H][splits][block][2]

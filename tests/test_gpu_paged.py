@@ -206,7 +206,7 @@ def attend(q, pool, table, lens, rows, dtype, scale, window=0, sinks=0, row0="st
     pages that the work is dealt as for a long cache, 128 queries at once."""
     total, Hq, hd = q.shape
     if far:
-        cap = int(4e9 / (4 * total * Hq * hd)) + 1
+        cap = int(1e10 / (4 * total * Hq * hd)) + 1
         wide = torch.full((table.shape[0], table.shape[1] + cap // pool.shape[3]), -1, dtype=torch.int32)
         wide[:, :table.shape[1]] = table
         table = wide
@@ -364,11 +364,11 @@ def test_attention_far(dtype, hd, case):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("window,sinks", [(1, 900), (64, 836), (500, 400), (1000, 0), (901, 128), (1 << 30, 3)])
+@pytest.mark.parametrize("window,sinks", [(1, 1150), (64, 1086), (500, 650), (1000, 150), (1200, 128), (1 << 30, 3)])
 def test_window_far(dtype, window, sinks):
     """Blocks of 128 queries whose first tiles and last ones lie apart, meet or overlap."""
-    check(dtype, [800, 0, 1300], [600, 3, 90], 8, 1, 128, 16, window + sinks, window, sinks, far=True)
-    check(dtype, [1200], [693], 8, 2, 128, 64, window + sinks, window, sinks, far=True)
+    check(dtype, [800, 0, 1300], [600, 3, 90], 24, 3, 128, 16, window + sinks, window, sinks, far=True)
+    check(dtype, [1200], [693], 24, 6, 128, 64, window + sinks, window, sinks, far=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -376,7 +376,7 @@ def test_parts_of_blocks_of_128(dtype):
     """Blocks whole, in two to eight parts and in more."""
     check(dtype, [4100], [40], 2, 1, 128, 16, 6, far=True)
     check(dtype, [3000, 900], [130, 1], 4, 2, 64, 64, 6, far=True)
-    check(dtype, [2500], [500], 16, 16, 64, 16, 7)
+    check(dtype, [2500], [500], 16, 16, 64, 16, 7, far=True)
     check(dtype, [2000, 0, 700], [20, 1, 300], 16, 16, 128, 16, 7, far=True)
 
 
