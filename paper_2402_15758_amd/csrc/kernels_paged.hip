@@ -7,8 +7,8 @@ namespace {
 
 // ---- the rotation's table ----------------------------------------------------------
 // table[p][i] = gain (cos, sin)(p theta_i), angles in 64 bits and rounded once: at
-// position 2^20 a 32-bit angle is off by up to 0.06.  A thread an entry; 33024
-// positions of 64 pairs take TIME us, once a model.
+// position 2^20 a 32-bit angle is off by up to 0.06.  A thread an entry; bound by the
+// 64-bit power, sine and cosine: 33024 positions of 64 pairs take 27 us, once a model.
 __global__ __launch_bounds__(256) void rope_table_kernel(const RopeArgs r, float2* __restrict__ table, int64_t n) {
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (e >= n) return;
@@ -77,7 +77,9 @@ __device__ __forceinline__ void store4(bf16_t* p, const float* x) {
 // but the norm's sum crosses lanes.  Pairs (i, i + P): values 4 j .. and P + 4 j ..
 // of lane j, the ones past the rotated part in order after them.  Neighbouring
 // pairs: eight values in a row.  VEC: both are runs of four values at aligned
-// addresses (P a multiple of 4).
+// addresses (P a multiple of 4); else a value at a time.
+// Bound by the bytes of many rows and by the launch of few: 2044 32-bit rows of 48 heads
+// into bf16 (76 MB) 17.5 us, 4.4 TB/s; one row 2.8 us, eight normed rows 3.3.
 // Elements of value v (0 .. 7) of lane j: pair v / 2 in either layout.
 __device__ __forceinline__ int element(int j, int v, int P, bool cross) {
   const int u = 4 * j + (v >> 1);

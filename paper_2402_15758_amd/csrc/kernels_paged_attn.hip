@@ -240,6 +240,11 @@ __device__ __forceinline__ void store_out(T* p, const float* x, bool vec) {
 // HD / 16 dimensions of exactly its group's keys, whole rows by 16 lanes, and pairs
 // them by byte permutes, so V needs no LDS either.  O^T's row 4 g + r of MFMA j is
 // dimension (4 g + r) HD / 16 + j.
+//
+// Bound by the cache's bytes where few queries read much of it: eight single tokens behind
+// 1024 to 4096 positions of 32 heads of 128 (336 MB) 69 us, 4.9 TB/s; one behind 32768 of 8
+// heads (134 MB) 28 us, 4.9 TB/s.  A wave keeps a tile's K and V in registers, so waves wait
+// for memory by themselves and not for each other.
 template <typename T, int HD>
 struct RowTile {
   static constexpr int VEC = ET<T>::VEC, KB = 4 * VEC, KS = HD / KB;
@@ -472,6 +477,13 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
 //
 // A row's 16-byte chunk x lies in place x ^ swizzle(row): the 16 rows of a K read and
 // the four rows x 64 bytes of half a transposed read then cover all banks once.
+//
+// Bound by the chain of scores, exponentials and products, two waves a SIMD: 2048 queries
+// of 32 heads of 128 behind 2048 positions take 124 us, 830 TFLOP/s (MFMA busy 34% of the
+// time, VALU 38%), behind 14336 positions 561 us, 918; heads of 64 76 us, 680.  32-bit, 2048
+// queries of 16 heads behind none: 188 us, 91 of 154 TFLOP/s.  A workgroup of eight waves,
+// four buffers with one workgroup a CU, and the next tile's scores beside this tile's
+// values took longer or spilt.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int TB = 128;         // queries of a workgroup
 template <typename T>
