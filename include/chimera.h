@@ -510,7 +510,7 @@ chimera_status chimera_rope_table(const chimera_rope* rope, void* table, int64_t
  * inputs.  A row whose sequence (-1 marks padding), position (within the table of
  * the rotation, too) or page there is not is skipped, its row of q_out left as it
  * was.  Rows of one call must name distinct slots: a slot named twice ends with a
- * mixture of its rows. */
+ * mixture of its rows.  At most 2^30 rows. */
 chimera_status chimera_paged_append(const chimera_paged* cache, int32_t dtype, const void* q, const void* k, const void* v,
                                     int64_t ld, int32_t n_heads, const int32_t* seq, const int32_t* pos, int32_t rows,
                                     const chimera_rope* rope, const void* table, const float* q_gain,
@@ -526,13 +526,14 @@ chimera_status chimera_paged_append(const chimera_paged* cache, int32_t dtype, c
  * those above p - window and the first `sinks`.  out = softmax(scale q K^T) V over
  * them.
  * Scores, softmax and sums are float32, the weights rounded once to bf16 where the
- * cache is, the result rounded once.  A score whose q K^T, or scale times it in base 2, passes 2^128 is an infinity: a negative one
- * weighs nothing, a row with a positive one or with nothing else becomes NaN.  |scale|
- * is at most 2^127.  Positions that the cache does not have are not seen; a row that
+ * cache is, the result rounded once.  A score whose q K^T, or scale times it in base 2,
+ * passes 2^128 is an infinity: a negative one weighs nothing, a row with a positive one
+ * or with nothing else becomes NaN.  |scale| is at most 2^127.  Positions that the cache does not have are not seen; a row that
  * sees none becomes zeros, and so do the rows of a sequence whose n_b is negative.
  * Nothing that a row does not see reaches it, infinities and NaN included.  n_b is at
- * most 2^30.  q: rows at multiples of 16 bytes; out at any element; ws: 16-byte
- * aligned, chimera_paged_attn_bytes long.  Equal calls give equal bits; a row's last
+ * most 2^30, rows * n_heads 2^26, batch * n_heads 2^23.  q: rows at multiples of 16
+ * bytes; out at any element, overlapping no input; ws: 16-byte aligned,
+ * chimera_paged_attn_bytes long.  Equal calls give equal bits; a row's last
  * bits may depend on the other rows of its call. */
 chimera_status chimera_paged_attn_bytes(const chimera_paged* cache, int32_t n_heads, int32_t rows, int64_t* bytes);
 chimera_status chimera_paged_attn(const chimera_paged* cache, const void* q, int64_t ldq, int32_t n_heads,

@@ -59,7 +59,7 @@ __device__ __forceinline__ QueryBlock find_block(const PagedView& c, const Paged
       len = min(step, len - last * step);
     }
   }
-  k.n = min(k.n, 1 << 30);
+  k.n = max(min(k.n, 1 << 30), -1);
   k.v0 = at * BQ;
   k.count = at < 0 ? 0 : max(min(rows * a.group - k.v0, BQ), 0);
   return k;

@@ -141,7 +141,7 @@ chimera_status chimera_paged_append(const chimera_paged* cache, int32_t dtype, c
   return guard([&] {
     check_paged(cache);
     check_dtype(dtype);
-    REQUIRE(rows >= 0, CHIMERA_EINVAL, "rows");
+    REQUIRE(rows >= 0 && rows <= 1 << 30, CHIMERA_EINVAL, "rows in [0, 2^30]");
     const int64_t hd = cache->head_dim;
     if (q == nullptr) {
       REQUIRE(n_heads == 0 && q_out == nullptr && q_gain == nullptr, CHIMERA_EINVAL,

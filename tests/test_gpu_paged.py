@@ -509,3 +509,86 @@ def test_offsets_past_32_bits():
     for r, (b, at) in enumerate([(0, 5), (1, 131)]):
         held = pool[int(table[b, at // page]), :, :, at % page]
         assert torch.equal(held.reshape(-1), x[r, H * hd:])
+
+
+def test_numbers_at_the_ends_of_their_range():
+    """Lengths, sequences and positions far outside: rows of zeros, rows left out."""
+    lo, hi = -(1 << 31), (1 << 31) - 1
+    q, pool, table = attn_inputs("bf16", [40, 3], [1, 1], 4, 2, 64, 16, 21, poison=False)
+    for window, sinks in ((0, 0), (1 << 30, 0), (7, 1 << 30)):
+        for rows in ([1, 1], [3, 40]):
+            got = attend(q[:1].expand(sum(rows), 4, 64).contiguous(), pool, table, [lo, -7], rows, "bf16", 0.125, window,
+                         sinks)
+            assert bool((got == 0).all())
+    # past the table: all that it has is seen
+    for far in (False, True):
+        got = attend(q, pool, table, [1 << 30, 3], [1, 1], "bf16", 0.125, far=far)
+        cap = table.shape[1] * 16
+        ref, mag, big = R.attention(q, pool, table, [cap - 1, 3], [1, 1], 0.125)
+        assert bool(((got - ref).abs() <= R.attention_bound("bf16", ref, mag, big, cap, 64)).all())
+    dp, dt = pool.cuda(), table.cuda()
+    before, x = dp.clone(), torch.randn(6, 8 * 64, device="cuda").bfloat16()
+    out = torch.full((6, 256), 3.0, dtype=torch.bfloat16, device="cuda")
+    seq = torch.tensor([lo, hi, 0, 0, 2, -1], dtype=torch.int32, device="cuda")
+    pos = torch.tensor([0, 0, lo, hi, 0, 5], dtype=torch.int32, device="cuda")
+    p = x.data_ptr()
+    for rope in (None, "half"):
+        r, rt, _ = rope_of(ROPES[rope], 64, 50) if rope else (None, None, None)
+        B.chimera_paged_append(cache_of(dp, dt, "bf16"), B.CHIMERA_BF16, p, p + 512, p + 768, 512, 4, seq.data_ptr(),
+                               pos.data_ptr(), 6, r, rt.data_ptr() if rope else None, None, None, 0.0, out.data_ptr(),
+                               256, stream())
+        assert torch.equal(dp, before) and bool((out == 3).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_thousand_query_heads(dtype):
+    check(dtype, [50, 0], [1, 1], 1024, 1, 64, 16, 22, row0=None, behind=0)
+    check(dtype, [50, 9], [1, 2], 1000, 8, 128, 16, 22)
+    check(dtype, [30], [2], 1024, 1024, 64, 4, 22)
+
+
+def test_a_captured_call_follows_the_device():
+    """Lengths, rows and pages change between replays; the call's shape does not."""
+    for dtype, hd, total, cap in (("bf16", 128, 300, 600), ("f32", 64, 40, 200), ("bf16", 64, 7, 5000)):
+        g = torch.Generator().manual_seed(total)
+        page, batch, Hq, H = 16, 5, 4, 2
+        table, n_pages = table_of(g, batch, cap, page)
+        pool = torch.randn(n_pages, 2, H, page, hd, generator=g).to(R.TYPES[dtype])
+        dq = torch.zeros(total, Hq * hd, dtype=R.TYPES[dtype], device="cuda")
+        out = torch.zeros_like(dq)
+        dt, dp = table.cuda(), pool.cuda()
+        n = torch.zeros(batch, dtype=torch.int32, device="cuda")
+        starts = torch.zeros(batch + 1, dtype=torch.int32, device="cuda")
+        c = cache_of(dp, dt, dtype)
+        nb = B.chimera_paged_attn_bytes(c, Hq, total)
+        ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+
+        def call():
+            B.chimera_paged_attn(c, dq.data_ptr(), Hq * hd, Hq, starts.data_ptr(), n.data_ptr(), total, 0, 0, 0.1,
+                                 out.data_ptr(), Hq * hd, ws.data_ptr(), nb, stream())
+
+        graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            call()
+        for i in range(4):
+            cuts = sorted(torch.randint(0, total + 1, (batch - 1,), generator=g).tolist())
+            rows = [b - a for a, b in zip([0] + cuts, cuts + [total])]
+            lens = [int(torch.randint(0, max(cap - r, 1), (1,), generator=g)) for r in rows]
+            order = torch.randperm(n_pages, generator=g)[:table.numel()].view(table.shape).int()
+            q = torch.randn(total, Hq, hd, generator=g).to(R.TYPES[dtype])
+            dq.copy_(q.reshape(total, -1))
+            dt.copy_(order)
+            n.copy_(torch.tensor(lens))
+            starts.copy_(torch.tensor([0] + cuts + [total]))
+            out.fill_(7.0)
+            ws.fill_(0xFF)
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            ref, mag, big = R.attention(q, pool, order, lens, rows, R.f32(0.1))
+            bound = R.attention_bound(dtype, ref, mag, big, cap + total, hd)
+            assert bool(((got.double().cpu().view(total, Hq, hd) - ref).abs() <= bound).all())
+            call()
+            torch.cuda.synchronize()
+            assert torch.equal(got, out)

@@ -85,6 +85,7 @@ def test_rope_table_refusals():
 def test_append_refusals():
     refused(E, "dtype", lambda: append(dt=2))
     refused(E, "rows", lambda: append(rows=-1))
+    refused(E, "rows", lambda: append(rows=(1 << 30) + 1))
     for n in ("k", "v", "seq", "pos", "out"):
         refused(E, "null", lambda: append(**{n: None}))
     refused(E, "stride", lambda: append(ld=255))
