@@ -13,7 +13,7 @@
 
 namespace {
 
-// 2^(y / 32) for y <= 0: y = n + f, |f| <= 1/2, 2^(n / 32) = 2^(n >> 5) times a table's
+// 2^(y / 32): y = n + f, |f| <= 1/2, 2^(n / 32) = 2^(n >> 5) times a table's
 // entry, and Taylor's series of e^(f ln 2 / 32) up to the fifth power (the next is below
 // 2^-48).  A weight is exp((z - m) / T) = 2^(y / 32) with y = (z - m) 32 / (T ln 2): the
 // sum of a row's errors stays below 2^-47 of its weights.  0 from 2^-1100 on.
@@ -111,7 +111,7 @@ __device__ __forceinline__ void load_part(const T* z, int n, int lane, float (&x
 // Grid (rows, groups of four parts, target | draft), a wave a part.  A NaN or +inf makes a
 // part's sum NaN: such a row has no distribution.  Bound by 25 instructions an entry, most
 // of them in 64 bits: 704 bf16 rows of 128256 (181 MB) 80 us, VALU busy 74%; 64 32-bit rows
-// of 32000 (8 MB) 5 us.  Four parts a wave: the same times.
+// of 32000 (8 MB) 5 us.  Four parts a wave: the same times.  Many bf16 rows: below.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
   __shared__ double table[32];
@@ -148,6 +148,99 @@ __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
     const int64_t at = ((int64_t)blockIdx.z * a.B * a.N + row) * a.parts + part;
     a.part_m[at] = m;
     a.part_s[at] = s;
+  }
+}
+
+// The same of bf16 rows by a table: a logit has 13 bits between 2^-25 and 2^7 in magnitude,
+// and exp(z / T) of all of them stays within a double's range from T = 1/4 on.  A part
+// whose logits all lie there is summed with 0 for its largest; the others as above.
+// A workgroup lays the table out once and its waves take part after part, the next one's
+// entries on their way while one is summed.  Bound by memory and the table's reads, 8
+// instructions an entry: 704 rows of 128256 (181 MB) 40 us, 4.5 TB/s.
+constexpr int TABLED = 8192;
+constexpr uint32_t TABLED_UP = 26 << 7;  // takes the exponents to 4 x 32 .. 4 x 32 + 31
+__global__ __launch_bounds__(1024, 8) void accept_parts_tabled_kernel(const AcceptArgs a, int64_t items) {
+  __shared__ double w[TABLED], table[32];
+  const int lane = threadIdx.x & 63;
+  fill_table(table);
+  __syncthreads();
+  for (int i = threadIdx.x; i < TABLED; i += 1024) {
+    const uint32_t bits = (uint32_t)(i >> 12) << 15 | ((0x4000u | (i & 0xfff)) - TABLED_UP);
+    w[i] = pow32(exponent(__uint_as_float(bits << 16), 0.0, a.scale), table);
+  }
+  __syncthreads();
+  const int64_t stride = (int64_t)gridDim.x * 16;
+  const int rows = a.B * a.N;
+  int4 x[2];
+  bool here = false;
+  auto load = [&](int64_t item) {
+    const int all = (int)(item / a.parts), part = (int)(item - (int64_t)all * a.parts);
+    const bool of_draft = all >= rows;
+    const int row = of_draft ? all - rows : all, b = row / a.N;
+    const bf16_t* z = of_draft ? (const bf16_t*)a.draft + (int64_t)row * a.ldd : (const bf16_t*)a.logits + (int64_t)row * a.ld;
+    here = a.tokens[(int64_t)b * a.N] >= 0 && !(of_draft && !((a.inner >> (row - b * a.N)) & 1));
+    if (!here) return;
+    const int n = a.V - part * ACCEPT_PART;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int v = lane * 8 + 512 * i;
+      const bf16_t* p = z + part * ACCEPT_PART + v;
+      if (v + 8 <= n) {
+        x[i] = ld16(p);
+      } else {
+        uint32_t u[4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t one = v + k < n ? (uint32_t)p[k] : 0xff80u;
+          u[k / 2] = k & 1 ? u[k / 2] | one << 16 : one;
+        }
+        x[i] = int4{(int)u[0], (int)u[1], (int)u[2], (int)u[3]};
+      }
+    }
+  };
+  int64_t item = (int64_t)blockIdx.x * 16 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (item < items) load(item);
+  for (; item < items; item += stride) {
+    const uint32_t u[8] = {(uint32_t)x[0].x, (uint32_t)x[0].y, (uint32_t)x[0].z, (uint32_t)x[0].w,
+                           (uint32_t)x[1].x, (uint32_t)x[1].y, (uint32_t)x[1].z, (uint32_t)x[1].w};
+    const bool now = here;
+    if (item + stride < items) load(item + stride);
+    if (!now) continue;
+    uint32_t off = 0;
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // a carry between the two happens only where the lower one is out of the table
+      const uint32_t c = u[i] + (TABLED_UP << 16 | TABLED_UP);
+      off |= c ^ 0x40004000u;
+      const char* t = (const char*)w;
+      s = s + *(const double*)(t + ((c << 3 & 0x7ff8u) | (c & 0x8000u)));
+      s = s + *(const double*)(t + ((c >> 13 & 0x7ff8u) | (c >> 16 & 0x8000u)));
+    }
+    float m = 0.f;
+    if (__ballot((off & 0x70007000u) != 0) != 0) {
+      float y[16];
+      bool bad = false;
+      m = -CH_INF;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        y[k] = __uint_as_float(k & 1 ? u[k / 2] & 0xffff0000u : u[k / 2] << 16);
+        bad = bad || !(y[k] < CH_INF);
+        m = fmaxf(m, y[k]);
+      }
+      m = wave_max(m);
+      s = 0.0;
+      if (m != -CH_INF) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s = s + pow32(exponent(y[k], (double)m, a.scale), table);
+      }
+      if (bad) s = __builtin_nan("");
+    }
+    s = wave_sum_f64(s);
+    if (lane == 0) {
+      a.part_m[item] = m;
+      a.part_s[item] = s;
+    }
   }
 }
 
@@ -495,10 +588,18 @@ __global__ void accept_first_kernel(const PrefillEnds e, unsigned long long seed
   tokens[j] = 0;
 }
 
+// The table costs 3 us: 6048 parts 29 us with it and 26 without, 8064 18.9 and 18.2, 10240
+// 24.5 and 25.1, 12096 32 and 35, 96768 72 and 106 (whole calls).  One workgroup a CU: 79.
+constexpr int64_t TABLED_PARTS = 10000;
+constexpr int TABLED_WGS = 512;  // two a CU
 template <typename T, bool VEC>
 void accept_go(const AcceptArgs& a, hipStream_t st) {
   const int rows = a.B * a.N, kinds = a.draft != nullptr ? 2 : 1;
-  hipLaunchKernelGGL((accept_parts_kernel<T, VEC>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
+  const int64_t items = (int64_t)rows * kinds * a.parts;
+  if (sizeof(T) == 2 && VEC && items >= TABLED_PARTS && a.scale <= accept_scale(0.25f))
+    hipLaunchKernelGGL(accept_parts_tabled_kernel, dim3(TABLED_WGS), dim3(1024), 0, st, a, items);
+  else
+    hipLaunchKernelGGL((accept_parts_kernel<T, VEC>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
   if (a.draft != nullptr && a.N > 1) {
     hipLaunchKernelGGL((accept_walk_kernel<T>), dim3(a.B), dim3(1024), 0, st, a);
     hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3((a.parts + 3) / 4, a.B), dim3(256), 0, st, a);

@@ -230,3 +230,56 @@ def test_accepted_at_the_targets_rate():
         first = torch.tensor([o[0][0] for o in run(logits, draft, tokens, parents, u, 1.0, V)])
         freq = torch.bincount(first, minlength=V).double() / n
         assert bool(((freq - p).abs() <= 5 * torch.sqrt(p * (1 - p) / n)).all())
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("temperature", [0.2499, 0.25, 1.0, 7.0])
+@pytest.mark.parametrize("vocab,pad", [(2048, 0), (2050, 0), (2050, 6)])
+def test_many_bf16_rows(drawn, temperature, vocab, pad):
+    """Enough parts for the sums by a table (from 1/4 on, where rows lie at multiples of 16
+    bytes): the walks of the rule, and those of few rows at once."""
+    parents = tree(9, 1) if drawn else tree(64, 4)
+    batch = 420 if drawn else 85
+    logits, draft, tokens, u = inputs(batch, parents, vocab, drawn, "bf16", 31, 0.8, temperature)
+    logits = torch.nn.functional.pad(logits, (0, pad), value=90.0)
+    draft = torch.nn.functional.pad(draft, (0, pad), value=90.0) if drawn else None
+    check(logits, draft, tokens, parents, u, temperature, vocab)
+    all_of = run(logits, draft, tokens, parents, u, temperature, vocab)
+    N = len(parents)
+    few = run(logits[:5 * N], None if draft is None else draft[:5 * N], tokens[:5], parents, u[:5], temperature, vocab)
+    assert all_of[:5] == few
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_many_bf16_rows_outside_the_table(drawn):
+    """Zeros, tiny and large logits, masked ones and rows without a distribution among
+    rows of a table: parts of either kind in one row, too."""
+    vocab, N = 4096, 9
+    parents = tree(N, 1)
+    logits, draft, tokens, u = inputs(320, parents, vocab, drawn, "bf16", 32, 0.9)
+    for x in (logits, draft) if drawn else (logits,):
+        x = x.view(320, N, vocab)
+        x[0:20, :, 100] = 0.0
+        x[20:40, :, :1024] = 0.0
+        x[40:60, :, 1024:2048] = 2.0 ** -30
+        x[60:80] += 127.0
+        x[80:100] -= 140.0
+        x[100:120] *= 2000.0
+        x[120:140, :, 1000:] = -math.inf
+        x[140:160, :, 5:4090] = -math.inf
+        x[160:180, :, ::2] = -math.inf
+        x[180:190, 1:] = -math.inf
+        x[190:200, 2, 77] = math.nan
+        x[200:210, 1, 4095] = math.inf
+        x[210:230] = 3.0
+        x[230:250] = -0.0
+        x[250:260] = 2.0 ** 7
+        x[260:270] = -(2.0 ** 7 - 0.5)
+        x[270:280] = 2.0 ** -25
+    g = torch.Generator().manual_seed(33)
+    for temperature in (1.0, 0.25):
+        if drawn:  # from what the draft's rows became
+            q = torch.softmax(draft.double() / temperature, -1)
+            rows = [r for r in range(320 * N) if r % N < N - 1 and not bool(q[r].isnan().any())]
+            tokens.view(-1)[[r + 1 for r in rows]] = torch.multinomial(q[rows], 1, generator=g)[:, 0]
+        check(logits, draft, tokens, parents, u, temperature, vocab)
