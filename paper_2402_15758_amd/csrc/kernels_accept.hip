@@ -46,10 +46,13 @@ __device__ __forceinline__ double pow32(double y, const double* table) {
 // (z - m) 32 / (T ln 2); scale: 32 / (T ln 2), at most 2^156
 __device__ __forceinline__ double exponent(float z, double m, double scale) { return ((double)z - m) * scale; }
 
-__device__ __forceinline__ double shfl_f64(double v, int lane) {
+__device__ __forceinline__ double f64_of(uint32_t lo, uint32_t hi) {
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double v) {  // 0 from lanes that are not there
   const uint64_t u = (uint64_t)__double_as_longlong(v);
-  return __longlong_as_double((long long)((uint64_t)(uint32_t)__shfl((int)(uint32_t)u, lane) |
-                                          ((uint64_t)(uint32_t)__shfl((int)(uint32_t)(u >> 32), lane) << 32)));
+  return f64_of((uint32_t)dpp_mov_i<CTRL>((int)(uint32_t)u), (uint32_t)dpp_mov_i<CTRL>((int)(uint32_t)(u >> 32)));
 }
 // A uniform lane's value, without a trip through LDS.
 __device__ __forceinline__ double lane_f64(double v, int lane) {
@@ -60,19 +63,29 @@ __device__ __forceinline__ double lane_f64(double v, int lane) {
 }
 // Over the 64 lanes, in the same order on each.
 __device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v = v + shfl_f64(v, (threadIdx.x & 63) ^ d);
-  return v;
+  v = v + dpp_f64<DPP_XOR1>(v);
+  v = v + dpp_f64<DPP_XOR2>(v);
+  v = v + dpp_f64<DPP_MIRROR8>(v);
+  v = v + dpp_f64<DPP_MIRROR16>(v);
+  uint64_t u = (uint64_t)__double_as_longlong(v);
+  auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+  auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  v = f64_of(lo[0], hi[0]) + f64_of(lo[1], hi[1]);
+  u = (uint64_t)__double_as_longlong(v);
+  lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return f64_of(lo[0], hi[0]) + f64_of(lo[1], hi[1]);
 }
-// The sum of lanes 0 .. own.
+// The sum of lanes 0 .. own: within rows of 16, then the rows before.
 __device__ __forceinline__ double wave_scan_f64(double v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const double w = shfl_f64(v, max(lane - d, 0));
-    v = lane >= d ? v + w : v;
-  }
-  return v;
+  enum { SHR1 = 0x111, SHR2 = 0x112, SHR4 = 0x114, SHR8 = 0x118 };
+  v = v + dpp_f64<SHR1>(v);
+  v = v + dpp_f64<SHR2>(v);
+  v = v + dpp_f64<SHR4>(v);
+  v = v + dpp_f64<SHR8>(v);
+  const double r0 = lane_f64(v, 15), r1 = r0 + lane_f64(v, 31), r2 = r1 + lane_f64(v, 47);
+  const int row = (threadIdx.x & 63) >> 4;
+  return v + (row == 0 ? 0.0 : row == 1 ? r0 : row == 2 ? r1 : r2);
 }
 
 template <typename T>
@@ -427,6 +440,7 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   __shared__ double wave_s[16], redo[64];
   __shared__ int part_sh, first_sh[16], last_sh[16];
   __shared__ double before_sh, target_sh;
+  const double u0 = a.u[row0];
   if (a.draft != nullptr && a.N > 1) {
     fill_table(sh.table);
     if (tid == 0) sh.walk = a.walks[b];
@@ -464,11 +478,8 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   Weights<T> f{(const T*)a.logits + row * a.ld, resid ? (const T*)a.draft + row * a.ldd : nullptr, w.p.m, w.q.m, a.scale,
                resid ? 1.0 / w.p.s : 1.0, resid ? 1.0 / w.q.s : 1.0, sh.table};
   int ng = n_gone;
-  auto is_gone = [&](int v) {
-    bool g = false;
-    for (int i = 0; i < ng; ++i) g = g || gone[i] == v;
-    return g;
-  };
+  const int gone_l = lane < ng ? gone[lane] : -1;  // one a lane
+  auto gone_of = [&](int i) { return __builtin_amdgcn_readlane(gone_l, i); };
   // Parts that hold a rejected token are summed without it, a wave each: taking it off
   // the sum would leave rounding where it was most of it.
   const int64_t parts0 = row * a.parts;
@@ -480,20 +491,26 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   }
   for (int i = wave - 1; i < ng; i += 15) {
     if (wave == 0) break;
-    const int v0 = gone[i] / ACCEPT_PART * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
+    const int v0 = gone_of(i) / ACCEPT_PART * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
     constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
     float x[16];
     load_part<T, VEC>(f.z + v0, n, lane, x);
+    uint32_t out = 0;  // this lane's entries that are gone
+    for (int j = 0; j < ng; ++j) {
+      const int r = gone_of(j) - v0;
+      if (r >= 0 && r < ACCEPT_PART && lane == r / E % 64) out |= 1u << (r / (64 * E) * E + r % E);
+    }
     double s = 0.0;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       const double one = pow32(exponent(x[k], w.p.m, a.scale), sh.table);
-      s = s + (is_gone(v0 + lane * E + 64 * E * (k / E) + k % E) ? 0.0 : one);
+      s = s + ((out >> k) & 1 ? 0.0 : one);
     }
     s = wave_sum_f64(s);
     if (lane == 0) redo[i] = s;
   }
   __syncthreads();
+  const double redo_l = lane < ng ? redo[lane] : 0.0;
   // The part where the running sum passes, by one wave, 64 parts at a time.  Rounding
   // may leave no weight at all behind rejections (the mass that was left was its own
   // error): then the row's own probabilities decide.
@@ -503,29 +520,29 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
         if (i >= a.parts) return 0.0;
         const bool kept = i < 64 && attempt == 0;
         if (f.zq != nullptr) return kept ? ps0 : a.resid[(int64_t)b * a.parts + i];
-        for (int j = 0; j < ng; ++j)
-          if (gone[j] / ACCEPT_PART == i) return redo[j];
         const float pm = kept ? pm0 : a.part_m[parts0 + i];
         const double ps = kept ? ps0 : a.part_s[parts0 + i];
-        return pm == -CH_INF ? 0.0 : ps * pow32(exponent(pm, w.p.m, a.scale), sh.table) * f.one;
+        double of = pm == -CH_INF ? 0.0 : ps * pow32(exponent(pm, w.p.m, a.scale), sh.table) * f.one;
+        for (int j = 0; j < ng; ++j) of = gone_of(j) / ACCEPT_PART == i ? lane_f64(redo_l, j) : of;
+        return of;
       };
-      double total = 0.0;
-      for (int i0 = 0; i0 < a.parts; i0 += 64) total = total + wave_sum_f64(part_weight(i0 + lane));
-      const double u0 = a.u[row0];
+      const double pw0 = part_weight(lane);
+      double total = wave_sum_f64(pw0);
+      for (int i0 = 64; i0 < a.parts; i0 += 64) total = total + wave_sum_f64(part_weight(i0 + lane));
       const double target = (u0 > 0.0 ? u0 : 0.0) * total;
       double before = 0.0, last_before = 0.0;
       int last = -1;
       for (int i0 = 0; i0 < a.parts; i0 += 64) {
-        const double pw = part_weight(i0 + lane);
+        const double pw = i0 == 0 ? pw0 : part_weight(i0 + lane);
         const double upto = before + wave_scan_f64(pw);
         const uint64_t over = __ballot(pw > 0.0 && upto > target), some = __ballot(pw > 0.0);
         const int at = over != 0 ? __ffsll((long long)over) - 1 : some != 0 ? 63 - __clzll((long long)some) : -1;
         if (at >= 0) {
           last = i0 + at;
-          last_before = shfl_f64(upto - pw, at);
+          last_before = lane_f64(upto - pw, __builtin_amdgcn_readfirstlane(at));
         }
         if (over != 0) break;
-        before = shfl_f64(upto, 63);
+        before = lane_f64(upto, 63);
       }
       if (lane == 0) {
         part_sh = last;
@@ -547,7 +564,9 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   // within the part, an entry a thread
   static_assert(ACCEPT_PART == 1024, "an entry a thread");
   const int v = part_sh * ACCEPT_PART + tid;
-  const double x = v < a.V && !is_gone(v) ? f(v) : 0.0;
+  bool held = v < a.V;
+  for (int j = 0; j < ng; ++j) held = held && gone_of(j) != v;
+  const double x = held ? f(v) : 0.0;
   const double scan = wave_scan_f64(x);
   if (lane == 63) wave_s[wave] = scan;
   __syncthreads();
