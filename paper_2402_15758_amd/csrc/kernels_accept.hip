@@ -284,7 +284,7 @@ __device__ __forceinline__ RowSum row_sum(const AcceptArgs& a, int64_t row, cons
 // of their ids; the walk goes on at the first accepted one and ends where there is
 // none.  The sums of all rows with children and all nodes' probabilities come first, so
 // the walk itself touches no memory but for the row of a node without children.  Bound by
-// that chain of round trips: 64 chains of 5 over 126 parts a row 8 us.
+// that chain: a tree of 64 nodes over 32 parts a row 4 us.
 struct WalkSpace {
   double table[32];
   RowSum rows[2][64];
@@ -391,30 +391,27 @@ struct Weights {
   }
 };
 
-// Drawn tokens: the walks, a workgroup a sequence, and then every part of the residual,
-// grid (groups of four parts, sequences), a wave a part, since a workgroup a sequence would
-// leave the card idle (64 rows of 128256, two exponentials an entry: 16 us).
-template <typename T>
-__global__ __launch_bounds__(1024) void accept_walk_kernel(const AcceptArgs a) {
-  __shared__ WalkSpace sh;
-  accept_walk<T, 16>(a, blockIdx.x, sh);
-  if (threadIdx.x == 0) a.walks[blockIdx.x] = sh.walk;
-}
-
+// Drawn tokens: every part of the residual, grid (groups of RESID parts, sequences), a wave
+// a part, since a workgroup a sequence would leave the card idle.  Each workgroup walks by
+// itself and the first of a sequence leaves the walk for the next launch.  Bound by the
+// walk's chain and 64-bit instructions, 50 an entry: 8 sequences of 32000 9 us, 64 of 128256
+// 22.  Whole calls with 4, 8 or 16 parts a workgroup: 19.5, 19.8 and 22.1 us for the 8
+// sequences, 71, 69 and 67 for the 64; with a launch for the walks 21.3 and 70.
+constexpr int RESID = 8;  // parts of a workgroup
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void accept_resid_kernel(const AcceptArgs a) {
-  __shared__ double table[32];
+__global__ __launch_bounds__(64 * RESID) void accept_resid_kernel(const AcceptArgs a) {
+  __shared__ WalkSpace sh;
   const int b = blockIdx.y, lane = threadIdx.x & 63;
-  const int part = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Walk w = a.walks[b];
+  const int part = blockIdx.x * RESID + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  accept_walk<T, RESID>(a, b, sh);
+  const Walk w = sh.walk;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.walks[b] = w;
   if (w.node < 0 || !w.ok || w.rejected == 0) return;
-  fill_table(table);
-  __syncthreads();
   const int v0 = part * ACCEPT_PART;
   if (v0 >= a.V) return;
   const int64_t row = (int64_t)b * a.N + w.node;
   const Weights<T> f{(const T*)a.logits + row * a.ld, (const T*)a.draft + row * a.ldd, w.p.m, w.q.m, a.scale,
-                     1.0 / w.p.s, 1.0 / w.q.s, table};
+                     1.0 / w.p.s, 1.0 / w.q.s, sh.table};
   float x[16], xq[16];
   const int n = min(ACCEPT_PART, a.V - v0);
   load_part<T, VEC>(f.z + v0, n, lane, x);
@@ -428,7 +425,7 @@ __global__ __launch_bounds__(256) void accept_resid_kernel(const AcceptArgs a) {
 
 // A workgroup of 1024 a sequence: the walk, its results, and the first entry whose
 // running sum passes u[0] of the whole, by parts and then within one.  Bound by its chain
-// of round trips and barriers: a tree of 64 nodes 14 us with its walk, 64 chains 7.5
+// of round trips and barriers: a tree of 64 nodes 10 us with its walk, 64 chains 6.5
 // without.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
@@ -619,10 +616,8 @@ void accept_go(const AcceptArgs& a, hipStream_t st) {
     hipLaunchKernelGGL(accept_parts_tabled_kernel, dim3(TABLED_WGS), dim3(1024), 0, st, a, items);
   else
     hipLaunchKernelGGL((accept_parts_kernel<T, VEC>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
-  if (a.draft != nullptr && a.N > 1) {
-    hipLaunchKernelGGL((accept_walk_kernel<T>), dim3(a.B), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3((a.parts + 3) / 4, a.B), dim3(256), 0, st, a);
-  }
+  if (a.draft != nullptr && a.N > 1)
+    hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3((a.parts + RESID - 1) / RESID, a.B), dim3(64 * RESID), 0, st, a);
   hipLaunchKernelGGL((accept_pick_kernel<T, VEC>), dim3(a.B), dim3(1024), 0, st, a);
 }
 template <typename T>
