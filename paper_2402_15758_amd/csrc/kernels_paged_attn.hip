@@ -899,9 +899,9 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
 
 // The parts of a query, joined in a fixed order.  Bound by two dependent round trips.  Up
 // to JOIN_FEW of them: 16 queries a workgroup, 16 threads a query, all parts on their way
-// at once (eight single tokens 72 us, 80 with the other form; chunks under a window 54
-// and 92).  More, which blocks of the card's size hold in no registers: a workgroup a query,
-// each wave every fourth part, eight on their way at once (64 parts of 32 queries 5.7 us).
+// at once (eight single tokens 72 us, 80 with the other form; 2 to 3 parts of 16000 queries
+// 7 us, 45 MB).  More: a workgroup a query, each wave every fourth part, eight on their way
+// at once (64 parts of 32 queries 4.7 us).
 constexpr int JOIN_FEW = 8;
 
 template <typename T, int HD, int BQ, int TILE>
@@ -919,10 +919,14 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, cons
   float4 o[JOIN_FEW][D / 4];
 #pragma unroll
   for (int i = 0; i < JOIN_FEW; ++i) {
-    const int k = min(i, parts - 1);
-    ml[i] = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)k * BQ) * 2);
+    ml[i] = float2{-CH_INF, 0.f};
 #pragma unroll
-    for (int j = 0; j < D / 4; ++j) o[i][j] = *reinterpret_cast<const float4*>(po + (int64_t)k * BQ * HD + 4 * j);
+    for (int j = 0; j < D / 4; ++j) o[i][j] = float4{0.f, 0.f, 0.f, 0.f};
+    if (i < parts) {
+      ml[i] = *reinterpret_cast<const float2*>(a.part_ml + (first + (int64_t)i * BQ) * 2);
+#pragma unroll
+      for (int j = 0; j < D / 4; ++j) o[i][j] = *reinterpret_cast<const float4*>(po + (int64_t)i * BQ * HD + 4 * j);
+    }
   }
   float mt = ml[0].x;
 #pragma unroll
@@ -932,7 +936,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, cons
   for (int j = 0; j < D; ++j) x[j] = 0.f;
 #pragma unroll
   for (int i = 0; i < JOIN_FEW; ++i) {
-    if (i >= parts || ml[i].x == -CH_INF) continue;  // not there, or nothing seen
+    if (ml[i].x == -CH_INF) continue;  // not there, or nothing seen
     const float f = __builtin_amdgcn_exp2f(ml[i].x - mt);
     lt = fmaf(ml[i].y, f, lt);
 #pragma unroll
