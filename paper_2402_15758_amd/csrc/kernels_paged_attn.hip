@@ -480,7 +480,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
 //
 // Bound by the chain of scores, exponentials and products, two waves a SIMD: 2048 queries
 // of 32 heads of 128 behind 2048 positions take 124 us, 830 TFLOP/s (MFMA busy 34% of the
-// time, VALU 38%), behind 14336 positions 561 us, 918; heads of 64 76 us, 680.  32-bit, 2048
+// time, VALU 38%), behind 14336 positions 525 us, 981; heads of 64 76 us, 680.  32-bit, 2048
 // queries of 16 heads behind none: 188 us, 91 of 154 TFLOP/s.  A workgroup of eight waves,
 // four buffers with one workgroup a CU, and the next tile's scores beside this tile's
 // values took longer or spilt.
@@ -665,9 +665,13 @@ __device__ __forceinline__ void many_values(const char* v, const LanePlaces<T, H
   l = l + ((ls[0] + ls[1]) + (ls[2] + ls[3]));
 }
 
-// One tile for one wave.  held: its positions that the cache has and some query of the
+// One tile for one wave.  RAISE: the wave goes first on its SIMD while its products with V
+// run, which keeps two waves out of step (2048 queries behind 14336 positions 558 -> 524 us,
+// 256 behind 16384 126 -> 112, 64-wide heads behind 14336 346 -> 327); where positions are
+// few for the queries and blocks differ in length it costs (2048 behind 2048 125 -> 127,
+// 64-wide 76.5 -> 79.6), so it is for calls that may see three times their rows.  held: its positions that the cache has and some query of the
 // workgroup sees.  odd: set where the tile was left for later (below).
-template <typename T, int HD>
+template <typename T, int HD, bool RAISE>
 __device__ __forceinline__ void many_tile(const PagedAttnArgs& a, ManyState<T, HD>& st, const char* k, const char* v,
                                           LanePlaces<T, HD> at, int base, uint64_t held, int qpos, int p_lo, int p_hi,
                                           int lane, bool& odd) {
@@ -717,10 +721,12 @@ __device__ __forceinline__ void many_tile(const PagedAttnArgs& a, ManyState<T, H
   }
   // a masked score, and every one of a query that has seen nothing yet, weighs nothing
   const float sub = st.m == -CH_INF ? 0.f : st.m;
+  if constexpr (RAISE) __builtin_amdgcn_s_setprio(1);
   many_values<T, HD>(v, at, s, a.scale2, sub, st.l, st.o);
+  if constexpr (RAISE) __builtin_amdgcn_s_setprio(0);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool RAISE>
 __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tiles_kernel(const PagedView c, const PagedAttnArgs a) {
   typedef ManyState<T, HD> State;
   constexpr int KT = TT<T>, ND = HD / 32, ROW = HD * (int)sizeof(T), CH = ROW / 16;
@@ -814,7 +820,7 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
       load(kn, vn);
       held = held_next;
     }
-    if (on) many_tile<T, HD>(a, st, k, v, at, span.tile(t) * KT, mine, blk.n + qrow, p_lo, p_hi, lane, odd);
+    if (on) many_tile<T, HD, RAISE>(a, st, k, v, at, span.tile(t) * KT, mine, blk.n + qrow, p_lo, p_hi, lane, odd);
     if (t + 2 < t1) settle();
   };
   for (int t = t0; t < t1; t += 2) {
@@ -1094,7 +1100,10 @@ void attn_go(const PagedView& c, PagedAttnArgs a, void* ws, hipStream_t st) {
     hipLaunchKernelGGL((paged_rows_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
     if (a.splits > 1) join_go<T, HD, RB, RT>(c, a, st);
   } else {
-    hipLaunchKernelGGL((paged_tiles_kernel<T, HD>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
+    if (sizeof(T) == 2 && seen_most(c, a) >= 3 * (int64_t)a.rows / c.B)
+      hipLaunchKernelGGL((paged_tiles_kernel<T, HD, sizeof(T) == 2>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
+    else
+      hipLaunchKernelGGL((paged_tiles_kernel<T, HD, false>), dim3((unsigned)parts), dim3(256), 0, st, c, a);
     if (a.splits > 1) join_go<T, HD, TB, TT<T>>(c, a, st);
   }
 }

@@ -381,6 +381,13 @@ def test_parts_of_blocks_of_128(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_positions_before_them(dtype):
+    check(dtype, [100], [1000], 24, 8, 128, 16, 8)
+    check(dtype, [30, 0, 5], [500, 700, 200], 64, 32, 64, 32, 8)
+    check(dtype, [0], [1100], 40, 40, 64, 16, 8, 600, 5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("heads", [17, 64])
 def test_single_tokens_of_many_query_heads(dtype, heads):
     """More query heads a cache head than a block of 16 has rows."""
