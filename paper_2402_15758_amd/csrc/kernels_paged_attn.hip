@@ -242,9 +242,10 @@ __device__ __forceinline__ void store_out(T* p, const float* x, bool vec) {
 // dimension (4 g + r) HD / 16 + j.
 //
 // Bound by the cache's bytes where few queries read much of it: eight single tokens behind
-// 1024 to 4096 positions of 32 heads of 128 (336 MB) 69 us, 4.9 TB/s; one behind 32768 of 8
-// heads (134 MB) 28 us, 4.9 TB/s.  A wave keeps a tile's K and V in registers, so waves wait
-// for memory by themselves and not for each other.
+// 1024 to 4096 positions of 32 heads of 128 (336 MB) 65 us, 5.2 TB/s (69 with each page asked
+// for when its tile's turn comes); one behind 32768 of 8 heads (134 MB) 27 us, 5.0 TB/s.
+// A wave keeps a tile's K and V in registers, so waves wait for memory by themselves and
+// not for each other.
 template <typename T, int HD>
 struct RowTile {
   static constexpr int VEC = ET<T>::VEC, KB = 4 * VEC, KS = HD / KB;
@@ -314,6 +315,18 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
   const int* ptab = c.page_table + (int64_t)blk.b * c.max_pages;
   const T* pool = (const T*)c.pool;
 
+  // The page of a position that some query sees is asked for a tile ahead; a row that none
+  // sees is read as row 0 of the pool and counts for nothing.
+  int page = 0, slot_in = 0;
+  bool seen = false;
+  auto ask = [&](int t) {
+    const int pos = span.tile(t) * RT + (lane & 31);
+    seen = some_see(a, pos, span.p_lo, span.p_hi) && pos < c.cap;
+    const int p = seen ? pos : 0, pi = c.ps.quot(p);
+    slot_in = p - pi * c.ps.d;
+    page = ptab[pi];
+  };
+  if (t0 + wave < t1) ask(t0 + wave);
   const int vq = blk.v0 + min(c16, blk.count - 1);
   const int qrow = vq / a.group;
   const int qpos = blk.n + qrow;
@@ -335,11 +348,10 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
   bool odd = false;
   for (int t = t0 + wave; t < t1; t += 4) {
     const int base = span.tile(t) * RT;
-    const int pos = base + (lane & 31);
-    // a row that no query sees is read as row 0 of the pool and counts for nothing
-    const uint32_t row = some_see(a, pos, span.p_lo, span.p_hi) ? paged_row(c, ptab, pos) : PAGED_NONE;
-    const uint32_t held = (uint32_t)__ballot(row != PAGED_NONE);
-    const int safe = row == PAGED_NONE ? 0 : (int)row;
+    const bool there = seen && page >= 0 && page < c.n_pages;
+    const uint32_t held = (uint32_t)__ballot(there);
+    const int safe = there ? (int)((uint32_t)page * c.page_rows + (uint32_t)slot_in) : 0;
+    if (t + 4 < t1) ask(t + 4);
     Tile x;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
