@@ -92,16 +92,28 @@ template <typename T>
 __device__ __forceinline__ float logit(const void* row, int64_t i) {
   return ET<T>::to_f(((const T*)row)[i]);
 }
-// Sixteen of a part's entries a lane, -inf past n; VEC: 16 bytes at once.  Lane l holds
-// entries l * E + 64 E i + e of run i, E = 16 / sizeof(T) (1 without VEC).
-template <typename T, bool VEC>
+// 16 bytes at any element: rows of an odd vocabulary start at every other one (64 chains
+// over 128255 bf16 tokens 71 us, 185 an entry at a time).
+typedef int at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef int at4 __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ int4 ld16_any(const bf16_t* p) {
+  const at2 x = *reinterpret_cast<const at2*>(p);
+  return int4{x.x, x.y, x.z, x.w};
+}
+__device__ __forceinline__ int4 ld16_any(const float* p) {
+  const at4 x = *reinterpret_cast<const at4*>(p);
+  return int4{x.x, x.y, x.z, x.w};
+}
+// Sixteen of a part's entries a lane, -inf past n.  Lane l holds entries l E + 64 E i + e of
+// run i, E = 16 / sizeof(T).
+template <typename T>
 __device__ __forceinline__ void load_part(const T* z, int n, int lane, float (&x)[16]) {
-  constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
+  constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
   for (int i = 0; i < 16 / E; ++i) {
     const int v = lane * E + 64 * E * i;
-    if (VEC && v + E <= n) {
-      const int4 w = ld16(z + v);
+    if (v + E <= n) {
+      const int4 w = ld16_any(z + v);
       if constexpr (sizeof(T) == 4) {
         x[4 * i] = __int_as_float(w.x), x[4 * i + 1] = __int_as_float(w.y);
         x[4 * i + 2] = __int_as_float(w.z), x[4 * i + 3] = __int_as_float(w.w);
@@ -125,7 +137,7 @@ __device__ __forceinline__ void load_part(const T* z, int n, int lane, float (&x
 // part's sum NaN: such a row has no distribution.  Bound by 25 instructions an entry, most
 // of them in 64 bits: 704 bf16 rows of 128256 (181 MB) 80 us, VALU busy 74%; 64 32-bit rows
 // of 32000 (8 MB) 5 us.  Four parts a wave: the same times.  Many bf16 rows: below.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
   __shared__ double table[32];
   const int row = blockIdx.x, lane = threadIdx.x & 63;
@@ -138,7 +150,7 @@ __global__ __launch_bounds__(256) void accept_parts_kernel(const AcceptArgs a) {
   const int root = a.tokens[(int64_t)b * a.N];
   const int v0 = part * ACCEPT_PART;
   float x[16];
-  if (part < a.parts) load_part<T, VEC>(z + v0, min(ACCEPT_PART, a.V - v0), lane, x);
+  if (part < a.parts) load_part<T>(z + v0, min(ACCEPT_PART, a.V - v0), lane, x);
   fill_table(table);
   __syncthreads();
   if (root < 0 || part >= a.parts) return;  // an empty place
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(1024, 8) void accept_parts_tabled_kernel(const Acce
       const int v = lane * 8 + 512 * i;
       const bf16_t* p = z + part * ACCEPT_PART + v;
       if (v + 8 <= n) {
-        x[i] = ld16(p);
+        x[i] = ld16_any(p);
       } else {
         uint32_t u[4];
 #pragma unroll
@@ -398,7 +410,7 @@ struct Weights {
 // 22.  Whole calls with 4, 8 or 16 parts a workgroup: 19.5, 19.8 and 22.1 us for the 8
 // sequences, 71, 69 and 67 for the 64; with a launch for the walks 21.3 and 70.
 constexpr int RESID = 8;  // parts of a workgroup
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(64 * RESID) void accept_resid_kernel(const AcceptArgs a) {
   __shared__ WalkSpace sh;
   const int b = blockIdx.y, lane = threadIdx.x & 63;
@@ -414,8 +426,8 @@ __global__ __launch_bounds__(64 * RESID) void accept_resid_kernel(const AcceptAr
                      1.0 / w.p.s, 1.0 / w.q.s, sh.table};
   float x[16], xq[16];
   const int n = min(ACCEPT_PART, a.V - v0);
-  load_part<T, VEC>(f.z + v0, n, lane, x);
-  load_part<T, VEC>(f.zq + v0, n, lane, xq);
+  load_part<T>(f.z + v0, n, lane, x);
+  load_part<T>(f.zq + v0, n, lane, xq);
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s = s + f.of(x[i], xq[i]);
@@ -427,7 +439,7 @@ __global__ __launch_bounds__(64 * RESID) void accept_resid_kernel(const AcceptAr
 // running sum passes u[0] of the whole, by parts and then within one.  Bound by its chain
 // of round trips and barriers: a tree of 64 nodes 10 us with its walk, 64 chains 6.5
 // without.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row0 = (int64_t)b * a.N;
@@ -489,9 +501,9 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   for (int i = wave - 1; i < ng; i += 15) {
     if (wave == 0) break;
     const int v0 = gone_of(i) / ACCEPT_PART * ACCEPT_PART, n = min(ACCEPT_PART, a.V - v0);
-    constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
+    constexpr int E = 16 / (int)sizeof(T);
     float x[16];
-    load_part<T, VEC>(f.z + v0, n, lane, x);
+    load_part<T>(f.z + v0, n, lane, x);
     uint32_t out = 0;  // this lane's entries that are gone
     for (int j = 0; j < ng; ++j) {
       const int r = gone_of(j) - v0;
@@ -608,27 +620,18 @@ __global__ void accept_first_kernel(const PrefillEnds e, unsigned long long seed
 // 24.5 and 25.1, 12096 32 and 35, 96768 72 and 106 (whole calls).  One workgroup a CU: 79.
 constexpr int64_t TABLED_PARTS = 10000;
 constexpr int TABLED_WGS = 512;  // two a CU
-template <typename T, bool VEC>
+template <typename T>
 void accept_go(const AcceptArgs& a, hipStream_t st) {
   const int rows = a.B * a.N, kinds = a.draft != nullptr ? 2 : 1;
   const int64_t items = (int64_t)rows * kinds * a.parts;
-  if (sizeof(T) == 2 && VEC && items >= TABLED_PARTS && a.scale <= accept_scale(0.25f))
+  if (sizeof(T) == 2 && items >= TABLED_PARTS && a.scale <= accept_scale(0.25f))
     hipLaunchKernelGGL(accept_parts_tabled_kernel, dim3(TABLED_WGS), dim3(1024), 0, st, a, items);
   else
-    hipLaunchKernelGGL((accept_parts_kernel<T, VEC>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((accept_parts_kernel<T>), dim3(rows, (a.parts + 3) / 4, kinds), dim3(256), 0, st, a);
   if (a.draft != nullptr && a.N > 1)
-    hipLaunchKernelGGL((accept_resid_kernel<T, VEC>), dim3((a.parts + RESID - 1) / RESID, a.B), dim3(64 * RESID), 0, st, a);
-  hipLaunchKernelGGL((accept_pick_kernel<T, VEC>), dim3(a.B), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((accept_resid_kernel<T>), dim3((a.parts + RESID - 1) / RESID, a.B), dim3(64 * RESID), 0, st, a);
+  hipLaunchKernelGGL((accept_pick_kernel<T>), dim3(a.B), dim3(1024), 0, st, a);
 }
-template <typename T>
-void accept_t(const AcceptArgs& a, hipStream_t st) {
-  auto whole = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
-  if (whole(a.logits, a.ld) && whole(a.draft, a.draft != nullptr ? a.ldd : 0))
-    accept_go<T, true>(a, st);
-  else
-    accept_go<T, false>(a, st);
-}
-
 int64_t up(int64_t b) { return (b + 255) / 256 * 256; }
 
 }  // namespace
@@ -653,9 +656,9 @@ void accept_carve(AcceptArgs& a, void* ws) {
 
 void launch_accept(int dtype, const AcceptArgs& a, hipStream_t st) {
   if (dtype == DT_BF16)
-    accept_t<bf16_t>(a, st);
+    accept_go<bf16_t>(a, st);
   else
-    accept_t<float>(a, st);
+    accept_go<float>(a, st);
 }
 
 void launch_accept_uniforms(const int* n_b, int B, int N, unsigned long long seed, double* u, hipStream_t st) {

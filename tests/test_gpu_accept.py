@@ -236,8 +236,8 @@ def test_accepted_at_the_targets_rate():
 @pytest.mark.parametrize("temperature", [0.2499, 0.25, 1.0, 7.0])
 @pytest.mark.parametrize("vocab,pad", [(2048, 0), (2050, 0), (2050, 6)])
 def test_many_bf16_rows(drawn, temperature, vocab, pad):
-    """Enough parts for the sums by a table (from 1/4 on, where rows lie at multiples of 16
-    bytes): the walks of the rule, and those of few rows at once."""
+    """Enough parts for the sums by a table (from 1/4 on): the walks of the rule, and those
+    of few rows at once."""
     parents = tree(9, 1) if drawn else tree(64, 4)
     batch = 420 if drawn else 85
     logits, draft, tokens, u = inputs(batch, parents, vocab, drawn, "bf16", 31, 0.8, temperature)
