@@ -29,11 +29,13 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const RopeArgs r, float
 }
 
 // ---- rows --------------------------------------------------------------------------
-// Four values at any element, or 16 (8) bytes at once where they are aligned.
+// Four values at any element: 16 (8) bytes at once, or VEC false, one by one.
+typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u2_any __attribute__((ext_vector_type(2), aligned(2)));
 template <bool VEC>
 __device__ __forceinline__ void load4(const float* p, float* x) {
   if constexpr (VEC) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
+    const f4_any v = *reinterpret_cast<const f4_any*>(p);
     x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
   } else {
 #pragma unroll
@@ -43,7 +45,7 @@ __device__ __forceinline__ void load4(const float* p, float* x) {
 template <bool VEC>
 __device__ __forceinline__ void load4(const bf16_t* p, float* x) {
   if constexpr (VEC) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    const u2_any v = *reinterpret_cast<const u2_any*>(p);
     x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
     x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
   } else {
@@ -54,7 +56,7 @@ __device__ __forceinline__ void load4(const bf16_t* p, float* x) {
 template <bool VEC>
 __device__ __forceinline__ void store4(float* p, const float* x) {
   if constexpr (VEC) {
-    *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f4_any*>(p) = f4_any{x[0], x[1], x[2], x[3]};
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = x[i];
@@ -65,7 +67,7 @@ __device__ __forceinline__ void store4(bf16_t* p, const float* x) {
   if constexpr (VEC) {
     typedef float f2 __attribute__((ext_vector_type(2)));
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    *reinterpret_cast<uint2*>(p) = uint2{__builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[0], x[1]}, b2)),
+    *reinterpret_cast<u2_any*>(p) = u2_any{__builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[0], x[1]}, b2)),
                                          __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[2], x[3]}, b2))};
   } else {
 #pragma unroll
@@ -76,8 +78,8 @@ __device__ __forceinline__ void store4(bf16_t* p, const float* x) {
 // HD / 8 lanes a head, eight values a lane: four pairs of the rotation, so nothing
 // but the norm's sum crosses lanes.  Pairs (i, i + P): values 4 j .. and P + 4 j ..
 // of lane j, the ones past the rotated part in order after them.  Neighbouring
-// pairs: eight values in a row.  VEC: both are runs of four values at aligned
-// addresses (P a multiple of 4); else a value at a time.
+// pairs: eight values in a row.  VEC: both are runs of four values (P a multiple of
+// 4); else a value at a time.
 // Bound by the bytes of many rows and by the launch of few: 2044 32-bit rows of 48 heads
 // into bf16 (76 MB) 17.5 us, 4.4 TB/s; one row 2.8 us, eight normed rows 3.3.
 // Elements of value v (0 .. 7) of lane j: pair v / 2 in either layout.
@@ -233,11 +235,7 @@ void launch_rope_table(const RopeArgs& r, void* table, int positions, hipStream_
 }
 
 void launch_paged_append(int dtype, int held, const PagedView& c, const AppendArgs& a, hipStream_t st) {
-  const int ei = dtype == DT_BF16 ? 2 : 4, ec = held == DT_BF16 ? 2 : 4;
-  auto runs = [](const void* p, int64_t ld, int es) { return ((uintptr_t)p % (4 * es)) == 0 && ld % 4 == 0; };
-  auto gain = [](const float* p) { return ((uintptr_t)p & 15) == 0; };
-  const bool vec = (a.cross == 0 || a.pairs % 4 == 0) && runs(a.q, a.ld, ei) && runs(a.k, a.ld, ei) &&
-                   runs(a.v, a.ld, ei) && (a.Hq == 0 || runs(a.q_out, a.ldo, ec)) && gain(a.q_gain) && gain(a.k_gain);
+  const bool vec = a.cross == 0 || a.pairs % 4 == 0;
   if (dtype == DT_BF16)
     held == DT_BF16 ? append_t<bf16_t, bf16_t>(c, a, vec, st) : append_t<bf16_t, float>(c, a, vec, st);
   else
