@@ -209,23 +209,19 @@ __device__ __forceinline__ void tile_alone(const PagedView& c, const PagedAttnAr
   }
 }
 
-// DV values of one row into the caller's output.
+// DV values of one row into the caller's output, at any element.
 template <typename T, int DV>
-__device__ __forceinline__ void store_out(T* p, const float* x, bool vec) {
-  if (!vec) {
-#pragma unroll
-    for (int i = 0; i < DV; ++i) p[i] = ET<T>::from_f(x[i]);
-  } else if constexpr (sizeof(T) == 2) {
-    uint32_t w[DV / 2];
+__device__ __forceinline__ void store_out(T* p, const float* x) {
+  if constexpr (sizeof(T) == 2) {
+    typedef uint32_t words __attribute__((ext_vector_type(DV / 2), aligned(2)));
+    words w;
 #pragma unroll
     for (int i = 0; i < DV / 2; ++i) w[i] = cvt_pk_bf16(x[2 * i], x[2 * i + 1]);
-    if constexpr (DV == 8)
-      st16(p, int4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]});
-    else
-      *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
+    *reinterpret_cast<words*>(p) = w;
   } else {
+    typedef float four __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-    for (int i = 0; i < DV; i += 4) *reinterpret_cast<float4*>(p + i) = float4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    for (int i = 0; i < DV; i += 4) *reinterpret_cast<four*>(p + i) = four{x[i], x[i + 1], x[i + 2], x[i + 3]};
   }
 }
 
@@ -465,7 +461,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
     const int r = (blk.v0 + q) / a.group, h = blk.v0 + q - r * a.group;
 #pragma unroll
     for (int j = 0; j < DV; ++j) x[j] = mt == -CH_INF ? 0.f : x[j] / lt;
-    store_out<T, DV>((T*)a.out + (int64_t)(blk.row0 + r) * a.ldo + (kvh * a.group + h) * HD + d0, x, a.vec_out != 0);
+    store_out<T, DV>((T*)a.out + (int64_t)(blk.row0 + r) * a.ldo + (kvh * a.group + h) * HD + d0, x);
     return;
   }
   const int64_t at = (((int64_t)slot * c.H + kvh) * a.splits + split) * RB + q;
@@ -884,7 +880,7 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
           float x[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[j] = st.m == -CH_INF ? 0.f : st.o[db][4 * i + j] * inv;
-          store_out<T, 4>(dst + 32 * db + 8 * i + 4 * h, x, a.vec_out != 0);
+          store_out<T, 4>(dst + 32 * db + 8 * i + 4 * h, x);
         }
     } else {
 #pragma unroll
@@ -894,7 +890,7 @@ __global__ __launch_bounds__(256, sizeof(T) * HD == 512 ? 1 : 2) void paged_tile
         for (int d = 0; d < ND; ++d) x[d] = st.m == -CH_INF ? 0.f : st.o[d][r] / lt;
         const int dim = (8 * (r >> 2) + 4 * h + (r & 3)) * ND;
         if constexpr (ND == 4) {
-          store_out<T, 4>(dst + dim, x, a.vec_out != 0);
+          store_out<T, 4>(dst + dim, x);
         } else {
           dst[dim] = x[0];
           dst[dim + 1] = x[1];
@@ -968,8 +964,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedView c, cons
   const int r = (blk.v0 + q) / a.group, h = blk.v0 + q - r * a.group;
 #pragma unroll
   for (int j = 0; j < D; ++j) x[j] = mt == -CH_INF ? 0.f : x[j] / lt;
-  store_out<T, D>((T*)a.out + (int64_t)(blk.row0 + r) * a.ldo + (kvh * a.group + h) * HD + threadIdx.x % 16 * D, x,
-                  a.vec_out != 0);
+  store_out<T, D>((T*)a.out + (int64_t)(blk.row0 + r) * a.ldo + (kvh * a.group + h) * HD + threadIdx.x % 16 * D, x);
 }
 
 template <typename T, int HD, int BQ, int TILE>

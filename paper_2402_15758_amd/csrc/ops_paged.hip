@@ -239,7 +239,6 @@ chimera_status chimera_paged_attn(const chimera_paged* cache, const void* q, int
     // score is no weight's last bit
     a.scale2 = std::max(std::fabs(scale) * 1.44269504088896340736f, 0x1p-140f);
     a.flip = scale < 0.f;
-    a.vec_out = ((uintptr_t)out & 15) == 0 && ldo * es % 16 == 0;
     launch_paged_attn(cache->dtype, view(cache), a, ws, st);
     HIPCK(hipGetLastError());
   });

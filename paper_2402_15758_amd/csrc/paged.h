@@ -77,7 +77,6 @@ struct PagedAttnArgs {
   // a launch's own: parts of a block's positions at most and tiles of one at least, blocks
   // of queries of one cache head, those of each sequence (0: as its rows take)
   int splits, least, slots, per;
-  int vec_out;              // out rows at multiples of 16 bytes
   float* part_o;            // [slots][H][splits][block][hd]
   float* part_ml;           // [slots][H][splits][block][2]
 };
