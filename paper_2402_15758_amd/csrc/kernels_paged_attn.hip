@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedView c, cons
 // Bound by the chain of scores, exponentials and products, two waves a SIMD: 2048 queries
 // of 32 heads of 128 behind 2048 positions take 124 us, 830 TFLOP/s (MFMA busy 34% of the
 // time, VALU 38%), behind 14336 positions 525 us, 981; heads of 64 76 us, 680.  32-bit, 2048
-// queries of 16 heads behind none: 188 us, 91 of 154 TFLOP/s.  A workgroup of eight waves,
+// queries of 16 heads behind none: 182 us, 94 of 154 TFLOP/s.  A workgroup of eight waves,
 // four buffers with one workgroup a CU, and the next tile's scores beside this tile's
 // values took longer or spilt.
 typedef float f32x16 __attribute__((ext_vector_type(16)));

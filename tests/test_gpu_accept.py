@@ -234,7 +234,7 @@ def test_accepted_at_the_targets_rate():
 
 @pytest.mark.parametrize("drawn", [False, True])
 @pytest.mark.parametrize("temperature", [0.2499, 0.25, 1.0, 7.0])
-@pytest.mark.parametrize("vocab,pad", [(2048, 0), (2050, 0), (2050, 6)])
+@pytest.mark.parametrize("vocab,pad", [(2048, 0), (2049, 0), (2050, 6)])
 def test_many_bf16_rows(drawn, temperature, vocab, pad):
     """Enough parts for the sums by a table (from 1/4 on): the walks of the rule, and those
     of few rows at once."""
