@@ -549,8 +549,9 @@ chimera_status chimera_paged_attn(const chimera_paged* cache, const void* q, int
  * random numbers: u[0] draws the next token, u[i] tests node i.
  *  - draft NULL: the children of a node were chosen (the draft's best).  They are
  *    tested in the order of their ids; child c is accepted where u[c] (1 - the mass of
- *    the siblings rejected before it) < p(its token).  Where all are rejected the next
- *    token comes from p without them, normalised.
+ *    the siblings rejected before it) < p(its token), of which a token rejected among
+ *    them has none left.  Where all are rejected the next token comes from p without
+ *    them, normalised.  Rejections at one node count for nothing at another.
  *  - draft given, a chain: node i + 1's token was drawn from q = softmax(draft row i /
  *    temperature).  It is accepted where u[i + 1] q(token) < p(token), else the next
  *    token comes from max(p - q, 0), normalised.

@@ -373,7 +373,8 @@ __device__ void accept_walk(const AcceptArgs& a, int b, WalkSpace& sh) {
           }
           w.rejected |= 1ull << c;
           left = left - pc;
-          if (tok == __builtin_amdgcn_readlane(tok, c)) p = 0.0;  // a sibling of the same token
+          // a sibling of the same token; below other nodes it is a token like any other
+          if (parent == w.node && tok == __builtin_amdgcn_readlane(tok, c)) p = 0.0;
         }
         if (next < 0) break;
         w.node = next;
