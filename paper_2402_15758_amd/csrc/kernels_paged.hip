@@ -132,29 +132,26 @@ __device__ __forceinline__ float head_sum(float v) {  // over the HD / 8 lanes o
   return v + dpp_mov<DPP_MIRROR8>(v);
 }
 
-// y = x (mean(x^2) + eps)^-1/2 gain.  Squares that pass 2^128 are summed again at
-// 2^-128 of their size, where eps counts for nothing; an infinity makes its own
-// value NaN and the others 0, as the formula does.
+// y = x (mean(x^2) + eps)^-1/2 gain.  Where mean + eps passes 2^128 it is formed again at
+// 2^-136 of its size: 128 squares of the largest float stay below 2^127 then.  An infinity
+// makes its own value NaN and the others 0, as the formula does.
 template <int HD>
 __device__ __forceinline__ void head_norm(float (&x)[8], const float (&gain)[8], float eps) {
   float ss = 0.f;
 #pragma unroll
   for (int v = 0; v < 8; ++v) ss = fmaf(x[v], x[v], ss);
-  ss = head_sum<HD>(ss);
-  if (__ballot(ss == CH_INF) != 0) {
-    if (ss == CH_INF) {
-#pragma unroll
-      for (int v = 0; v < 8; ++v) x[v] = x[v] * 0x1p-64f;
-      eps = 0.f;
-    }
+  float t = head_sum<HD>(ss) * (1.0f / HD) + eps, back = 1.f;
+  if (__ballot(t == CH_INF) != 0) {
+    const float k = t == CH_INF ? 0x1p-68f : 1.f;
     float s2 = 0.f;
 #pragma unroll
-    for (int v = 0; v < 8; ++v) s2 = fmaf(x[v], x[v], s2);
-    ss = head_sum<HD>(s2);
+    for (int v = 0; v < 8; ++v) s2 = fmaf(x[v] * k, x[v] * k, s2);
+    t = head_sum<HD>(s2) * (1.0f / HD) + eps * k * k;
+    back = k;
   }
-  const float r = 1.0f / sqrtf(ss * (1.0f / HD) + eps);
+  const float r = 1.0f / sqrtf(t);
 #pragma unroll
-  for (int v = 0; v < 8; ++v) x[v] = x[v] * r * gain[v];
+  for (int v = 0; v < 8; ++v) x[v] = x[v] * r * back * gain[v];
 }
 
 // Grid (blocks of a row's heads, rows).  A lane does the same eight places of
