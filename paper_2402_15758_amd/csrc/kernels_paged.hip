@@ -132,22 +132,28 @@ __device__ __forceinline__ float head_sum(float v) {  // over the HD / 8 lanes o
   return v + dpp_mov<DPP_MIRROR8>(v);
 }
 
-// y = x (mean(x^2) + eps)^-1/2 gain.  Where mean + eps passes 2^128 it is formed again at
-// 2^-136 of its size: 128 squares of the largest float stay below 2^127 then.  An infinity
-// makes its own value NaN and the others 0, as the formula does.
+// y = x (mean(x^2) + eps)^-1/2 gain.  Where mean + eps is not between 2^-100 and 2^128 it
+// is formed again of values scaled by k, a power of two: by 2^60, which leaves no square
+// that counts below the normal numbers, or by 2^-68, so that 128 squares of the largest float
+// stay below 2^127.  An infinity makes its own value NaN and the others 0, as the formula
+// does.
 template <int HD>
 __device__ __forceinline__ void head_norm(float (&x)[8], const float (&gain)[8], float eps) {
   float ss = 0.f;
 #pragma unroll
   for (int v = 0; v < 8; ++v) ss = fmaf(x[v], x[v], ss);
   float t = head_sum<HD>(ss) * (1.0f / HD) + eps, back = 1.f;
-  if (__ballot(t == CH_INF) != 0) {
-    const float k = t == CH_INF ? 0x1p-68f : 1.f;
+  const bool low = t < 0x1p-100f, high = t == CH_INF;
+  if (__ballot(low || high) != 0) {
+    const float k = low ? 0x1p60f : high ? 0x1p-68f : 1.f;
     float s2 = 0.f;
 #pragma unroll
     for (int v = 0; v < 8; ++v) s2 = fmaf(x[v] * k, x[v] * k, s2);
     t = head_sum<HD>(s2) * (1.0f / HD) + eps * k * k;
-    back = k;
+    // small values are scaled before their product, which might lose bits, large ones after
+#pragma unroll
+    for (int v = 0; v < 8; ++v) x[v] = low ? x[v] * k : x[v];
+    back = low ? 1.f : k;
   }
   const float r = 1.0f / sqrtf(t);
 #pragma unroll

@@ -57,3 +57,19 @@ def test_largest_rows(dtype, held, hd):
     x = x.to(R.TYPES[dtype])
     for eps in (1e-5, 1e30, 3e38):
         norms(x, eps, held)
+
+
+@pytest.mark.parametrize("dtype,held", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_smallest_rows(dtype, held, hd):
+    """Squares and an eps below the least normal float, down to subnormal values; zeros."""
+    x = rows_of(hd, hd + 1)
+    x[0] *= 1e-20
+    x[1] *= 1e-22
+    x[2] *= 1e-30
+    x[3] *= torch.tensor([2.0 ** -46, 2.0 ** -50, 2.0 ** -54])[:, None]  # on either side of where sums are scaled
+    x[4] *= 1e-40
+    x[5, 0] = 0.0
+    x = x.to(R.TYPES[dtype])
+    for eps in (1e-5, 1e-31, 1e-38, 1e-41, 2.0 ** -149):
+        norms(x, eps, held)
