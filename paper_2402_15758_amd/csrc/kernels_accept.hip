@@ -16,7 +16,7 @@ namespace {
 // 2^(y / 32): y = n + f, |f| <= 1/2, 2^(n / 32) = 2^(n >> 5) times a table's
 // entry, and Taylor's series of e^(f ln 2 / 32) up to the fifth power (the next is below
 // 2^-48).  A weight is exp((z - m) / T) = 2^(y / 32) with y = (z - m) 32 / (T ln 2): the
-// sum of a row's errors stays below 2^-47 of its weights.  0 from 2^-1100 on.
+// sum of a row's errors stays below 2^-47 of its weights.  0 below 2^-1075.
 __device__ const double POW32[32] = {
     0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
     0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
@@ -31,8 +31,10 @@ constexpr double LN2_32[5] = {0x1.62e42fefa39efp-6, 0x1.ebfbdff82c58fp-13, 0x1.c
 __device__ __forceinline__ void fill_table(double* table) {  // LDS, [32]
   if (threadIdx.x < 32) table[threadIdx.x] = POW32[threadIdx.x];
 }
-__device__ __forceinline__ double pow32(double y, const double* table) {
-  y = fmax(y, -35200.0);
+// by: a factor within 2^750 of 1, as a table's sums are, which joins before the power of two
+// can pass the range.
+__device__ __forceinline__ double pow32(double y, const double* table, double by = 1.0) {
+  y = fmax(y, -70400.0);
   const double n = rint(y), f = y - n;
   const int i = (int)n;
   double p = LN2_32[4];
@@ -41,7 +43,7 @@ __device__ __forceinline__ double pow32(double y, const double* table) {
   p = fma(p, f, LN2_32[1]);
   p = fma(p, f, LN2_32[0]);
   const double t = table[i & 31];
-  return ldexp(fma(p * f, t, t), i >> 5);
+  return ldexp(fma(p * f, t, t) * by, i >> 5);
 }
 // (z - m) 32 / (T ln 2); scale: 32 / (T ln 2), at most 2^156
 __device__ __forceinline__ double exponent(float z, double m, double scale) { return ((double)z - m) * scale; }
@@ -532,7 +534,9 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
         if (f.zq != nullptr) return kept ? ps0 : a.resid[(int64_t)b * a.parts + i];
         const float pm = kept ? pm0 : a.part_m[parts0 + i];
         const double ps = kept ? ps0 : a.part_s[parts0 + i];
-        double of = pm == -CH_INF ? 0.0 : ps * pow32(exponent(pm, w.p.m, a.scale), sh.table) * f.one;
+        double of = pm == -CH_INF ? 0.0 : pow32(exponent(pm, w.p.m, a.scale), sh.table, ps);
+        // a sum of 1024 that no entry has a weight behind
+        of = of < 0x1p-1064 ? 0.0 : of;
         for (int j = 0; j < ng; ++j) of = gone_of(j) / ACCEPT_PART == i ? lane_f64(redo_l, j) : of;
         return of;
       };
