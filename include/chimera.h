@@ -557,9 +557,10 @@ chimera_status chimera_paged_attn(const chimera_paged* cache, const void* q, int
  *    token comes from max(p - q, 0), normalised.
  * After a node without children it comes from p.  It is the least v for which the
  * weights of 0 .. v add up to more than u[0] of their sum.  All of it is computed in
- * 64 bits.  Results: n_new [batch] tokens, new_tokens [batch][K + 1] (K the tree's
- * depth): the accepted ones in order of depth, then the next; path_nodes [batch][K +
- * 1] (nullable): the accepted nodes from the root; entries past n_new are -1.
+ * 64 bits; where rounding has rejected all there is, so that no weight is left, the
+ * next token comes from p.  Results: n_new [batch] tokens, new_tokens [batch][K + 1] (K
+ * the tree's depth): the accepted ones in order of depth, then the next; path_nodes
+ * [batch][K + 1] (nullable): the accepted nodes from the root; entries past n_new are -1.
  * A node whose token is not in 0 .. vocab - 1 is not there (padding of ragged trees),
  * and a sequence whose node 0 is negative is an empty place: n_new 0.  A row on the
  * path with a NaN, a +inf or nothing but -inf has no distribution: the walk ends
