@@ -525,7 +525,7 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
   const double redo_l = lane < ng ? redo[lane] : 0.0;
   // The part where the running sum passes, by one wave, 64 parts at a time.  Rounding
   // may leave no weight at all behind rejections (the mass that was left was its own
-  // error): then the row's own probabilities decide.
+  // error): then the row's own probabilities decide, of which one is not 0.
   for (int attempt = 0; attempt < 2; ++attempt) {
     if (wave == 0) {
       auto part_weight = [&](int i) {
@@ -570,10 +570,6 @@ __global__ __launch_bounds__(1024) void accept_pick_kernel(const AcceptArgs a) {
     ng = 0;
     f.zq = nullptr;
     f.one = 1.0;
-  }
-  if (part_sh < 0) {  // u was no number
-    if (tid == 0) a.new_tokens[(int64_t)b * K1 + w.depth] = a.none;
-    return;
   }
   // within the part, an entry a thread
   static_assert(ACCEPT_PART == 1024, "an entry a thread");

@@ -29,50 +29,26 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const RopeArgs r, float
 }
 
 // ---- rows --------------------------------------------------------------------------
-// Four values at any element: 16 (8) bytes at once, or VEC false, one by one.
+// Four values at any element: 16 (8) bytes at once.
 typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u2_any __attribute__((ext_vector_type(2), aligned(2)));
-template <bool VEC>
 __device__ __forceinline__ void load4(const float* p, float* x) {
-  if constexpr (VEC) {
-    const f4_any v = *reinterpret_cast<const f4_any*>(p);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = p[i];
-  }
+  const f4_any v = *reinterpret_cast<const f4_any*>(p);
+  x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
 }
-template <bool VEC>
 __device__ __forceinline__ void load4(const bf16_t* p, float* x) {
-  if constexpr (VEC) {
-    const u2_any v = *reinterpret_cast<const u2_any*>(p);
-    x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
-    x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = bf2f(p[i]);
-  }
+  const u2_any v = *reinterpret_cast<const u2_any*>(p);
+  x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
+  x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
 }
-template <bool VEC>
 __device__ __forceinline__ void store4(float* p, const float* x) {
-  if constexpr (VEC) {
-    *reinterpret_cast<f4_any*>(p) = f4_any{x[0], x[1], x[2], x[3]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = x[i];
-  }
+  *reinterpret_cast<f4_any*>(p) = f4_any{x[0], x[1], x[2], x[3]};
 }
-template <bool VEC>
 __device__ __forceinline__ void store4(bf16_t* p, const float* x) {
-  if constexpr (VEC) {
-    typedef float f2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    *reinterpret_cast<u2_any*>(p) = u2_any{__builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[0], x[1]}, b2)),
-                                         __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[2], x[3]}, b2))};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = f2bf(x[i]);
-  }
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  *reinterpret_cast<u2_any*>(p) = u2_any{__builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[0], x[1]}, b2)),
+                                       __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[2], x[3]}, b2))};
 }
 
 // HD / 8 lanes a head, eight values a lane: four pairs of the rotation, so nothing
@@ -94,8 +70,8 @@ __device__ __forceinline__ void load_pairs(const T* p, int j, int P, bool cross,
   if constexpr (VEC) {
     const bool turned = cross && 4 * j < P;
     float a[8];
-    load4<true>(p + (turned ? 4 * j : 8 * j), a);
-    load4<true>(p + (turned ? P + 4 * j : 8 * j + 4), a + 4);
+    load4(p + (turned ? 4 * j : 8 * j), a);
+    load4(p + (turned ? P + 4 * j : 8 * j + 4), a + 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       x[2 * i] = turned ? a[i] : a[2 * i];
@@ -116,8 +92,8 @@ __device__ __forceinline__ void store_pairs(T* p, int j, int P, bool cross, cons
       a[i] = turned ? x[2 * i] : x[i];
       a[4 + i] = turned ? x[2 * i + 1] : x[4 + i];
     }
-    store4<true>(p + (turned ? 4 * j : 8 * j), a);
-    store4<true>(p + (turned ? P + 4 * j : 8 * j + 4), a + 4);
+    store4(p + (turned ? 4 * j : 8 * j), a);
+    store4(p + (turned ? P + 4 * j : 8 * j + 4), a + 4);
   } else {
 #pragma unroll
     for (int v = 0; v < 8; ++v) p[element(j, v, P, cross)] = ET<T>::from_f(x[v]);

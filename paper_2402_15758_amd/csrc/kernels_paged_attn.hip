@@ -10,8 +10,6 @@
 
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f;
-
 // ---- which queries, which positions ----------------------------------------------
 struct QueryBlock {
   int b, row0, n;           // sequence, its first row, positions before it
