@@ -15,8 +15,12 @@ namespace {
 
 // 2^(y / 32): y = n + f, |f| <= 1/2, 2^(n / 32) = 2^(n >> 5) times a table's
 // entry, and Taylor's series of e^(f ln 2 / 32) up to the fifth power (the next is below
-// 2^-48).  A weight is exp((z - m) / T) = 2^(y / 32) with y = (z - m) 32 / (T ln 2): the
-// sum of a row's errors stays below 2^-47 of its weights.  0 below 2^-1075.
+// 2^-48).  A weight is exp((z - m) / T) = 2^(y / 32) with y = (z - m) 32 / (T ln 2), 0 below
+// 2^-1075.  Its relative error stays below 2^-48 + |y| 2^-56, of which most is the scale's,
+// as if T were off by 2^-51 of itself, and a row's weights share that.  m is a row's or a
+// part's largest logit: where a weight counts |y| is below 1000 then and the error below
+// 2^-46.  Sums by the table of bf16 exponentials have m = 0 and |y| up to 23700, whose own
+// rounding adds 2^-44 to each weight.
 __device__ const double POW32[32] = {
     0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
     0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
