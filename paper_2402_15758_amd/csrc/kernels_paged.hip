@@ -57,7 +57,7 @@ __device__ __forceinline__ void store4(bf16_t* p, const float* x) {
 // pairs: eight values in a row.  VEC: both are runs of four values (P a multiple of
 // 4); else a value at a time.
 // Bound by the bytes of many rows and by the launch of few: 2044 32-bit rows of 48 heads
-// into bf16 (76 MB) 17.5 us, 4.4 TB/s; one row 2.8 us, eight normed rows 3.3.
+// into bf16 (76 MB) 17.6 us, 4.35 TB/s; one row 2.9 us, eight normed rows 3.3.
 // Elements of value v (0 .. 7) of lane j: pair v / 2 in either layout.
 __device__ __forceinline__ int element(int j, int v, int P, bool cross) {
   const int u = 4 * j + (v >> 1);
